@@ -18,6 +18,10 @@ the C names of include/zo.h:
                                                         the same over a list of separate tensors
   zo_gen_bits(out, tile_begin, seed, step, group)       raw probe blocks (uint8 tensor)
 
+The operators of a decode step (include/zo_decode.h) are bound in decode.py and reached here under their C
+names as well: zo_norm_rotate, zo_norm_rotate_back, zo_norm_rotate_put, zo_rotary_turns, zo_cache_attend,
+zo_cache_copy, zo_draw, ZoPages. They need torch, so they are loaded at their first use.
+
 If libzo.so has not been built the import succeeds but every call raises ZoLibraryMissing:
 there is no fallback implementation.
 """
@@ -275,3 +279,17 @@ def zo_set_max_blocks(max_blocks):
 
 def zo_version():
     return _lib().zo_version().decode()
+
+
+_DECODE = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_cache_attend",
+           "zo_cache_copy", "zo_draw", "ZoPages", "ZO_ERR_MEMORY", "ZO_ERR_FULL", "ZO_DIM_MAX", "ZO_ROTARY_LINEAR",
+           "ZO_ROTARY_BASE", "ZO_ROTARY_BANDS")
+
+
+def __getattr__(name):
+    if name in _DECODE:
+        from . import decode
+        for n in _DECODE:  # later uses find them here
+            globals()[n] = getattr(decode, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

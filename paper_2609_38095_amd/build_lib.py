@@ -1,4 +1,4 @@
-"""Compile libzo.so for gfx950 in-tree (hipcc for the HIP sweep, the host compiler for the rest),
+"""Compile libzo.so for gfx950 in-tree (hipcc for the HIP kernels, the host compiler for the rest),
 and libzo_calib.so, the read-modify-write ceiling probe the benchmark measures beside it (the
 sweeps' streaming loop with the probe work replaced by an XOR)."""
 
@@ -43,7 +43,10 @@ def build(verbose=False):
     objs, cmds = [], []
     for name in sorted(os.listdir(CSRC)):
         src = os.path.join(CSRC, name)
-        if name.endswith(".hip"):
+        if name.endswith(".hip") and name != "zo_sweep.hip":
+            objs.append(os.path.join(BUILD, name + ".o"))
+            cmds.append([HIPCC, *DEVICE_FLAGS, "-I", INCLUDE, "-c", src, "-o", objs[-1]])
+        elif name.endswith(".hip"):
             for part in range(SWEEP_PARTS):
                 objs.append(os.path.join(BUILD, f"{name}.{part}.o"))
                 cmds.append([HIPCC, *DEVICE_FLAGS, f"-DZO_PART={part}", "-I", INCLUDE, "-c", src, "-o", objs[-1]])

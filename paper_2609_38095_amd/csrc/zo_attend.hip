@@ -1,0 +1,542 @@
+// Attention of one new token of each sequence over the paged cache, for gfx950.
+//
+// Mathematics. One pass over the cached tokens with a running maximum m and sum l:
+// x_j = scale log2(e) q . k_j, p_j = 2^(x_j - m), l = sum p_j, o = sum p_j v_j; a larger maximum scales l
+// and o by 2^(m - m'). The maximum is raised only when a score passes it by more than 2^8, which
+// fp32 has room for, so that the usual tile neither exchanges maxima between lanes nor rescales o.
+// Parts of a sequence join by the same rule.
+//
+// Split. An item is one sequence, one key head and up to 16 of its query heads: they read the same
+// keys, so they are the columns of one matrix product, and the cache is read once. Every item is cut
+// into tiles of 32 (bf16) or 16 (fp32) tokens; all tiles of the call, in order, are dealt out in
+// equal runs to the workers, each of them a wave on its own (no barrier, no LDS in the loop). Lengths
+// are known on the device alone, so each worker adds them up itself. A run that covers a whole item
+// writes its output; other runs leave (m, l, o) in the workspace, at most two parts for each worker,
+// and join_kernel joins them.
+//
+// Tile. S^T = K Q^T and O^T = V^T P^T on the matrix cores. The contraction's index may be permuted if both
+// operands are, which lets every operand stay where its loads or the product before put it:
+//   - lane (r = lane % 16, g = lane / 16) loads key row r, 16 bytes at 16 g + 64 c: an operand as it is;
+//   - S^T leaves head r, keys 4 g .. 4 g + 3 of each 16 in lane (r, g): the second product's operand;
+//   - the values of those keys are loaded with lane r holding dims r D/16 .. (r + 1) D/16 - 1, whole
+//     rows by 16 lanes; for bf16 pairs of keys are put together by byte permutes (both members are in
+//     the lane); output row r of product e is then dim r D/16 + e.
+// Nothing passes through LDS. fp32 takes the fp32 matrix instructions: its products are exact to fp32.
+//
+// Bound by HBM: the keys and values of the live tokens, once.
+
+#include <algorithm>
+#include <cmath>
+
+#include "zo_checks.h"
+#include "zo_lanes.h"
+
+namespace zo {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr uint32_t kThreads = 256;
+constexpr uint32_t kWave = 64;
+constexpr float kLazy = 8.0f;  // how far (in powers of two) scores may pass the maximum in use
+
+struct Attend {
+  const char *q, *k, *v;
+  char* out;
+  float* lse;
+  float* parts;
+  const int32_t* ids;
+  const int32_t* lengths;
+  int64_t q_seq, q_head, out_seq, out_head, page_stride, head_stride, token_stride, table_stride;
+  uint32_t seqs, width, pages, page_tokens, heads, group, group_blocks, dim, workers, part_row;
+  float scale;  // times log2(e)
+};
+
+// A value that all lanes of a wave hold, in scalar registers.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ uint64_t uniform(uint64_t v) {
+  return static_cast<uint64_t>(uniform(static_cast<uint32_t>(v >> 32))) << 32 | uniform(static_cast<uint32_t>(v));
+}
+
+// The tokens of a sequence that the table can hold.
+__device__ __forceinline__ uint32_t live_tokens(const Attend& a, uint32_t seq) {
+  const int64_t room = static_cast<int64_t>(a.width) * a.page_tokens;
+  const int64_t n = a.lengths[seq];
+  return static_cast<uint32_t>(n < 0 ? 0 : n > room ? room : n);
+}
+
+// Tiles before each thread's sequences. Thread t counts sequences [t each, (t + 1) each).
+struct Deal {
+  uint64_t total;  // tiles of all items
+  uint32_t each;
+};
+
+template <uint32_t kTile>
+__device__ Deal deal(const Attend& a, uint64_t* before) {
+  __shared__ uint64_t wave_sum[kThreads / kWave];
+  Deal d;
+  d.each = (a.seqs + kThreads - 1) / kThreads;
+  uint64_t mine = 0;
+  for (uint32_t i = 0; i < d.each; ++i) {
+    const uint32_t s = threadIdx.x * d.each + i;
+    if (s < a.seqs) mine += (live_tokens(a, s) + kTile - 1) / kTile;
+  }
+  uint64_t upto = mine;
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const uint64_t lower = __shfl_up(upto, m, 64);
+    if (threadIdx.x % 64 >= static_cast<uint32_t>(m)) upto += lower;
+  }
+  if (threadIdx.x % 64 == 63) wave_sum[threadIdx.x / 64] = upto;
+  __syncthreads();
+  uint64_t offset = 0, all = 0;
+  for (uint32_t w = 0; w < kThreads / kWave; ++w) {
+    if (w < threadIdx.x / 64) offset += wave_sum[w];
+    all += wave_sum[w];
+  }
+  const uint64_t items = static_cast<uint64_t>(a.heads) * a.group_blocks;
+  before[threadIdx.x] = (offset + upto - mine) * items;
+  d.total = uniform(all * items);
+  __syncthreads();
+  return d;
+}
+
+// The first tile of worker w: total tiles in equal runs, the first ones a tile longer.
+struct Runs {
+  uint64_t each, longer;
+  uint32_t workers;
+  __device__ Runs(uint64_t total, uint32_t most) {
+    workers = total < most ? static_cast<uint32_t>(total) : most;
+    if (workers == 0) workers = 1;
+    each = (total >> 32) == 0 ? static_cast<uint32_t>(total) / workers : total / workers;
+    longer = total - each * workers;
+  }
+  __device__ uint64_t first(uint32_t w) const { return w * each + (w < longer ? w : longer); }
+  __device__ uint32_t worker_of(uint64_t tile) const {
+    const uint64_t head = longer * (each + 1);
+    if (tile < head) return static_cast<uint32_t>((tile >> 32) == 0 && (each >> 31) == 0 ? static_cast<uint32_t>(tile) / (static_cast<uint32_t>(each) + 1) : tile / (each + 1));
+    const uint64_t rest = tile - head;
+    return static_cast<uint32_t>(longer + ((rest >> 32) == 0 && (each >> 32) == 0 ? static_cast<uint32_t>(rest) / static_cast<uint32_t>(each) : rest / each));
+  }
+};
+
+// A part in the workspace: for each of the item's query heads a row [m, l, -, -, o[dim rounded up to 4]].
+__device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint32_t slot, uint32_t group) {
+  return a.parts + (static_cast<size_t>(worker) * 2 + slot) * group * a.part_row;
+}
+
+template <class S>
+struct Mfma;
+
+// bf16: tiles of 32 keys, 16 x 16 x 32 products.
+template <>
+struct Mfma<BF16> {
+  static constexpr uint32_t kTile = 32, kSubs = 2, kLoadDims = 8;
+};
+// fp32: tiles of 16 keys, 16 x 16 x 4 products.
+template <>
+struct Mfma<F32> {
+  static constexpr uint32_t kTile = 16, kSubs = 1, kLoadDims = 4;
+};
+
+__device__ __forceinline__ f32x4 mul_bf16(u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// kDim: the head size, or (kAny) the size that it is padded to with zeros; kAny also takes any
+// page size and any strides, with one lookup and one bounds check for each element's row.
+template <class S, uint32_t kDim, bool kAny>
+__global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim > 128 ? 2 : kDim > 64 ? 3 : 4)) attend_kernel(const Attend a) {
+  typedef typename S::storage T;
+  constexpr uint32_t kTile = Mfma<S>::kTile, kSubs = Mfma<S>::kSubs, kLoad = Mfma<S>::kLoadDims;
+  constexpr uint32_t kKeyLoads = kDim / (4 * kLoad);      // 16-byte loads of a key row for each lane
+  constexpr uint32_t kLaneDims = kDim / 16;               // dims of a value row for each lane
+  constexpr uint32_t kValWords = kLaneDims * sizeof(T) / 4;
+  constexpr uint32_t kKeys = 4 * kSubs;                   // keys of a tile for each lane
+  __shared__ uint64_t before[kThreads];
+  const Deal d = deal<kTile>(a, before);
+  const Runs runs(d.total, a.workers);
+  const uint32_t worker = uniform(blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave);
+  const uint32_t lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
+  if (worker >= runs.workers) return;
+  uint64_t at = runs.first(worker);
+  const uint64_t end = runs.first(worker + 1);
+  if (at >= end) return;
+
+  // the sequence that tile `at` lies in: the last thread's block that begins at or before it
+  uint32_t block = 0;
+#pragma unroll
+  for (uint32_t step = kThreads / 2; step > 0; step /= 2)
+    if (before[block + step] <= at) block += step;
+  block = uniform(block);
+  uint32_t seq = block * d.each;
+  const uint32_t items = a.heads * a.group_blocks;
+  uint64_t seq_first = uniform(before[block]);  // its first tile
+
+  while (at < end) {
+    uint32_t len, tiles;
+    for (;;) {  // `at` < the total: a sequence holds it
+      len = uniform(live_tokens(a, seq));
+      tiles = (len + kTile - 1) / kTile;
+      if (at < seq_first + static_cast<uint64_t>(tiles) * items) break;
+      seq_first += static_cast<uint64_t>(tiles) * items;
+      ++seq;
+    }
+    const uint64_t in_seq = at - seq_first;
+    const uint32_t item = (in_seq >> 32) == 0 ? static_cast<uint32_t>(in_seq) / tiles : static_cast<uint32_t>(in_seq / tiles);
+    const uint64_t item_first = seq_first + static_cast<uint64_t>(item) * tiles;
+    const uint32_t t_begin = static_cast<uint32_t>(at - item_first);
+    const uint32_t t_end = end - item_first < tiles ? static_cast<uint32_t>(end - item_first) : tiles;
+    const uint32_t head = item / a.group_blocks, gb = item - head * a.group_blocks;
+    const uint32_t in_group = min(16u, a.group - gb * 16);  // query heads of this item
+    const uint32_t q_head0 = head * a.group + gb * 16;
+    const int32_t* ids = a.ids + static_cast<int64_t>(seq) * a.table_stride;
+    const T* kp = reinterpret_cast<const T*>(a.k) + static_cast<int64_t>(head) * a.head_stride;
+    const T* vp = reinterpret_cast<const T*>(a.v) + static_cast<int64_t>(head) * a.head_stride;
+
+    // queries of head r, zeros for columns without one
+    u32x4 q[kKeyLoads];
+    {
+      const T* qp = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(seq) * a.q_seq +
+                    static_cast<int64_t>(q_head0 + (r < in_group ? r : 0)) * a.q_head;
+#pragma unroll
+      for (uint32_t c = 0; c < kKeyLoads; ++c) {
+        q[c] = u32x4{0, 0, 0, 0};
+        if constexpr (kAny) {
+          T tmp[kLoad] = {};
+#pragma unroll
+          for (uint32_t e = 0; e < kLoad; ++e) {
+            const uint32_t i = c * 4 * kLoad + g * kLoad + e;
+            if (r < in_group && i < a.dim) tmp[e] = qp[i];
+          }
+          __builtin_memcpy(&q[c], tmp, 16);
+        } else {
+          if (r < in_group) q[c] = *reinterpret_cast<const u32x4_any*>(qp + c * 4 * kLoad + g * kLoad);
+        }
+      }
+    }
+
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o[kLaneDims];
+#pragma unroll
+    for (uint32_t e = 0; e < kLaneDims; ++e) o[e] = f32x4{0, 0, 0, 0};
+
+    uint32_t slot = 0, row = 0;  // page and row of the tile's first token (the fast form walks them)
+    if constexpr (!kAny) {
+      slot = t_begin * kTile / a.page_tokens;
+      row = t_begin * kTile - slot * a.page_tokens;
+    }
+    for (uint32_t t = t_begin; t < t_end; ++t) {
+      u32x4 kr[kSubs][kKeyLoads];
+      uint32_t vr[kKeys][kValWords];
+      bool live[kKeys];     // of key 4 g + i of each 16
+      bool whole = true;    // every key of the tile is live
+      if constexpr (kAny) {
+        whole = false;
+#pragma unroll
+        for (uint32_t s = 0; s < kSubs; ++s) {
+          const uint32_t j = t * kTile + s * 16 + r;
+          const uint32_t p = j / a.page_tokens;
+          const int32_t id = j < len ? ids[p] : -1;
+          const bool there = static_cast<uint32_t>(id) < a.pages;
+          const T* src = kp + (there ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
+#pragma unroll
+          for (uint32_t c = 0; c < kKeyLoads; ++c) {
+            T tmp[kLoad] = {};
+#pragma unroll
+            for (uint32_t e = 0; e < kLoad; ++e) {
+              const uint32_t i = c * 4 * kLoad + g * kLoad + e;
+              if (there && i < a.dim) tmp[e] = src[i];
+            }
+            __builtin_memcpy(&kr[s][c], tmp, 16);
+          }
+        }
+#pragma unroll
+        for (uint32_t i = 0; i < kKeys; ++i) {
+          const uint32_t j = t * kTile + i / 4 * 16 + g * 4 + i % 4;
+          const uint32_t p = j / a.page_tokens;
+          const int32_t id = j < len ? ids[p] : -1;
+          live[i] = static_cast<uint32_t>(id) < a.pages;
+          const T* src = vp + (live[i] ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
+          T tmp[kLaneDims] = {};
+#pragma unroll
+          for (uint32_t e = 0; e < kLaneDims; ++e)
+            if (live[i] && r * kLaneDims + e < a.dim) tmp[e] = src[r * kLaneDims + e];
+          __builtin_memcpy(vr[i], tmp, sizeof tmp);
+        }
+      } else {
+        // pages hold whole sixteens of tokens, so each 16 keys lie in one page: its address is scalar
+        uint32_t count[kSubs];
+#pragma unroll
+        for (uint32_t s = 0; s < kSubs; ++s) {
+          const uint32_t j = t * kTile + s * 16;
+          const int32_t id = j < len ? static_cast<int32_t>(uniform(static_cast<uint32_t>(ids[slot]))) : -1;
+          const bool there = static_cast<uint32_t>(id) < a.pages;
+          count[s] = there ? min(16u, len - j) : 0u;
+          // rows behind the length are inside the page, and masked below; an absent page's are read from page 0
+          const int64_t base = (there ? id : 0) * a.page_stride + static_cast<int64_t>(row) * a.token_stride;
+          const uint32_t step = static_cast<uint32_t>(a.token_stride);
+          const T *ks = kp + base, *vs = vp + base;
+#pragma unroll
+          for (uint32_t c = 0; c < kKeyLoads; ++c)
+            kr[s][c] = *reinterpret_cast<const u32x4_any*>(ks + (r * step + g * kLoad) + c * 4 * kLoad);
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            const T* src = vs + ((g * 4 + i) * step + r * kLaneDims);
+            if constexpr (kValWords == 2) {
+              typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+              const u32x2_any w = *reinterpret_cast<const u32x2_any*>(src);
+              vr[s * 4 + i][0] = w.x;
+              vr[s * 4 + i][1] = w.y;
+            } else {
+#pragma unroll
+              for (uint32_t w = 0; w < kValWords; w += 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
+                vr[s * 4 + i][w] = x.x;
+                vr[s * 4 + i][w + 1] = x.y;
+                vr[s * 4 + i][w + 2] = x.z;
+                vr[s * 4 + i][w + 3] = x.w;
+              }
+            }
+          }
+          whole = whole && count[s] == 16;
+          row += 16;
+          if (row == a.page_tokens) {
+            row = 0;
+            ++slot;
+          }
+        }
+        if (!whole) {
+#pragma unroll
+          for (uint32_t i = 0; i < kKeys; ++i) live[i] = g * 4 + i % 4 < count[i / 4];
+        }
+      }
+
+      // scores of head r with keys 4 g .. 4 g + 3 of each 16
+      float x[kKeys];
+#pragma unroll
+      for (uint32_t s = 0; s < kSubs; ++s) {
+        f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t c = 0; c < kKeyLoads; ++c) {
+          if constexpr (sizeof(T) == 2) {
+            acc = mul_bf16(kr[s][c], q[c], acc);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kr[s][c][e]), __uint_as_float(q[c][e]), acc, 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[s * 4 + i] = acc[i] * a.scale;
+      }
+      if (!whole) {
+#pragma unroll
+        for (uint32_t i = 0; i < kKeys; ++i) {
+          x[i] = live[i] ? x[i] : -INFINITY;
+#pragma unroll
+          for (uint32_t w = 0; w < kValWords; ++w) vr[i][w] = live[i] ? vr[i][w] : 0u;  // 0 times whatever lies there
+        }
+      }
+      float top = x[0];
+#pragma unroll
+      for (uint32_t i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
+      if (__any(top > m + kLazy)) {
+        top = fmaxf(top, m);
+        top = fmaxf(top, __shfl_xor(top, 16, 64));
+        top = fmaxf(top, __shfl_xor(top, 32, 64));
+        const float scale = top == m ? 1.0f : exp2f(m - top);  // m = -inf: 0
+        l *= scale;
+#pragma unroll
+        for (uint32_t e = 0; e < kLaneDims; ++e) o[e] *= scale;
+        m = top;
+      }
+      const float ref = m == -INFINITY ? 0.0f : m;
+      float p[kKeys];
+#pragma unroll
+      for (uint32_t i = 0; i < kKeys; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(x[i] - ref);
+        l += p[i];
+      }
+
+      if constexpr (sizeof(T) == 2) {
+        // weights as a sum of two bf16: 16 bits of each, so that only the output is rounded to 8
+        u32x4 hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p0 = p[2 * i], p1 = p[2 * i + 1];
+          const float h0 = __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u), h1 = __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u);
+          hi[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+          lo[i] = pack_bf16x2(p0 - h0, p1 - h1);
+        }
+#pragma unroll
+        for (uint32_t w = 0; w < kValWords; ++w) {
+          u32x4 even, odd;  // dims 2 w and 2 w + 1 of the lane, keys in pairs
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            even[i] = __builtin_amdgcn_perm(vr[2 * i + 1][w], vr[2 * i][w], 0x05040100u);
+            odd[i] = __builtin_amdgcn_perm(vr[2 * i + 1][w], vr[2 * i][w], 0x07060302u);
+          }
+          o[2 * w] = mul_bf16(even, lo, mul_bf16(even, hi, o[2 * w]));
+          o[2 * w + 1] = mul_bf16(odd, lo, mul_bf16(odd, hi, o[2 * w + 1]));
+        }
+      } else {
+#pragma unroll
+        for (uint32_t e = 0; e < kLaneDims; ++e)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vr[i][e]), p[i], o[e], 0, 0, 0);
+      }
+    }
+    l += __shfl_xor(l, 16, 64);
+    l += __shfl_xor(l, 32, 64);
+
+    // lane (r, g) holds head r, dims (4 g + i) kLaneDims + e
+    if (t_begin == 0 && t_end == tiles) {
+      if (r < in_group) {
+        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
+        T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq) * a.out_seq + static_cast<int64_t>(q_head0 + r) * a.out_head;
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t e = 0; e < kLaneDims; ++e) {
+            const uint32_t dim = (4 * g + i) * kLaneDims + e;
+            if (!kAny || dim < a.dim) S::store1(op + dim, o[e][i] * inv);
+          }
+        if (a.lse && g == 0)
+          a.lse[static_cast<size_t>(seq) * a.heads * a.group + q_head0 + r] = l > 0.0f || l != l ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+      }
+    } else if (r < in_group) {
+      const uint32_t part_heads = min(16u, a.group);
+      float* part = part_at(a, worker, at == runs.first(worker) ? 0 : 1, part_heads) + static_cast<size_t>(r) * a.part_row;
+      if (g == 0) {
+        part[0] = m;
+        part[1] = l;
+      }
+#pragma unroll
+      for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+        for (uint32_t e = 0; e < kLaneDims; ++e) {
+          const uint32_t dim = (4 * g + i) * kLaneDims + e;
+          if (!kAny || dim < a.dim) part[4 + dim] = o[e][i];
+        }
+    }
+    at = item_first + t_end;
+  }
+}
+
+// One workgroup for each item: joins its parts, or writes zeros for an empty sequence.
+template <class S>
+__global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
+  typedef typename S::storage T;
+  constexpr uint32_t kTile = Mfma<S>::kTile;
+  __shared__ uint64_t before[kThreads];
+  __shared__ uint64_t found;
+  const Deal d = deal<kTile>(a, before);
+  const Runs runs(d.total, a.workers);
+  const uint32_t items = a.heads * a.group_blocks;
+  const uint32_t seq = blockIdx.x / items, item = blockIdx.x - seq * items;
+  if (threadIdx.x == 0) {
+    uint64_t first = before[seq / d.each];
+    for (uint32_t s = seq / d.each * d.each; s < seq; ++s) first += static_cast<uint64_t>((live_tokens(a, s) + kTile - 1) / kTile) * items;
+    found = first;
+  }
+  __syncthreads();
+  const uint32_t tiles = (live_tokens(a, seq) + kTile - 1) / kTile;
+  const uint32_t head = item / a.group_blocks, gb = item - head * a.group_blocks;
+  const uint32_t in_group = min(16u, a.group - gb * 16), q_head0 = head * a.group + gb * 16;
+  const uint64_t first = found + static_cast<uint64_t>(item) * tiles;
+  uint32_t w0 = 0, w1 = 0;
+  if (tiles > 0) {
+    w0 = runs.worker_of(first);
+    w1 = runs.worker_of(first + tiles - 1);
+    if (w0 == w1) return;  // one worker had all of it
+  }
+  const uint32_t slot0 = tiles > 0 && runs.first(w0) == first ? 0 : 1;  // of the first part; the others began their runs
+  const uint32_t part_heads = min(16u, a.group);
+  for (uint32_t i = threadIdx.x; i < in_group * a.dim; i += kThreads) {
+    const uint32_t h = i / a.dim, dim = i - h * a.dim;
+    float m = -INFINITY, l = 0.0f, o = 0.0f;
+    if (tiles > 0) {
+      for (uint32_t w = w0; w <= w1; ++w) m = fmaxf(m, part_at(a, w, w == w0 ? slot0 : 0, part_heads)[h * a.part_row]);
+      const float ref = m == -INFINITY ? 0.0f : m;
+      for (uint32_t w = w0; w <= w1; ++w) {
+        const float* part = part_at(a, w, w == w0 ? slot0 : 0, part_heads) + static_cast<size_t>(h) * a.part_row;
+        const float scale = exp2f(part[0] - ref);
+        l += part[1] * scale;
+        o += part[4 + dim] * scale;
+      }
+    }
+    const bool any = l > 0.0f || l != l;
+    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq) * a.out_seq + static_cast<int64_t>(q_head0 + h) * a.out_head;
+    S::store1(op + dim, any ? o / l : 0.0f);
+    if (a.lse && dim == 0)
+      a.lse[static_cast<size_t>(seq) * a.heads * a.group + q_head0 + h] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+  }
+}
+
+template <class S>
+int attend(const Attend& a, hipStream_t st) {
+  const dim3 grid((a.workers + kThreads / kWave - 1) / (kThreads / kWave)), block(kThreads);
+  // a page of whole sixteens, in which 32-bit offsets reach every row, and a head size with a kernel
+  const int64_t reach = 16 * a.token_stride + a.dim;
+  const bool fast = a.page_tokens % 16 == 0 && reach < (int64_t{1} << 28);
+  if (fast && a.dim == 64)
+    attend_kernel<S, 64, false><<<grid, block, 0, st>>>(a);
+  else if (fast && a.dim == 128)
+    attend_kernel<S, 128, false><<<grid, block, 0, st>>>(a);
+  else if (fast && a.dim == 256)
+    attend_kernel<S, 256, false><<<grid, block, 0, st>>>(a);
+  else if (a.dim <= 64)
+    attend_kernel<S, 64, true><<<grid, block, 0, st>>>(a);
+  else if (a.dim <= 128)
+    attend_kernel<S, 128, true><<<grid, block, 0, st>>>(a);
+  else
+    attend_kernel<S, 256, true><<<grid, block, 0, st>>>(a);
+  int rc = launched();
+  if (rc != ZO_OK) return rc;
+  join_kernel<S><<<dim3(a.seqs * a.heads * a.group_blocks), block, 0, st>>>(a);
+  return launched();
+}
+
+}  // namespace
+}  // namespace zo
+
+extern "C" int zo_cache_attend(const zo_attend* p, void* stream) {
+  using namespace zo;
+  if (p == nullptr) return ZO_ERR_NULL;
+  const int rc = check_attend(*p);
+  if (rc != ZO_OK) return rc;
+  if (p->table.seqs == 0 || p->q_heads == 0) return ZO_OK;
+  Attend a;
+  a.q = static_cast<const char*>(p->q.data);
+  a.k = static_cast<const char*>(p->cache.k);
+  a.v = static_cast<const char*>(p->cache.v);
+  a.out = static_cast<char*>(p->out.data);
+  a.lse = p->lse;
+  a.parts = static_cast<float*>(p->work);
+  a.ids = p->table.ids;
+  a.lengths = p->lengths;
+  a.q_seq = p->q.token_stride;
+  a.q_head = p->q.head_stride;
+  a.out_seq = p->out.token_stride;
+  a.out_head = p->out.head_stride;
+  a.page_stride = p->cache.page_stride;
+  a.head_stride = p->cache.head_stride;
+  a.token_stride = p->cache.token_stride;
+  a.table_stride = p->table.stride;
+  a.seqs = p->table.seqs;
+  a.width = p->table.width;
+  a.pages = p->cache.pages;
+  a.page_tokens = p->cache.page_tokens;
+  a.heads = p->cache.heads;
+  a.group = p->q_heads / p->cache.heads;
+  a.group_blocks = (a.group + 15) / 16;
+  a.dim = p->cache.dim;
+  a.workers = attend_workers(a.seqs, p->q_heads, a.heads, a.dim);
+  a.part_row = (a.dim + 3) / 4 * 4 + 4;
+  a.scale = p->scale * 1.4426950408889634f;
+  (void)hipGetLastError();
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  return p->dtype == ZO_F32 ? attend<F32>(a, st) : attend<BF16>(a, st);
+}

@@ -9,6 +9,7 @@
 #include <cstdint>
 
 #include "zo.h"
+#include "zo_decode.h"
 
 extern "C" {
 
@@ -52,6 +53,8 @@ const char* zo_strerror(int status) {
     case ZO_ERR_ARG: return "invalid argument (dtype, alignment, probe count or index range)";
     case ZO_ERR_NONFINITE: return "non-finite eps, lr, loss or coefficient";
     case ZO_ERR_HIP: return "the HIP runtime refused the launch";
+    case ZO_ERR_MEMORY: return "host memory ran out";
+    case ZO_ERR_FULL: return "the page book has no page left";
     default: return "unknown status";
   }
 }
