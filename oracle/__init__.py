@@ -15,6 +15,7 @@ Modules:
               fused transitions perturb2 / update_restore
   coeffs   -- curvature, alpha-saturated weight and per-probe coefficients
   step     -- one single-device step composed from the above
+  decode   -- the operators of a decode step (norms and rotation, cached attention, the draw of a token)
 
 Every function is pinned by CPU tests against values the paper or mathematics fixes;
 see tests/test_oracle_*.py. Floating point is float64 except where the storage format

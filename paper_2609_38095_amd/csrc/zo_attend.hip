@@ -366,8 +366,8 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p0 = p[2 * i], p1 = p[2 * i + 1];
-          const float h0 = __uint_as_float(__float_as_uint(p0) & 0xFFFF0000u), h1 = __uint_as_float(__float_as_uint(p1) & 0xFFFF0000u);
-          hi[i] = __builtin_amdgcn_perm(__float_as_uint(p1), __float_as_uint(p0), 0x07060302u);
+          hi[i] = pack_bf16x2(p0, p1);
+          const float h0 = __uint_as_float(hi[i] << 16), h1 = __uint_as_float(hi[i] & 0xFFFF0000u);
           lo[i] = pack_bf16x2(p0 - h0, p1 - h1);
         }
 #pragma unroll
