@@ -9,9 +9,10 @@
 // Split. An item is one sequence, one key head and up to 16 of its query heads: they read the same
 // keys, so they are the columns of one matrix product, and the cache is read once. Every item is cut
 // into tiles of 32 (bf16) or 16 (fp32) tokens; all tiles of the call, in order, are dealt out in
-// equal runs to the workers, each of them a wave on its own (no barrier, no LDS in the loop). Lengths
-// are known on the device alone, so each worker adds them up itself. A run that covers a whole item
-// writes its output; other runs leave (m, l, o) in the workspace, at most two parts for each worker,
+// equal runs to the workers, each of them a wave on its own (no barrier, no LDS in the loop). Lengths are
+// known on the device alone, so each worker adds them up itself. A run that covers a whole item writes
+// its output; other runs leave (m, l, o) in the workspace, at most two parts for each worker and one for a
+// workgroup whose four runs lie in one item,
 // and join_kernel joins them.
 //
 // Tile. S^T = K Q^T and O^T = V^T P^T on the matrix cores. The contraction's index may be permuted if both
@@ -38,13 +39,22 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kThreads = 256;
-constexpr uint32_t kWave = 64;
+constexpr uint32_t kWave = 64, kWaves = kThreads / kWave;
 constexpr float kLazy = 8.0f;  // how far (in powers of two) scores may pass the maximum in use
+
+// Where an item's parts are: those of workers first .. last, the first one's in `slot`, the others' in slot 0;
+// the waves of workgroups group0 .. group1 - 1 have theirs together, with the workgroup's first wave.
+// first = last: that worker wrote the output. Written by the worker of the item's last tile.
+struct Parts {
+  uint32_t first_slot;  // 2 first + slot
+  uint32_t last, group0, group1;
+};
 
 struct Attend {
   const char *q, *k, *v;
   char* out;
   float* lse;
+  Parts* items;
   float* parts;
   const int32_t* ids;
   const int32_t* lengths;
@@ -74,7 +84,7 @@ struct Deal {
 
 template <uint32_t kTile>
 __device__ Deal deal(const Attend& a, uint64_t* before) {
-  __shared__ uint64_t wave_sum[kThreads / kWave];
+  __shared__ uint64_t wave_sum[kWaves];
   Deal d;
   d.each = (a.seqs + kThreads - 1) / kThreads;
   uint64_t mine = 0;
@@ -91,7 +101,7 @@ __device__ Deal deal(const Attend& a, uint64_t* before) {
   if (threadIdx.x % 64 == 63) wave_sum[threadIdx.x / 64] = upto;
   __syncthreads();
   uint64_t offset = 0, all = 0;
-  for (uint32_t w = 0; w < kThreads / kWave; ++w) {
+  for (uint32_t w = 0; w < kWaves; ++w) {
     if (w < threadIdx.x / 64) offset += wave_sum[w];
     all += wave_sum[w];
   }
@@ -102,6 +112,11 @@ __device__ Deal deal(const Attend& a, uint64_t* before) {
   return d;
 }
 
+// Floor of n / d for n below 2^52: exact, since quotients of neighbours are further apart than an fp64 rounding.
+__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) {
+  return static_cast<uint64_t>(static_cast<double>(n) / static_cast<double>(d));
+}
+
 // The first tile of worker w: total tiles in equal runs, the first ones a tile longer.
 struct Runs {
   uint64_t each, longer;
@@ -109,21 +124,41 @@ struct Runs {
   __device__ Runs(uint64_t total, uint32_t most) {
     workers = total < most ? static_cast<uint32_t>(total) : most;
     if (workers == 0) workers = 1;
-    each = (total >> 32) == 0 ? static_cast<uint32_t>(total) / workers : total / workers;
+    each = uniform(quotient(total, workers));
     longer = total - each * workers;
   }
   __device__ uint64_t first(uint32_t w) const { return w * each + (w < longer ? w : longer); }
   __device__ uint32_t worker_of(uint64_t tile) const {
-    const uint64_t head = longer * (each + 1);
-    if (tile < head) return static_cast<uint32_t>((tile >> 32) == 0 && (each >> 31) == 0 ? static_cast<uint32_t>(tile) / (static_cast<uint32_t>(each) + 1) : tile / (each + 1));
-    const uint64_t rest = tile - head;
-    return static_cast<uint32_t>(longer + ((rest >> 32) == 0 && (each >> 32) == 0 ? static_cast<uint32_t>(rest) / static_cast<uint32_t>(each) : rest / each));
+    const uint64_t head = longer * (each + 1);  // tiles of the longer runs
+    return static_cast<uint32_t>(tile < head ? quotient(tile, each + 1) : longer + quotient(tile - head, each));
   }
 };
 
 // A part in the workspace: for each of the item's query heads a row [m, l, -, -, o[dim rounded up to 4]].
 __device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint32_t slot, uint32_t group) {
   return a.parts + (static_cast<size_t>(worker) * 2 + slot) * group * a.part_row;
+}
+
+// Waves for each SIMD: as many as the tile's keys and values (64 registers of a lane in the larger forms), the
+// sums and the queries leave room for without spilling into the loop. Loads in flight come from the waves:
+// asking for the next tile's before this one's use, at fewer waves, measured the same (bf16, 128 dims, 0.56 GB:
+// 98 us either way) or slower, and a spilled form 133.
+template <class S>
+constexpr uint32_t waves_for(uint32_t dim) {
+  return sizeof(typename S::storage) == 2 ? (dim > 128 ? 2 : dim > 64 ? 3 : 4) : (dim > 128 ? 1 : dim > 64 ? 2 : 4);
+}
+
+// Four dims of a head's output from its sums, and its log-sum once.
+template <class S>
+__device__ __forceinline__ void write_head(const Attend& a, uint32_t seq, uint32_t q_head, uint32_t dim, float m, float l, f32x4 o) {
+  typedef typename S::storage T;
+  const bool any = l > 0.0f || l != l;
+  T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq) * a.out_seq + static_cast<int64_t>(q_head) * a.out_head;
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i)
+    if (dim + i < a.dim) S::store1(op + dim + i, any ? o[i] / l : 0.0f);
+  if (a.lse && dim == 0)
+    a.lse[static_cast<size_t>(seq) * a.heads * a.group + q_head] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
 template <class S>
@@ -147,21 +182,24 @@ __device__ __forceinline__ f32x4 mul_bf16(u32x4 a, u32x4 b, f32x4 c) {
 // kDim: the head size, or (kAny) the size that it is padded to with zeros; kAny also takes any
 // page size and any strides, with one lookup and one bounds check for each element's row.
 template <class S, uint32_t kDim, bool kAny>
-__global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim > 128 ? 2 : kDim > 64 ? 3 : 4)) attend_kernel(const Attend a) {
+__global__ void __launch_bounds__(kThreads, kAny ? (kDim > 128 ? 1 : 2) : waves_for<S>(kDim)) attend_kernel(const Attend a) {
   typedef typename S::storage T;
   constexpr uint32_t kTile = Mfma<S>::kTile, kSubs = Mfma<S>::kSubs, kLoad = Mfma<S>::kLoadDims;
   constexpr uint32_t kKeyLoads = kDim / (4 * kLoad);      // 16-byte loads of a key row for each lane
   constexpr uint32_t kLaneDims = kDim / 16;               // dims of a value row for each lane
   constexpr uint32_t kValWords = kLaneDims * sizeof(T) / 4;
   constexpr uint32_t kKeys = 4 * kSubs;                   // keys of a tile for each lane
+  constexpr uint32_t kRow = kDim + 4;                     // of a head's sums in LDS, shifted by 4 banks
   __shared__ uint64_t before[kThreads];
+  __shared__ float2 wave_sums[kWaves][16];
+  __shared__ __align__(16) float wave_rows[kWaves][16][kRow];
   const Deal d = deal<kTile>(a, before);
   const Runs runs(d.total, a.workers);
-  const uint32_t worker = uniform(blockIdx.x * (kThreads / kWave) + threadIdx.x / kWave);
+  const uint32_t wave = uniform(threadIdx.x / kWave), worker = blockIdx.x * kWaves + wave;
   const uint32_t lane = threadIdx.x % kWave, r = lane % 16, g = lane / 16;
   if (worker >= runs.workers) return;
-  uint64_t at = runs.first(worker);
-  const uint64_t end = runs.first(worker + 1);
+  const uint64_t begin = runs.first(worker), end = runs.first(worker + 1);
+  uint64_t at = begin;
   if (at >= end) return;
 
   // the sequence that tile `at` lies in: the last thread's block that begins at or before it
@@ -171,8 +209,16 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
     if (before[block + step] <= at) block += step;
   block = uniform(block);
   uint32_t seq = block * d.each;
-  const uint32_t items = a.heads * a.group_blocks;
+  const uint32_t items = a.heads * a.group_blocks, part_heads = min(16u, a.group);
   uint64_t seq_first = uniform(before[block]);  // its first tile
+
+  // byte offsets of the lane's share of a key row, and of value rows 4 g .. 4 g + 3, from a sixteen's first row
+  // (the fast form: 32 bits behind a scalar address)
+  const uint32_t step = static_cast<uint32_t>(a.token_stride);
+  const uint32_t key_at = (r * step + g * kLoad) * sizeof(T);
+  uint32_t value_at[4];
+#pragma unroll
+  for (uint32_t i = 0; i < 4; ++i) value_at[i] = ((g * 4 + i) * step + r * kLaneDims) * sizeof(T);
 
   while (at < end) {
     uint32_t len, tiles;
@@ -183,18 +229,134 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
       seq_first += static_cast<uint64_t>(tiles) * items;
       ++seq;
     }
-    const uint64_t in_seq = at - seq_first;
-    const uint32_t item = (in_seq >> 32) == 0 ? static_cast<uint32_t>(in_seq) / tiles : static_cast<uint32_t>(in_seq / tiles);
+    const uint32_t item = uniform(static_cast<uint32_t>(quotient(at - seq_first, tiles)));
     const uint64_t item_first = seq_first + static_cast<uint64_t>(item) * tiles;
     const uint32_t t_begin = static_cast<uint32_t>(at - item_first);
     const uint32_t t_end = end - item_first < tiles ? static_cast<uint32_t>(end - item_first) : tiles;
-    const uint32_t head = item / a.group_blocks, gb = item - head * a.group_blocks;
+    const uint32_t head = uniform(item / a.group_blocks), gb = item - head * a.group_blocks;
     const uint32_t in_group = min(16u, a.group - gb * 16);  // query heads of this item
     const uint32_t q_head0 = head * a.group + gb * 16;
     const int32_t* ids = a.ids + static_cast<int64_t>(seq) * a.table_stride;
     const T* kp = reinterpret_cast<const T*>(a.k) + static_cast<int64_t>(head) * a.head_stride;
     const T* vp = reinterpret_cast<const T*>(a.v) + static_cast<int64_t>(head) * a.head_stride;
 
+    // The fast form has the page ids of 64 sixteens of tokens at a time, one in each lane: a lookup of its
+    // own for each would wait for the loads before it.
+    int32_t lane_id = -1;
+    uint32_t lane_ids = ~0u;  // which 64 these are
+    u32x4 kr[kSubs][kKeyLoads];
+    uint32_t vr[kKeys][kValWords];
+
+    // Issues the loads of a tile's keys. Fast: pages hold whole sixteens of tokens, so each 16 keys lie in
+    // one page and its address is scalar; rows behind the length are inside the page (and masked), an
+    // absent page's are read from page 0 (and masked). row: of the tile's first token in its page.
+    const auto sub_base = [&](uint32_t t, uint32_t s, uint32_t row, uint32_t& count) {
+      const uint32_t sub = t * kSubs + s, j = sub * 16;
+      const int32_t id = __builtin_amdgcn_readlane(lane_id, sub % 64);
+      const bool there = static_cast<uint32_t>(id) < a.pages;
+      count = there ? min(16u, len - j) : 0u;
+      const uint32_t page_row = row + s * 16 < a.page_tokens ? row + s * 16 : 0;
+      return (there ? id : 0) * a.page_stride + static_cast<int64_t>(page_row) * a.token_stride;
+    };
+    const auto load_keys = [&](uint32_t t, uint32_t row) {
+      if constexpr (kAny) {
+#pragma unroll
+        for (uint32_t s = 0; s < kSubs; ++s) {
+          const uint32_t j = t * kTile + s * 16 + r;
+          const uint32_t p = j / a.page_tokens;
+          const int32_t id = j < len ? ids[p] : -1;
+          const bool there = static_cast<uint32_t>(id) < a.pages;
+          const T* src = kp + (there ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
+#pragma unroll
+          for (uint32_t c = 0; c < kKeyLoads; ++c) {
+            T tmp[kLoad] = {};
+#pragma unroll
+            for (uint32_t e = 0; e < kLoad; ++e) {
+              const uint32_t i = c * 4 * kLoad + g * kLoad + e;
+              if (there && i < a.dim) tmp[e] = src[i];
+            }
+            __builtin_memcpy(&kr[s][c], tmp, 16);
+          }
+        }
+      } else {
+        if (t * kSubs / 64 != lane_ids) {
+          lane_ids = t * kSubs / 64;
+          const uint32_t j = (lane_ids * 64 + lane) * 16;
+          lane_id = j < len ? ids[j / a.page_tokens] : -1;
+          // waited for here, once in 64, and not at every use: such a wait would take in the loads of the tile
+          asm volatile("s_waitcnt vmcnt(0)" : "+v"(lane_id));
+        }
+        uint32_t at = key_at;
+        asm volatile("" : "+v"(at));  // a 32-bit offset behind the scalar address: widened outside the loop it costs two registers
+#pragma unroll
+        for (uint32_t s = 0; s < kSubs; ++s) {
+          uint32_t count;
+          const char* ks = reinterpret_cast<const char*>(kp + sub_base(t, s, row, count));
+#pragma unroll
+          for (uint32_t c = 0; c < kKeyLoads; ++c) kr[s][c] = ld_stream(ks + at + c * 64);
+        }
+      }
+    };
+    // Issues the loads of a tile's values, and says which of the lane's keys (4 g + i of each 16) are live; all
+    // ones: every key of the tile is.
+    const auto load_values = [&](uint32_t t, uint32_t row) {
+      uint32_t live = 0;
+      if constexpr (kAny) {
+#pragma unroll
+        for (uint32_t i = 0; i < kKeys; ++i) {
+          const uint32_t j = t * kTile + i / 4 * 16 + g * 4 + i % 4;
+          const uint32_t p = j / a.page_tokens;
+          const int32_t id = j < len ? ids[p] : -1;
+          const bool there = static_cast<uint32_t>(id) < a.pages;
+          live |= there ? 1u << i : 0u;
+          const T* src = vp + (there ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
+          T tmp[kLaneDims] = {};
+#pragma unroll
+          for (uint32_t e = 0; e < kLaneDims; ++e)
+            if (there && r * kLaneDims + e < a.dim) tmp[e] = src[r * kLaneDims + e];
+          __builtin_memcpy(vr[i], tmp, sizeof tmp);
+        }
+      } else {
+        bool whole = true;
+        uint32_t count[kSubs];
+#pragma unroll
+        for (uint32_t s = 0; s < kSubs; ++s) {
+          const char* vs = reinterpret_cast<const char*>(vp + sub_base(t, s, row, count[s]));
+          whole = whole && count[s] == 16;
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            uint32_t at = value_at[i];
+            asm volatile("" : "+v"(at));
+            const char* src = vs + at;
+            if constexpr (kValWords == 2) {
+              typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+              const u32x2_any w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any*>(src));
+              vr[s * 4 + i][0] = w.x;
+              vr[s * 4 + i][1] = w.y;
+            } else {
+#pragma unroll
+              for (uint32_t w = 0; w < kValWords; w += 4) {
+                const u32x4 x = ld_stream(src + w * 4);
+                vr[s * 4 + i][w] = x.x;
+                vr[s * 4 + i][w + 1] = x.y;
+                vr[s * 4 + i][w + 2] = x.z;
+                vr[s * 4 + i][w + 3] = x.w;
+              }
+            }
+          }
+        }
+        live = ~0u;
+        if (!whole) {
+          live = 0;
+#pragma unroll
+          for (uint32_t i = 0; i < kKeys; ++i) live |= g * 4 + i % 4 < count[i / 4] ? 1u << i : 0u;
+        }
+      }
+      return live;
+    };
+
+    uint32_t row = 0;
+    if constexpr (!kAny) row = uniform(t_begin * kTile % a.page_tokens);
     // queries of head r, zeros for columns without one
     u32x4 q[kKeyLoads];
     {
@@ -222,97 +384,13 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
 #pragma unroll
     for (uint32_t e = 0; e < kLaneDims; ++e) o[e] = f32x4{0, 0, 0, 0};
 
-    uint32_t slot = 0, row = 0;  // page and row of the tile's first token (the fast form walks them)
-    if constexpr (!kAny) {
-      slot = t_begin * kTile / a.page_tokens;
-      row = t_begin * kTile - slot * a.page_tokens;
-    }
     for (uint32_t t = t_begin; t < t_end; ++t) {
-      u32x4 kr[kSubs][kKeyLoads];
-      uint32_t vr[kKeys][kValWords];
-      bool live[kKeys];     // of key 4 g + i of each 16
-      bool whole = true;    // every key of the tile is live
-      if constexpr (kAny) {
-        whole = false;
-#pragma unroll
-        for (uint32_t s = 0; s < kSubs; ++s) {
-          const uint32_t j = t * kTile + s * 16 + r;
-          const uint32_t p = j / a.page_tokens;
-          const int32_t id = j < len ? ids[p] : -1;
-          const bool there = static_cast<uint32_t>(id) < a.pages;
-          const T* src = kp + (there ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
-#pragma unroll
-          for (uint32_t c = 0; c < kKeyLoads; ++c) {
-            T tmp[kLoad] = {};
-#pragma unroll
-            for (uint32_t e = 0; e < kLoad; ++e) {
-              const uint32_t i = c * 4 * kLoad + g * kLoad + e;
-              if (there && i < a.dim) tmp[e] = src[i];
-            }
-            __builtin_memcpy(&kr[s][c], tmp, 16);
-          }
-        }
-#pragma unroll
-        for (uint32_t i = 0; i < kKeys; ++i) {
-          const uint32_t j = t * kTile + i / 4 * 16 + g * 4 + i % 4;
-          const uint32_t p = j / a.page_tokens;
-          const int32_t id = j < len ? ids[p] : -1;
-          live[i] = static_cast<uint32_t>(id) < a.pages;
-          const T* src = vp + (live[i] ? id * a.page_stride + static_cast<int64_t>(j - p * a.page_tokens) * a.token_stride : 0);
-          T tmp[kLaneDims] = {};
-#pragma unroll
-          for (uint32_t e = 0; e < kLaneDims; ++e)
-            if (live[i] && r * kLaneDims + e < a.dim) tmp[e] = src[r * kLaneDims + e];
-          __builtin_memcpy(vr[i], tmp, sizeof tmp);
-        }
-      } else {
-        // pages hold whole sixteens of tokens, so each 16 keys lie in one page: its address is scalar
-        uint32_t count[kSubs];
-#pragma unroll
-        for (uint32_t s = 0; s < kSubs; ++s) {
-          const uint32_t j = t * kTile + s * 16;
-          const int32_t id = j < len ? static_cast<int32_t>(uniform(static_cast<uint32_t>(ids[slot]))) : -1;
-          const bool there = static_cast<uint32_t>(id) < a.pages;
-          count[s] = there ? min(16u, len - j) : 0u;
-          // rows behind the length are inside the page, and masked below; an absent page's are read from page 0
-          const int64_t base = (there ? id : 0) * a.page_stride + static_cast<int64_t>(row) * a.token_stride;
-          const uint32_t step = static_cast<uint32_t>(a.token_stride);
-          const T *ks = kp + base, *vs = vp + base;
-#pragma unroll
-          for (uint32_t c = 0; c < kKeyLoads; ++c)
-            kr[s][c] = *reinterpret_cast<const u32x4_any*>(ks + (r * step + g * kLoad) + c * 4 * kLoad);
-#pragma unroll
-          for (uint32_t i = 0; i < 4; ++i) {
-            const T* src = vs + ((g * 4 + i) * step + r * kLaneDims);
-            if constexpr (kValWords == 2) {
-              typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
-              const u32x2_any w = *reinterpret_cast<const u32x2_any*>(src);
-              vr[s * 4 + i][0] = w.x;
-              vr[s * 4 + i][1] = w.y;
-            } else {
-#pragma unroll
-              for (uint32_t w = 0; w < kValWords; w += 4) {
-                const u32x4 x = *reinterpret_cast<const u32x4_any*>(src + w * 4 / sizeof(T));
-                vr[s * 4 + i][w] = x.x;
-                vr[s * 4 + i][w + 1] = x.y;
-                vr[s * 4 + i][w + 2] = x.z;
-                vr[s * 4 + i][w + 3] = x.w;
-              }
-            }
-          }
-          whole = whole && count[s] == 16;
-          row += 16;
-          if (row == a.page_tokens) {
-            row = 0;
-            ++slot;
-          }
-        }
-        if (!whole) {
-#pragma unroll
-          for (uint32_t i = 0; i < kKeys; ++i) live[i] = g * 4 + i % 4 < count[i / 4];
-        }
+      load_keys(t, row);
+      const uint32_t live = load_values(t, row);
+      if constexpr (!kAny) {
+        row += kTile;
+        if (row >= a.page_tokens) row = a.page_tokens >= kTile ? row - a.page_tokens : 0;
       }
-
       // scores of head r with keys 4 g .. 4 g + 3 of each 16
       float x[kKeys];
 #pragma unroll
@@ -331,12 +409,12 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[s * 4 + i] = acc[i] * a.scale;
       }
-      if (!whole) {
+      if (live != ~0u) {
 #pragma unroll
         for (uint32_t i = 0; i < kKeys; ++i) {
-          x[i] = live[i] ? x[i] : -INFINITY;
+          x[i] = live >> i & 1 ? x[i] : -INFINITY;
 #pragma unroll
-          for (uint32_t w = 0; w < kValWords; ++w) vr[i][w] = live[i] ? vr[i][w] : 0u;  // 0 times whatever lies there
+          for (uint32_t w = 0; w < kValWords; ++w) vr[i][w] = live >> i & 1 ? vr[i][w] : 0u;  // 0 times whatever lies there
         }
       }
       float top = x[0];
@@ -346,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
         top = fmaxf(top, m);
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
-        const float scale = top == m ? 1.0f : exp2f(m - top);  // m = -inf: 0
+        const float scale = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);  // m = -inf: 0
         l *= scale;
 #pragma unroll
         for (uint32_t e = 0; e < kLaneDims; ++e) o[e] *= scale;
@@ -391,93 +469,149 @@ __global__ void __launch_bounds__(kThreads, (kAny ? (kDim > 128 ? 1 : 2) : kDim 
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
 
-    // lane (r, g) holds head r, dims (4 g + i) kLaneDims + e
-    if (t_begin == 0 && t_end == tiles) {
+    // Lane (r, g) holds head r, dims (4 g + i) kLaneDims + e. A worker with the whole item writes its output.
+    // A workgroup whose runs all lie inside one item joins them here, so that they leave one part.
+    const uint64_t item_end = item_first + tiles;
+    if (t_end == tiles && lane == 0) {
+      const uint32_t first = t_begin == 0 ? worker : runs.worker_of(item_first);
+      const uint32_t slot = runs.first(first) == item_first ? 0 : 1;
+      a.items[static_cast<size_t>(seq) * items + item] =
+          Parts{2 * first + slot, worker, (first + slot + kWaves - 1) / kWaves, (worker + (end == item_end ? 1 : 0)) / kWaves};
+    }
+    const uint32_t block0 = blockIdx.x * kWaves;
+    const bool together = !(t_begin == 0 && t_end == tiles) && block0 + kWaves <= runs.workers && runs.first(block0) >= item_first &&
+                          runs.first(block0 + kWaves) <= item_end;
+    if (together) {
+      if (g == 0) wave_sums[wave][r] = make_float2(m, l);
       if (r < in_group) {
-        const float inv = l > 0.0f || l != l ? 1.0f / l : 0.0f;
-        T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq) * a.out_seq + static_cast<int64_t>(q_head0 + r) * a.out_head;
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
 #pragma unroll
-          for (uint32_t e = 0; e < kLaneDims; ++e) {
-            const uint32_t dim = (4 * g + i) * kLaneDims + e;
-            if (!kAny || dim < a.dim) S::store1(op + dim, o[e][i] * inv);
-          }
-        if (a.lse && g == 0)
-          a.lse[static_cast<size_t>(seq) * a.heads * a.group + q_head0 + r] = l > 0.0f || l != l ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+          for (uint32_t e = 0; e < kLaneDims; e += 4)
+            *reinterpret_cast<f32x4*>(&wave_rows[wave][r][(4 * g + i) * kLaneDims + e]) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
       }
-    } else if (r < in_group) {
-      const uint32_t part_heads = min(16u, a.group);
-      float* part = part_at(a, worker, at == runs.first(worker) ? 0 : 1, part_heads) + static_cast<size_t>(r) * a.part_row;
-      if (g == 0) {
-        part[0] = m;
-        part[1] = l;
-      }
+      __syncthreads();
+      float* part = part_at(a, block0, 0, part_heads);
+      for (uint32_t i = threadIdx.x; i < in_group * (kDim / 4); i += kThreads) {
+        const uint32_t h = i / (kDim / 4), dim = i % (kDim / 4) * 4;
+        float2 sum[kWaves];
+        float top = -INFINITY, total = 0.0f;
 #pragma unroll
-      for (uint32_t i = 0; i < 4; ++i)
-#pragma unroll
-        for (uint32_t e = 0; e < kLaneDims; ++e) {
-          const uint32_t dim = (4 * g + i) * kLaneDims + e;
-          if (!kAny || dim < a.dim) part[4 + dim] = o[e][i];
+        for (uint32_t w = 0; w < kWaves; ++w) {
+          sum[w] = wave_sums[w][h];
+          top = fmaxf(top, sum[w].x);
         }
+        const float ref = top == -INFINITY ? 0.0f : top;
+        f32x4 all = {0, 0, 0, 0};
+#pragma unroll
+        for (uint32_t w = 0; w < kWaves; ++w) {
+          const float scale = __builtin_amdgcn_exp2f(sum[w].x - ref);
+          total += sum[w].y * scale;
+          all += *reinterpret_cast<const f32x4*>(&wave_rows[w][h][dim]) * scale;
+        }
+        float* row_at = part + static_cast<size_t>(h) * a.part_row;
+        if (dim == 0) *reinterpret_cast<float2*>(row_at) = make_float2(top, total);
+        if (!kAny || dim < a.dim) *reinterpret_cast<f32x4*>(row_at + 4 + dim) = all;
+      }
+      return;  // the runs end with it
+    }
+    if (r < in_group) {
+      if (t_begin == 0 && t_end == tiles) {
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t e = 0; e < kLaneDims; e += 4)
+            write_head<S>(a, seq, q_head0 + r, (4 * g + i) * kLaneDims + e, m, l, f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]});
+      } else {
+        float* part = part_at(a, worker, at == begin ? 0 : 1, part_heads) + static_cast<size_t>(r) * a.part_row;
+        if (g == 0) *reinterpret_cast<float2*>(part) = make_float2(m, l);
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+#pragma unroll
+          for (uint32_t e = 0; e < kLaneDims; e += 4) {
+            const uint32_t dim = (4 * g + i) * kLaneDims + e;
+            if (!kAny || dim < a.dim) *reinterpret_cast<f32x4*>(part + 4 + dim) = f32x4{o[e][i], o[e + 1][i], o[e + 2][i], o[e + 3][i]};
+          }
+      }
     }
     at = item_first + t_end;
   }
 }
 
-// One workgroup for each item: joins its parts, or writes zeros for an empty sequence.
-template <class S>
+// Joins the parts of an item, or writes zeros for an empty sequence. A workgroup has a run of kThreads /
+// kSlices float4 of the item's rows of all its heads; kSlices groups of its threads take every kSlices-th
+// part each and join theirs through LDS, so that an item of many parts is not read one after another.
+template <class S, uint32_t kSlices>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
-  typedef typename S::storage T;
-  constexpr uint32_t kTile = Mfma<S>::kTile;
-  __shared__ uint64_t before[kThreads];
-  __shared__ uint64_t found;
-  const Deal d = deal<kTile>(a, before);
-  const Runs runs(d.total, a.workers);
+  constexpr uint32_t kQuads = kThreads / kSlices;
+  __shared__ float2 sums[kSlices > 1 ? kThreads : 1];
+  __shared__ f32x4 rows[kSlices > 1 ? kThreads : 1];
   const uint32_t items = a.heads * a.group_blocks;
   const uint32_t seq = blockIdx.x / items, item = blockIdx.x - seq * items;
-  if (threadIdx.x == 0) {
-    uint64_t first = before[seq / d.each];
-    for (uint32_t s = seq / d.each * d.each; s < seq; ++s) first += static_cast<uint64_t>((live_tokens(a, s) + kTile - 1) / kTile) * items;
-    found = first;
-  }
-  __syncthreads();
-  const uint32_t tiles = (live_tokens(a, seq) + kTile - 1) / kTile;
   const uint32_t head = item / a.group_blocks, gb = item - head * a.group_blocks;
   const uint32_t in_group = min(16u, a.group - gb * 16), q_head0 = head * a.group + gb * 16;
-  const uint64_t first = found + static_cast<uint64_t>(item) * tiles;
-  uint32_t w0 = 0, w1 = 0;
-  if (tiles > 0) {
-    w0 = runs.worker_of(first);
-    w1 = runs.worker_of(first + tiles - 1);
-    if (w0 == w1) return;  // one worker had all of it
+  const uint32_t part_heads = min(16u, a.group), quads = (a.dim + 3) / 4;
+  const uint32_t slice = threadIdx.x / kQuads, e = blockIdx.y * kQuads + threadIdx.x % kQuads;
+  const uint32_t h = e / quads, dim = (e - h * quads) * 4;
+  const bool mine = h < in_group;
+  const Parts at = a.items[blockIdx.x];
+  const uint32_t first = at.first_slot / 2, slot = at.first_slot & 1;
+  // parts: single waves up to the workgroups that lie in the item, these, single waves behind them
+  const uint32_t groups = at.group1 > at.group0 ? at.group1 - at.group0 : 0;
+  const uint32_t head_parts = groups ? at.group0 * kWaves - first : at.last - first + 1;
+  uint32_t count = groups ? head_parts + groups + (at.last + 1 - at.group1 * kWaves) : head_parts;
+  if (live_tokens(a, seq) == 0)
+    count = 0;  // no worker came here, and `at` holds anything
+  else if (at.last == first)
+    return;
+
+  float m = -INFINITY, l = 0.0f;
+  f32x4 o = {0, 0, 0, 0};
+  const auto add = [&](float pm, float pl, f32x4 po) {
+    const float top = fmaxf(m, pm), ref = top == -INFINITY ? 0.0f : top;
+    const float s = __builtin_amdgcn_exp2f(m - ref), ps = __builtin_amdgcn_exp2f(pm - ref);
+    l = l * s + pl * ps;
+    o = o * s + po * ps;
+    m = top;
+  };
+  if (mine) {
+#pragma unroll 4
+    for (uint32_t w = slice; w < count; w += kSlices) {
+      const uint32_t behind = w - head_parts;
+      const uint32_t worker = w < head_parts ? first + w : behind < groups ? (at.group0 + behind) * kWaves : at.group1 * kWaves + behind - groups;
+      const float* part = part_at(a, worker, w == 0 ? slot : 0, part_heads) + static_cast<size_t>(h) * a.part_row;
+      const float2 ml = *reinterpret_cast<const float2*>(part);
+      add(ml.x, ml.y, *reinterpret_cast<const f32x4*>(part + 4 + dim));
+    }
   }
-  const uint32_t slot0 = tiles > 0 && runs.first(w0) == first ? 0 : 1;  // of the first part; the others began their runs
-  const uint32_t part_heads = min(16u, a.group);
-  for (uint32_t i = threadIdx.x; i < in_group * a.dim; i += kThreads) {
-    const uint32_t h = i / a.dim, dim = i - h * a.dim;
-    float m = -INFINITY, l = 0.0f, o = 0.0f;
-    if (tiles > 0) {
-      for (uint32_t w = w0; w <= w1; ++w) m = fmaxf(m, part_at(a, w, w == w0 ? slot0 : 0, part_heads)[h * a.part_row]);
-      const float ref = m == -INFINITY ? 0.0f : m;
-      for (uint32_t w = w0; w <= w1; ++w) {
-        const float* part = part_at(a, w, w == w0 ? slot0 : 0, part_heads) + static_cast<size_t>(h) * a.part_row;
-        const float scale = exp2f(part[0] - ref);
-        l += part[1] * scale;
-        o += part[4 + dim] * scale;
+  if constexpr (kSlices > 1) {
+    sums[threadIdx.x] = make_float2(m, l);
+    rows[threadIdx.x] = o;
+#pragma unroll
+    for (uint32_t n = kSlices / 2; n > 0; n /= 2) {
+      __syncthreads();
+      if (slice < n) {
+        const float2 ml = sums[threadIdx.x + n * kQuads];
+        add(ml.x, ml.y, rows[threadIdx.x + n * kQuads]);
+        sums[threadIdx.x] = make_float2(m, l);
+        rows[threadIdx.x] = o;
       }
     }
-    const bool any = l > 0.0f || l != l;
-    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(seq) * a.out_seq + static_cast<int64_t>(q_head0 + h) * a.out_head;
-    S::store1(op + dim, any ? o / l : 0.0f);
-    if (a.lse && dim == 0)
-      a.lse[static_cast<size_t>(seq) * a.heads * a.group + q_head0 + h] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
   }
+  if (mine && slice == 0) write_head<S>(a, seq, q_head0 + h, dim, m, l, o);
+}
+
+template <class S, uint32_t kSlices>
+void join(const Attend& a, hipStream_t st) {
+  const uint32_t rows = std::min(16u, a.group) * ((a.dim + 3) / 4);
+  const dim3 grid(a.seqs * a.heads * a.group_blocks, (rows - 1) / (kThreads / kSlices) + 1);
+  join_kernel<S, kSlices><<<grid, dim3(kThreads), 0, st>>>(a);
 }
 
 template <class S>
-int attend(const Attend& a, hipStream_t st) {
-  const dim3 grid((a.workers + kThreads / kWave - 1) / (kThreads / kWave)), block(kThreads);
+int attend(Attend& a, hipStream_t st) {
+  a.workers = std::min(attend_workers(a.dim), 1024 * waves_for<S>(a.dim));
+  const dim3 grid(a.workers / kWaves), block(kThreads);
   // a page of whole sixteens, in which 32-bit offsets reach every row, and a head size with a kernel
   const int64_t reach = 16 * a.token_stride + a.dim;
   const bool fast = a.page_tokens % 16 == 0 && reach < (int64_t{1} << 28);
@@ -495,7 +629,16 @@ int attend(const Attend& a, hipStream_t st) {
     attend_kernel<S, 256, true><<<grid, block, 0, st>>>(a);
   int rc = launched();
   if (rc != ZO_OK) return rc;
-  join_kernel<S><<<dim3(a.seqs * a.heads * a.group_blocks), block, 0, st>>>(a);
+  // as many slices as an item has parts when all sequences are as long as the table
+  const uint64_t items = static_cast<uint64_t>(a.seqs) * a.heads * a.group_blocks;
+  const uint64_t room = static_cast<uint64_t>(a.width) * a.page_tokens;
+  const uint64_t parts = std::min(a.workers / items, room / Mfma<S>::kTile) / kWaves;
+  if (parts >= 24)
+    join<S, 32>(a, st);
+  else if (parts >= 6)
+    join<S, 8>(a, st);
+  else
+    join<S, 2>(a, st);
   return launched();
 }
 
@@ -514,7 +657,8 @@ extern "C" int zo_cache_attend(const zo_attend* p, void* stream) {
   a.v = static_cast<const char*>(p->cache.v);
   a.out = static_cast<char*>(p->out.data);
   a.lse = p->lse;
-  a.parts = static_cast<float*>(p->work);
+  a.items = static_cast<Parts*>(p->work);
+  a.parts = reinterpret_cast<float*>(static_cast<char*>(p->work) + attend_items_bytes(p->table.seqs, p->q_heads, p->cache.heads));
   a.ids = p->table.ids;
   a.lengths = p->lengths;
   a.q_seq = p->q.token_stride;
@@ -533,7 +677,6 @@ extern "C" int zo_cache_attend(const zo_attend* p, void* stream) {
   a.group = p->q_heads / p->cache.heads;
   a.group_blocks = (a.group + 15) / 16;
   a.dim = p->cache.dim;
-  a.workers = attend_workers(a.seqs, p->q_heads, a.heads, a.dim);
   a.part_row = (a.dim + 3) / 4 * 4 + 4;
   a.scale = p->scale * 1.4426950408889634f;
   (void)hipGetLastError();

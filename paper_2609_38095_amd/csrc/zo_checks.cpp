@@ -200,12 +200,12 @@ int check_back(const zo_rotate_back& b) {
   return ZO_OK;
 }
 
-uint32_t attend_workers(uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim) {
-  (void)seqs;
-  (void)q_heads;
-  (void)heads;
-  return 1024 * (dim > 128 ? 2 : dim > 64 ? 3 : 4);
+// 16 bytes for each item: a sequence, a key head, up to 16 of its query heads.
+uint64_t attend_items_bytes(uint32_t seqs, uint32_t q_heads, uint32_t heads) {
+  return static_cast<uint64_t>(seqs) * heads * ((q_heads / heads + 15) / 16) * 16;
 }
+
+uint32_t attend_workers(uint32_t dim) { return 1024 * (dim > 128 ? 2 : dim > 64 ? 3 : 4); }
 
 int check_attend(const zo_attend& a) {
   if (!dtype_ok(a.dtype)) return ZO_ERR_ARG;
@@ -220,6 +220,9 @@ int check_attend(const zo_attend& a) {
   ZO_TRY(check_rows(a.out, a.table.seqs, a.q_heads, a.cache.dim, elem, true));
   // a worker writes a head's output while others still read their queries
   ZO_TRY(check_apart(a.out, a.q_heads, a.q, a.q_heads, false, a.table.seqs, a.cache.dim, elem));
+  // tiles of 16 tokens are numbered below 2^52 (a token that no memory of its own holds may count many times)
+  if (static_cast<uint64_t>(a.table.width) * a.cache.page_tokens / 16 >= (1ull << 52) / (static_cast<uint64_t>(a.table.seqs) * a.q_heads))
+    return ZO_ERR_ARG;
   if (a.lengths == nullptr || a.work == nullptr) return ZO_ERR_NULL;
   if (!aligned(a.lengths, 4) || !aligned(a.lse, 4) || !aligned(a.work, 16)) return ZO_ERR_ARG;
   if (a.work_bytes < zo_cache_attend_work(a.table.seqs, a.q_heads, a.cache.heads, a.cache.dim)) return ZO_ERR_ARG;
@@ -285,7 +288,7 @@ uint64_t zo_cache_attend_work(uint32_t seqs, uint32_t q_heads, uint32_t heads, u
   if (heads == 0 || q_heads % heads != 0 || dim > ZO_DIM_MAX) return 0;
   const uint64_t group = q_heads / heads < 16 ? q_heads / heads : 16;
   const uint64_t row = (dim + 3) / 4 * 4 + 4;
-  return 2ull * zo::attend_workers(seqs, q_heads, heads, dim) * group * row * sizeof(float);
+  return zo::attend_items_bytes(seqs, q_heads, heads) + 2ull * zo::attend_workers(dim) * group * row * sizeof(float);
 }
 
 int zo_rotary_turns(zo_rotary_kind kind, uint32_t rotary, double base, double factor, double original, double low,

@@ -28,7 +28,8 @@ bool rows_overlap(const zo_heads& a, uint32_t a_heads, const zo_heads& b, uint32
 // (waves) among which the tiles are split.
 constexpr uint32_t kBackBlocks = 512;
 uint32_t back_blocks(uint32_t tokens, uint32_t heads);
-uint32_t attend_workers(uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim);
+uint64_t attend_items_bytes(uint32_t seqs, uint32_t q_heads, uint32_t heads);  // the parts' whereabouts
+uint32_t attend_workers(uint32_t dim);  // at most
 
 }  // namespace zo
 
