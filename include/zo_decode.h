@@ -190,20 +190,21 @@ uint64_t zo_cache_attend_work(uint32_t seqs, uint32_t q_heads, uint32_t heads, u
 int zo_cache_attend(const zo_attend* a, void* stream);
 
 /*
- * zo_cache_copy -- copies tokens 0 .. rows - 1 of page src to page dst, keys and values of every
- * head, for each of n_moves moves in each of n_caches caches (the layers of a model, all of the same
- * shape). caches and moves are host arrays. All moves read what the pages held before the call: no
- * dst is repeated or is the src of a move.
+ * zo_cache_copy -- copies tokens 0 .. rows - 1 of page src to page dst, every head, for each of n_moves
+ * moves in each of n_tensors tensors: the keys and the values of each layer of a model, all of the shape
+ * and strides of `shape` (whose k and v are not used). tensors (device addresses) and moves are host
+ * arrays. All moves read what the pages held before the call: no dst is repeated or is the src of a
+ * move.
  * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, a page or rows out of range, rows = 0, a
- * repeated dst, a dst that is a src, caches of different shape), ZO_ERR_MEMORY, ZO_ERR_HIP (earlier
- * batches may already be enqueued).
+ * repeated dst, a dst that is a src, pages that overlap, pages of 2^30 elements or more), ZO_ERR_MEMORY,
+ * ZO_ERR_HIP (earlier batches may already be enqueued).
  */
 typedef struct {
   int32_t src, dst, rows;
 } zo_page_move;
 
-int zo_cache_copy(const zo_cache* caches, uint32_t n_caches, const zo_page_move* moves, uint32_t n_moves,
-                  zo_dtype dtype, void* stream);
+int zo_cache_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves,
+                  uint32_t n_moves, zo_dtype dtype, void* stream);
 
 /*
  * zo_draw -- draws a token for each row of logits from given random numbers.

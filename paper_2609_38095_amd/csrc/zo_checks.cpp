@@ -240,21 +240,21 @@ int check_draw(const zo_draw_args& a) {
   return ZO_OK;
 }
 
-int check_copy(const zo_cache* caches, uint32_t n_caches, const zo_page_move* moves, uint32_t n_moves, int32_t dtype) {
+int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype) {
   if (!dtype_ok(dtype)) return ZO_ERR_ARG;
-  if (n_caches == 0 || n_moves == 0) return ZO_OK;
-  if (caches == nullptr || moves == nullptr) return ZO_ERR_NULL;
-  const zo_cache& first = caches[0];
+  if (n_tensors == 0 || n_moves == 0) return ZO_OK;
+  if (shape == nullptr || tensors == nullptr || moves == nullptr) return ZO_ERR_NULL;
+  zo_cache first = *shape;
+  first.k = first.v = tensors[0];
+  const size_t elem = elem_bytes(dtype);
+  ZO_TRY(check_cache(first, elem, true));
   // vectors of a head's page and a launch's workgroups are numbered in 32 bits
   if (static_cast<uint64_t>(first.page_tokens) * first.dim > (1ull << 28) || first.heads > 0xFFFFu ||
       static_cast<uint64_t>(first.page_tokens) * first.dim * first.heads > (1ull << 30))
     return ZO_ERR_ARG;
-  for (uint32_t i = 0; i < n_caches; ++i) {
-    const zo_cache& c = caches[i];
-    ZO_TRY(check_cache(c, elem_bytes(dtype), true));
-    if (c.pages != first.pages || c.heads != first.heads || c.page_tokens != first.page_tokens || c.dim != first.dim ||
-        c.page_stride != first.page_stride || c.head_stride != first.head_stride || c.token_stride != first.token_stride)
-      return ZO_ERR_ARG;
+  for (uint32_t i = 0; i < n_tensors; ++i) {
+    if (tensors[i] == nullptr) return ZO_ERR_NULL;
+    if (!aligned(tensors[i], elem)) return ZO_ERR_ARG;
   }
   try {
     // bit 0: a destination, bit 1: a source

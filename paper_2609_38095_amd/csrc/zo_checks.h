@@ -17,7 +17,7 @@ int check_put(const zo_rotate_put& p);
 int check_back(const zo_rotate_back& b);
 int check_attend(const zo_attend& a);
 int check_draw(const zo_draw_args& a);
-int check_copy(const zo_cache* caches, uint32_t n_caches, const zo_page_move* moves, uint32_t n_moves, int32_t dtype);
+int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype);
 
 // Whether two sets of rows may share an element. Exact for rows of one interleaved buffer (equal
 // token strides, a token's heads inside one stride), otherwise by the ranges that they span.

@@ -80,14 +80,14 @@ void launch(const Copy& c, uint32_t heads, dim3 grid, hipStream_t st) {
 }  // namespace
 }  // namespace zo
 
-extern "C" int zo_cache_copy(const zo_cache* caches, uint32_t n_caches, const zo_page_move* moves, uint32_t n_moves, zo_dtype dtype,
-                             void* stream) {
+extern "C" int zo_cache_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves,
+                             uint32_t n_moves, zo_dtype dtype, void* stream) {
   using namespace zo;
-  const int rc = check_copy(caches, n_caches, moves, n_moves, dtype);
+  const int rc = check_copy(shape, tensors, n_tensors, moves, n_moves, dtype);
   if (rc != ZO_OK) return rc;
-  if (n_caches == 0 || n_moves == 0) return ZO_OK;
+  if (n_tensors == 0 || n_moves == 0) return ZO_OK;
   const int64_t elem = static_cast<int64_t>(elem_bytes(dtype));
-  const zo_cache& f = caches[0];
+  const zo_cache& f = *shape;
   Copy c;
   c.page_stride = f.page_stride * elem;
   c.head_stride = f.head_stride * elem;
@@ -104,13 +104,10 @@ extern "C" int zo_cache_copy(const zo_cache* caches, uint32_t n_caches, const zo
     uint32_t rows = 0;
     for (uint32_t i = 0; i < n; ++i) rows = std::max(rows, static_cast<uint32_t>(c.move[i].rows));
     c.vec_parts = (rows * c.row_vecs - 1) / kThreads + 1;
-    for (uint32_t t0 = 0; t0 < n_caches; t0 += kTensors / 2) {
-      const uint32_t layers = std::min(kTensors / 2, n_caches - t0);
-      for (uint32_t i = 0; i < layers; ++i) {
-        c.tensor[2 * i] = static_cast<char*>(caches[t0 + i].k);
-        c.tensor[2 * i + 1] = static_cast<char*>(caches[t0 + i].v);
-      }
-      const dim3 grid(c.vec_parts * c.head_parts * n, 2 * layers);
+    for (uint32_t t0 = 0; t0 < n_tensors; t0 += kTensors) {
+      const uint32_t count = std::min(kTensors, n_tensors - t0);
+      for (uint32_t i = 0; i < count; ++i) c.tensor[i] = static_cast<char*>(tensors[t0 + i]);
+      const dim3 grid(c.vec_parts * c.head_parts * n, count);
       if (vectors)
         launch<16>(c, together, grid, st);
       else if (elem == 4)

@@ -19,7 +19,7 @@ stream of its own allocates on that stream, and waiting for tensors that other s
 is the caller's.
 """
 
-import contextlib
+import array
 import ctypes
 import struct
 
@@ -48,6 +48,7 @@ _CACHE = struct.Struct("QQqqqIIII")
 _NO_ROWS = (0, 0, 0)
 _TYPES = {torch.float32: ZO_F32, torch.bfloat16: ZO_BF16}
 
+_TENSORS = {torch.Tensor, torch.nn.Parameter}
 _READY = None
 
 
@@ -67,7 +68,7 @@ def _lib():
                 ("zo_norm_rotate", [args, vp], i32), ("zo_norm_rotate_put", [args, vp], i32),
                 ("zo_norm_rotate_back", [args, vp], i32), ("zo_norm_rotate_back_work", [u32, u32, u32, u32], u64),
                 ("zo_cache_attend", [args, vp], i32), ("zo_cache_attend_work", [u32, u32, u32, u32], u64),
-                ("zo_cache_copy", [args, u32, vp, u32, i32, vp], i32), ("zo_draw", [args, vp], i32),
+                ("zo_cache_copy", [args, args, u32, vp, u32, i32, vp], i32), ("zo_draw", [args, vp], i32),
                 ("zo_pages_open", [u32, u32], vp), ("zo_pages_close", [vp], None),
                 ("zo_pages_add", [vp, u32, pu], i32), ("zo_pages_fork", [vp, u32, pu], i32),
                 ("zo_pages_extend", [vp, u32, u32, move], i32), ("zo_pages_drop", [vp, u32], i32),
@@ -82,72 +83,97 @@ def _lib():
 
 def _on(stream):
     """Allocations of a call with a stream of its own belong to that stream."""
-    if stream is None:
-        return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))
     return torch.cuda.stream(stream)
 
 
-def _tensor(t, name, dtype, like, dims):
+def _new(like, shape, stream, dtype=None):
+    """A tensor on `like`'s device for a result or a workspace."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+    with _on(stream):
+        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
+
+
+def _launch_stream(like, stream):
+    """The hipStream_t to launch on, torch's current one by default; the tensors are on the current device."""
+    if stream is None:
+        index = like.get_device()
+        if index == torch._C._cuda_getDevice():
+            return torch._C._cuda_getCurrentRawStream(index)
+    return _stream(like, stream)
+
+
+# Each check is one expression over what a sound argument has; what it does not take is named by _refuse. (A
+# call on a few tokens takes less time on the GPU than ten tensors' checks one by one take here.)
+
+def _refuse(t, name, dtype, like, shape, what):
+    """Raises what is wrong with an argument."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions")
-    if like is not None and t.get_device() != like.get_device():
+    if t.get_device() != like.get_device():
         raise ValueError(f"{name} lives on {t.device}, the other tensors on {like.device}")
-    return t
+    if t.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    raise ValueError(f"{name}: {what}")
 
 
-def _dtype(t, name):
+def _dtype(t, name, dims):
+    """The library's name of a tensor's type; the tensor that a call's others are compared with."""
     dtype = _TYPES.get(getattr(t, "dtype", None))
     if dtype is None:
         raise TypeError(f"{name} must be a float32 or bfloat16 tensor")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
+    if t.dim() != dims:
+        raise ValueError(f"{name} must have {dims} dimensions")
     return dtype
 
 
 def _rows(t, name, like, shape):
     """(address, token stride, head stride) of a tensor [tokens, heads, dim]."""
-    _tensor(t, name, like.dtype, like, 3)
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
-    a, b, c = t.stride()
-    if c != 1 and shape[2] > 1:
-        raise ValueError(f"the last dimension of {name} must be contiguous")
-    return t.data_ptr(), a, b
+    if type(t) in _TENSORS and t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device():
+        a, b, c = t.stride()
+        if c == 1 or shape[2] == 1:
+            return t.data_ptr(), a, b
+    _refuse(t, name, like.dtype, like, shape, "the last dimension must be contiguous")
 
 
 def _vector(t, name, dtype, like, n):
     """The address of a contiguous tensor of n elements; 0 for None."""
     if t is None:
         return 0
-    _tensor(t, name, dtype, like, 1)
-    if t.shape[0] != n or (n > 1 and t.stride(0) != 1):
-        raise ValueError(f"{name} must be contiguous and hold {n} elements")
-    return t.data_ptr()
+    if type(t) in _TENSORS and t.dtype is dtype and t.shape == (n,) and t.get_device() == like.get_device() \
+            and (n < 2 or t.stride(0) == 1):
+        return t.data_ptr()
+    _refuse(t, name, dtype, like, (n,), "must be contiguous")
 
 
 def _cache(k, v, like):
-    """The packed fields of a cache [pages, heads, page_tokens, dim]."""
-    _tensor(k, "k_cache", like.dtype, like, 4)
-    _tensor(v, "v_cache", like.dtype, like, 4)
-    strides = k.stride()
-    if v.shape != k.shape or v.stride() != strides:
-        raise ValueError("k_cache and v_cache must have the same shape and strides")
-    pages, heads, page_tokens, dim = k.shape
-    if strides[3] != 1 and dim > 1:
-        raise ValueError("the last dimension of the cache must be contiguous")
-    return k.data_ptr(), v.data_ptr(), strides[0], strides[1], strides[2], pages, heads, page_tokens, dim
+    """The fields of a cache [pages, heads, page_tokens, dim]."""
+    shape = getattr(k, "shape", None)
+    if shape is not None and len(shape) == 4:
+        strides = k.stride()
+        if type(v) in _TENSORS and k.dtype is like.dtype and v.dtype is like.dtype and v.shape == shape \
+                and v.stride() == strides and k.get_device() == like.get_device() == v.get_device() \
+                and (strides[3] == 1 or shape[3] == 1):
+            return (k.data_ptr(), v.data_ptr(), *strides[:3], *shape)
+    else:
+        raise ValueError("k_cache must be a tensor [pages, heads, page_tokens, dim]")
+    _refuse(k, "k_cache", like.dtype, like, shape, "") if k.dtype != like.dtype or k.get_device() != like.get_device() else \
+        _refuse(v, "v_cache", like.dtype, like, shape, "the strides of k_cache, the last dimension contiguous, are needed")
 
 
 def _table(table, like):
-    _tensor(table, "table", torch.int32, like, 2)
-    n, width = table.shape
-    if width > 1 and table.stride(1) != 1:
-        raise ValueError("the rows of the table must be contiguous")
-    return table.data_ptr(), table.stride(0), n, width
+    if type(table) in _TENSORS and table.dtype is torch.int32 and table.get_device() == like.get_device() and table.dim() == 2:
+        n, width = table.shape
+        a, b = table.stride()
+        if b == 1 or width < 2:
+            return table.data_ptr(), a, n, width
+    _refuse(table, "table", torch.int32, like, getattr(table, "shape", ()), "must be [sequences, pages], its rows contiguous")
 
 
 def zo_rotary_turns(rotary, base=10000.0, kind=ZO_ROTARY_LINEAR, factor=1.0, original=0.0, low=1.0, high=4.0):
@@ -161,11 +187,13 @@ def _sides(q, k):
     like = q if q is not None else k
     if like is None:
         raise ValueError("queries or keys are needed")
-    dtype = _dtype(like, "q" if q is not None else "k")
-    if like.dim() != 3:
-        raise ValueError("q and k must be [tokens, heads, dim]")
-    tokens, dim = like.shape[0], like.shape[2]
-    return like, dtype, tokens, dim, 0 if q is None else q.shape[1], 0 if k is None else k.shape[1]
+    dtype = _dtype(like, "q and k", 3)
+    tokens, heads, dim = like.shape
+    if k is None:
+        return like, dtype, tokens, dim, heads, 0
+    if not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise TypeError("k must be a CUDA (HIP) torch tensor [tokens, heads, dim]")
+    return like, dtype, tokens, dim, 0 if q is None else heads, k.shape[1]
 
 
 def _turns(turns):
@@ -182,29 +210,22 @@ def zo_norm_rotate(q, k, positions, turns=None, interleaved=False, magnitude=1.0
     """(q_out, k_out): each head of q and k [tokens, heads, dim] normed (where it has a gamma) and its first
     2 len(turns) dims rotated by its token's position. q or k may be None. In place: q_out = q."""
     like, dtype, tokens, dim, hq, hk = _sides(q, k)
+    if q is not None and q_out is None:
+        q_out = _new(like, (tokens, hq, dim), stream)
+    if k is not None and k_out is None:
+        k_out = _new(like, (tokens, hk, dim), stream)
     qs = ks = qo = ko = _NO_ROWS
-    if stream is not None and (q is not None and q_out is None or k is not None and k_out is None):
-        with _on(stream):
-            q_out = torch.empty((tokens, hq, dim), dtype=q.dtype, device=q.device) if q is not None and q_out is None else q_out
-            k_out = torch.empty((tokens, hk, dim), dtype=k.dtype, device=k.device) if k is not None and k_out is None else k_out
     if q is not None:
-        shape = q.shape
-        qs = _rows(q, "q", like, shape)
-        if q_out is None:
-            q_out = torch.empty(shape, dtype=like.dtype, device=like.device)
-        qo = _rows(q_out, "q_out", like, shape)
+        qs, qo = _rows(q, "q", like, q.shape), _rows(q_out, "q_out", like, q.shape)
     if k is not None:
         shape = (tokens, hk, dim)
-        ks = _rows(k, "k", like, shape)
-        if k_out is None:
-            k_out = torch.empty(shape, dtype=like.dtype, device=like.device)
-        ko = _rows(k_out, "k_out", like, shape)
+        ks, ko = _rows(k, "k", like, shape), _rows(k_out, "k_out", like, shape)
     turns, at, rotary = _turns(turns)
     args = _ROTATE.pack(*qs, *ks, *qo, *ko, _vector(q_gamma, "q_gamma", like.dtype, like, dim),
                         _vector(k_gamma, "k_gamma", like.dtype, like, dim),
                         _vector(positions, "positions", torch.int32, like, tokens), at, tokens, hq, hk, dim, rotary,
                         interleaved, norm_eps, magnitude, dtype)
-    _check(_lib().zo_norm_rotate(args, _stream(like, stream)), "zo_norm_rotate")
+    _check(_lib().zo_norm_rotate(args, _launch_stream(like, stream)), "zo_norm_rotate")
     return q_out, k_out
 
 
@@ -217,8 +238,7 @@ def zo_norm_rotate_put(q, k, v, k_cache, v_cache, table, positions, turns=None, 
     if q is not None:
         qs = _rows(q, "q", like, q.shape)
         if q_out is None:
-            with _on(stream):
-                q_out = torch.empty((tokens, hq, dim), dtype=like.dtype, device=like.device)
+            q_out = _new(like, (tokens, hq, dim), stream)
         qo = _rows(q_out, "q_out", like, q.shape)
     shape = (tokens, hk, dim)
     turns, at, rotary = _turns(turns)
@@ -227,7 +247,7 @@ def zo_norm_rotate_put(q, k, v, k_cache, v_cache, table, positions, turns=None, 
                      _vector(positions, "positions", torch.int32, like, tokens), at, tokens, hq, hk, dim, rotary,
                      interleaved, norm_eps, magnitude, dtype, *_rows(v, "v", like, shape), *_cache(k_cache, v_cache, like),
                      *_table(table, like), _vector(seqs, "seqs", torch.int32, like, tokens))
-    _check(_lib().zo_norm_rotate_put(args, _stream(like, stream)), "zo_norm_rotate_put")
+    _check(_lib().zo_norm_rotate_put(args, _launch_stream(like, stream)), "zo_norm_rotate_put")
     return q_out
 
 
@@ -237,16 +257,14 @@ def zo_norm_rotate_back(dq_out, dk_out, q, k, positions, turns=None, interleaved
     are float32 (None without the gamma). q and k are read only where there is a gamma."""
     like, dtype, tokens, dim, hq, hk = _sides(dq_out, dk_out)
     lib = _lib()
-    dev = like.device
-    with _on(stream):
-        if dq_out is not None and dq is None:
-            dq = torch.empty((tokens, hq, dim), dtype=like.dtype, device=dev)
-        if dk_out is not None and dk is None:
-            dk = torch.empty((tokens, hk, dim), dtype=like.dtype, device=dev)
-        dq_gamma = torch.empty(dim, dtype=torch.float32, device=dev) if q_gamma is not None and hq else None
-        dk_gamma = torch.empty(dim, dtype=torch.float32, device=dev) if k_gamma is not None and hk else None
-        if work is None and (dq_gamma is not None or dk_gamma is not None):
-            work = torch.empty(max(lib.zo_norm_rotate_back_work(tokens, hq, hk, dim), 16), dtype=torch.uint8, device=dev)
+    if dq_out is not None and dq is None:
+        dq = _new(like, (tokens, hq, dim), stream)
+    if dk_out is not None and dk is None:
+        dk = _new(like, (tokens, hk, dim), stream)
+    dq_gamma = _new(like, (dim,), stream, torch.float32) if q_gamma is not None and hq else None
+    dk_gamma = _new(like, (dim,), stream, torch.float32) if k_gamma is not None and hk else None
+    if work is None and (dq_gamma is not None or dk_gamma is not None):
+        work = _new(like, (max(lib.zo_norm_rotate_back_work(tokens, hq, hk, dim), 16),), stream, torch.uint8)
     sq, sk = (tokens, hq, dim), (tokens, hk, dim)
     rows = lambda t, name, shape, on: _rows(t, name, like, shape) if on else _NO_ROWS  # noqa: E731
     turns, at, rotary = _turns(turns)
@@ -257,7 +275,7 @@ def zo_norm_rotate_back(dq_out, dk_out, q, k, positions, turns=None, interleaved
                       interleaved, norm_eps, magnitude, dtype, *rows(dq, "dq", sq, hq), *rows(dk, "dk", sk, hk),
                       0 if dq_gamma is None else dq_gamma.data_ptr(), 0 if dk_gamma is None else dk_gamma.data_ptr(),
                       *_work(work, like))
-    _check(lib.zo_norm_rotate_back(args, _stream(like, stream)), "zo_norm_rotate_back")
+    _check(lib.zo_norm_rotate_back(args, _launch_stream(like, stream)), "zo_norm_rotate_back")
     return dq, dk, dq_gamma, dk_gamma
 
 
@@ -274,9 +292,7 @@ def zo_cache_attend(q, k_cache, v_cache, table, lengths, scale=None, out=None, l
     """out [sequences, heads, dim] of one new token of each sequence: attention of its queries q over the first
     lengths[s] tokens of its pages table[s]. scale: dim ** -0.5 by default. lse: also returns log sum exp
     of the scores, float32 [sequences, heads]. work: a tensor of zo_cache_attend_work() bytes (allocated if None)."""
-    dtype = _dtype(q, "q")
-    if q.dim() != 3:
-        raise ValueError("q must be [sequences, heads, dim]")
+    dtype = _dtype(q, "q", 3)
     seqs, heads, dim = shape = q.shape
     qs = _rows(q, "q", q, shape)
     cache = _cache(k_cache, v_cache, q)
@@ -286,20 +302,16 @@ def zo_cache_attend(q, k_cache, v_cache, table, lengths, scale=None, out=None, l
     if ids[2] != seqs:
         raise ValueError("the table has one row for each sequence")
     lib = _lib()
-    with _on(stream) if stream is not None else _HERE:
-        if out is None:
-            out = torch.empty(shape, dtype=q.dtype, device=q.device)
-        sums = torch.empty((seqs, heads), dtype=torch.float32, device=q.device) if lse else None
-        if work is None:
-            work = torch.empty(lib.zo_cache_attend_work(seqs, heads, cache[6], dim), dtype=torch.uint8, device=q.device)
+    if out is None:
+        out = _new(q, shape, stream)
+    sums = _new(q, (seqs, heads), stream, torch.float32) if lse else None
+    if work is None:
+        work = _new(q, (lib.zo_cache_attend_work(seqs, heads, cache[6], dim),), stream, torch.uint8)
     args = _ATTEND.pack(*qs, *_rows(out, "out", q, shape), *cache, *ids,
                         _vector(lengths, "lengths", torch.int32, q, seqs), 0 if sums is None else sums.data_ptr(),
                         *_work(work, q), heads, dim ** -0.5 if scale is None else scale, dtype)
-    _check(lib.zo_cache_attend(args, _stream(q, stream)), "zo_cache_attend")
+    _check(lib.zo_cache_attend(args, _launch_stream(q, stream)), "zo_cache_attend")
     return (out, sums) if lse else out
-
-
-_HERE = contextlib.nullcontext()
 
 
 def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):
@@ -308,40 +320,44 @@ def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):
     k_caches, v_caches = list(k_caches), list(v_caches)
     if len(k_caches) != len(v_caches):
         raise ValueError("one v_cache for each k_cache")
-    src = np.asarray(src, dtype=np.int32).reshape(-1)
-    moves = np.empty((len(src), 3), np.int32)
     if not k_caches:
         return
     like = k_caches[0]
-    dtype = _dtype(like, "k_cache")
-    caches = [_cache(k, v, like) for k, v in zip(k_caches, v_caches)]
+    dtype = _dtype(like, "k_cache", 4)
+    fields = _cache(like, v_caches[0], like)
+    kind, device, shape, strides = like.dtype, like.get_device(), like.shape, like.stride()
+    at = []
+    for t in k_caches + v_caches:
+        if not (type(t) in _TENSORS and t.dtype is kind and t.get_device() == device and t.shape == shape
+                and t.stride() == strides):
+            _refuse(t, "each cache", kind, like, shape, "must have the strides of the first")
+        at.append(t.data_ptr())
+    src = np.asarray(src, dtype=np.int32)
+    moves = np.empty((src.size, 3), np.int32)
     moves[:, 0], moves[:, 1] = src, dst
-    moves[:, 2] = caches[0][7] if rows is None else rows
-    packed = struct.pack(_CACHE.format * len(caches), *[f for c in caches for f in c])
-    _check(_lib().zo_cache_copy(packed, len(caches), moves.ctypes.data, len(moves), dtype, _stream(like, stream)),
-           "zo_cache_copy")
+    moves[:, 2] = shape[2] if rows is None else rows
+    _check(_lib().zo_cache_copy(_CACHE.pack(*fields), array.array("Q", at).tobytes(), len(at), moves.ctypes.data, len(moves),
+                                dtype, _launch_stream(like, stream)), "zo_cache_copy")
 
 
 def zo_draw(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=False, tokens=None, stream=None):
     """int32 tokens [rows] drawn from logits [rows, vocab] with the random numbers u [rows] in [0, 1), each row with
     its temperature, top_k (int32), top_p and min_p (device tensors [rows] or None). logprobs: also returns
     the drawn tokens' log probabilities among what was kept, float32."""
-    dtype = _dtype(logits, "logits")
-    _tensor(logits, "logits", logits.dtype, None, 2)
+    dtype = _dtype(logits, "logits", 2)
     rows, vocab = logits.shape
     if vocab > 1 and logits.stride(1) != 1:
         raise ValueError("rows of logits must be contiguous")
-    with _on(stream) if stream is not None else _HERE:
-        if tokens is None:
-            tokens = torch.empty(rows, dtype=torch.int32, device=logits.device)
-        probs = torch.empty(rows, dtype=torch.float32, device=logits.device) if logprobs else None
+    if tokens is None:
+        tokens = _new(logits, (rows,), stream, torch.int32)
+    probs = _new(logits, (rows,), stream, torch.float32) if logprobs else None
     f32 = torch.float32
     args = _DRAW.pack(logits.data_ptr(), logits.stride(0), _vector(u, "u", f32, logits, rows),
                       _vector(temperature, "temperature", f32, logits, rows), _vector(top_k, "top_k", torch.int32, logits, rows),
                       _vector(top_p, "top_p", f32, logits, rows), _vector(min_p, "min_p", f32, logits, rows),
                       _vector(tokens, "tokens", torch.int32, logits, rows), 0 if probs is None else probs.data_ptr(),
                       rows, vocab, dtype)
-    _check(_lib().zo_draw(args, _stream(logits, stream)), "zo_draw")
+    _check(_lib().zo_draw(args, _launch_stream(logits, stream)), "zo_draw")
     return (tokens, probs) if logprobs else tokens
 
 

@@ -237,20 +237,22 @@ void argument_checks() {
   REQUIRE(wit([](zo_attend& b) { b.table.seqs = 0x7FFFFFFF; }) == ZO_ERR_ARG);
 
   const zo_page_move moves[2] = {{1, 2, 16}, {3, 4, 1}};
-  REQUIRE(check_copy(&c, 1, moves, 2, ZO_BF16) == ZO_OK && check_copy(nullptr, 0, moves, 2, ZO_BF16) == ZO_OK);
+  void* tensors[2] = {c.k, c.v};
+  REQUIRE(check_copy(&c, tensors, 2, moves, 2, ZO_BF16) == ZO_OK && check_copy(nullptr, nullptr, 0, moves, 2, ZO_BF16) == ZO_OK);
   const auto bad_move = [&](zo_page_move m) {
     const zo_page_move list[2] = {moves[0], m};
-    return check_copy(&c, 1, list, 2, ZO_BF16);
+    return check_copy(&c, tensors, 2, list, 2, ZO_BF16);
   };
   REQUIRE(bad_move({3, 100, 1}) == ZO_ERR_ARG && bad_move({-1, 5, 1}) == ZO_ERR_ARG && bad_move({3, 5, 17}) == ZO_ERR_ARG);
   REQUIRE(bad_move({3, 5, 0}) == ZO_ERR_ARG && bad_move({3, 2, 1}) == ZO_ERR_ARG && bad_move({3, 1, 1}) == ZO_ERR_ARG);
   REQUIRE(bad_move({2, 5, 1}) == ZO_ERR_ARG && bad_move({5, 5, 1}) == ZO_ERR_ARG && bad_move({1, 5, 3}) == ZO_OK);
-  zo_cache two[2] = {c, c};
-  two[1].head_stride = 64;
-  two[1].token_stride = 8 * 64;
-  REQUIRE(check_copy(two, 2, moves, 2, ZO_BF16) == ZO_ERR_ARG);
+  REQUIRE(check_copy(nullptr, tensors, 2, moves, 2, ZO_BF16) == ZO_ERR_NULL && check_copy(&c, nullptr, 2, moves, 2, ZO_BF16) == ZO_ERR_NULL);
+  tensors[1] = nullptr;
+  REQUIRE(check_copy(&c, tensors, 2, moves, 2, ZO_BF16) == ZO_ERR_NULL);
+  tensors[1] = at(0x9000001);
+  REQUIRE(check_copy(&c, tensors, 2, moves, 2, ZO_BF16) == ZO_ERR_ARG);
   c.token_stride = 32;  // tokens that overlap
-  REQUIRE(check_copy(&c, 1, moves, 2, ZO_BF16) == ZO_ERR_ARG);
+  REQUIRE(check_copy(&c, tensors, 1, moves, 2, ZO_BF16) == ZO_ERR_ARG);
 }
 
 int main() {

@@ -107,9 +107,12 @@ def test_null_and_invalid_structs_are_refused():
     assert draw(rows=0, logits=0, u=0, tokens=0) == zo.ZO_OK
     cache = decode._CACHE.pack(0x1000, 0x9000, 64, 64, 8, 4, 1, 8, 8)
     moves = np.array([[0, 1, 8]], np.int32)
-    assert lib.zo_cache_copy(cache, 1, None, 1, 0, None) == lib.zo_cache_copy(None, 1, moves.ctypes.data, 1, 0, None) == zo.ZO_ERR_NULL
-    assert lib.zo_cache_copy(cache, 0, moves.ctypes.data, 1, 0, None) == lib.zo_cache_copy(cache, 1, None, 0, 0, None) == zo.ZO_OK
-    assert lib.zo_cache_copy(cache, 1, moves.ctypes.data, 1, 9, None) == zo.ZO_ERR_ARG
+    two = np.array([0x1000, 0x9000], np.uint64).tobytes()
+    at = moves.ctypes.data
+    assert lib.zo_cache_copy(cache, two, 2, None, 1, 0, None) == lib.zo_cache_copy(None, two, 2, at, 1, 0, None) == zo.ZO_ERR_NULL
+    assert lib.zo_cache_copy(cache, None, 2, at, 1, 0, None) == zo.ZO_ERR_NULL
+    assert lib.zo_cache_copy(cache, two, 0, at, 1, 0, None) == lib.zo_cache_copy(cache, two, 2, None, 0, 0, None) == zo.ZO_OK
+    assert lib.zo_cache_copy(cache, two, 2, at, 1, 9, None) == zo.ZO_ERR_ARG
 
 
 def test_binding_refuses_what_is_not_on_the_device():
@@ -123,8 +126,8 @@ def test_binding_refuses_what_is_not_on_the_device():
         zo.zo_norm_rotate(None, None, i)
     with pytest.raises(TypeError):
         zo.zo_cache_attend(x, x, x, i, i)
-    with pytest.raises(ValueError):
-        zo.zo_cache_attend(x[0], x, x, i, i)
+    with pytest.raises(TypeError):
+        zo.zo_cache_attend(None, x, x, i, i)
     with pytest.raises(TypeError):
         zo.zo_draw(x[0], i)
     with pytest.raises(ValueError):
