@@ -3,17 +3,23 @@
 // Mathematics. Weights are whole numbers, w_i = round(2^44 exp((l_i - max) / T)), from fp64 exponentials;
 // their sums (below 2^62 for 2^18 tokens) are exact in any order, so the token is the same whatever the
 // order of the additions, and atomics may be used. Top-k, top-p and min-p each keep a prefix of the
-// falling order, so what is kept is all logits above a cut and, of those equal to it, the first `ties`
-// by index. The cut is found without sorting: logits map to 32-bit keys of the same order; a
-// histogram of counts and weights over 2,048 equal ranges of keys tells in which range the k-th
-// token, or the token at which the weight reaches top_p's share, lies; that range is divided again until
-// it holds a single key (at most three times).
-// The drawn token is then found in index order: weights of runs of 512 tokens, their running sums,
-// and the tokens of the run that holds the drawn share.
+// falling order (logit, then index), so what is kept is all tokens down to a last one. That one is found
+// without sorting the row:
+//   top-k up to 512  The k-th largest of the threads' own maxima is below no more than k - 1 tokens. What
+//                    reaches it (few more than k) goes into a list in LDS, the only part that is sorted
+//                    and weighed.
+//   top-p alone      Weights are added up in 2,888 equal ranges of (l - max) / T; the range in which
+//                    top_p's share is reached goes into the list, and tokens above it are kept anyway.
+//   otherwise        (more ties than the list holds, or a larger k) Ranges of 32-bit keys of the logits'
+//                    order are divided until one key is left, by 2,048 counts and weights at a time.
+// The drawn token is then found in index order: weights of runs of 512 tokens, their running sums, and
+// the tokens of the run that holds the drawn share.
 //
-// The row is read from HBM once; later passes find it in the L2 (608 KB at 152 k fp32 logits).
+// The row is read from HBM once; later passes find it in the L2 (608 KB at 152 k fp32 logits). Bound by
+// the fp64 exponentials of one CU where every token's weight is needed, else by its reads.
 
 #include <cmath>
+#include <type_traits>
 
 #include "zo_checks.h"
 #include "zo_lanes.h"
@@ -26,24 +32,56 @@ constexpr uint32_t kBuckets = 2048;
 constexpr uint32_t kRun = 512;                  // tokens of a run: 8 for each lane of a wave
 constexpr uint32_t kRuns = (1u << 18) / kRun;   // at most
 constexpr double kOne = 17592186044416.0;       // 2^44
+constexpr uint32_t kList = 4096;                // tokens that are sorted, at most
+constexpr int32_t kMostK = 512;                 // top-k by the threads' maxima
+constexpr uint32_t kSteps = 1024;               // of the exponential's table, for a factor of 2
+constexpr uint32_t kRanges = 2888;              // of 16 steps, down to the smallest weight (45 halvings)
 
-// Order of logits as unsigned numbers; NaN as -inf, both zeros as one.
+
+// A logit as it counts: NaN as -inf, +inf as the largest finite number. The median of three of which one is a NaN is
+// the smallest; the instruction itself, since the compiler takes the median with -inf for a minimum, NaN or not.
+__device__ __forceinline__ float sound(float l) {
+  float r;
+  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(l), "v"(-INFINITY), "v"(3.40282346638528860e38f));
+  return r;
+}
+
+// Order of logits as unsigned numbers; both zeros are one.
 __device__ __forceinline__ uint32_t key_of(float l) {
-  const uint32_t b = __float_as_uint(l == l ? l + 0.0f : -INFINITY);
+  const uint32_t b = __float_as_uint(l + 0.0f);
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key);
 }
 
+// exp by table and polynomial (P. Tang, 1989): x = (1024 q + j + f) ln 2 / 1024, |f| <= 1/2, exp x = 2^q 2^(j/1024) e^r
+// with r = f ln 2 / 1024 below 3.4e-4, where the third-degree Taylor polynomial is off by 6e-16; with the rounding of
+// x - r times its weight, the weight is off by less than 2^-49 where its last place is 2^-44. The whole number
+// n = 1024 q + j also gives the token's range, counted down from the largest logit.
 struct Weigh {
   double max, inv;  // 1 / temperature
-  bool at_inf;      // the largest logit is +inf
+  const double* table;  // 2^(44 + j / 1024), LDS
+  // n: 0 .. -16 kRanges (of a weight that is not 0). Straight-line code, so that several tokens' chains of
+  // operations overlap. Rounding to whole numbers is the addition of a power of two whose last place is 1,
+  // and scaling by 2^q an addition to the exponent: fp64 operations take twice as long as others, its
+  // conversions longer.
+  __device__ __forceinline__ uint64_t operator()(float l, int& n) const {
+    const double x = fmax((static_cast<double>(l) - max) * inv, -32.0);  // a weight of 0 from -31.2 on (and of 0 times inf)
+    constexpr double kRound = 6755399441055744.0;  // 1.5 2^52
+    const double shifted = fma(x, kSteps * 1.4426950408889634074, kRound), k = shifted - kRound;
+    n = static_cast<int>(__builtin_bit_cast(uint64_t, shifted));
+    const double r = fma(k, -0.69314718055994530942 / kSteps, x);
+    const double e = fma(r * r, fma(r, 1.0 / 6, 0.5), r);
+    const double t = table[n & (kSteps - 1)];
+    const uint64_t y = __builtin_bit_cast(uint64_t, fma(t, e, t));
+    const uint32_t scaled = static_cast<uint32_t>(y >> 32) + (static_cast<uint32_t>(n & ~static_cast<int>(kSteps - 1)) << 10);
+    const double w = __builtin_bit_cast(double, static_cast<uint64_t>(scaled) << 32 | static_cast<uint32_t>(y));
+    return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+  }
   __device__ __forceinline__ uint64_t operator()(float l) const {
-    if (at_inf) return l == INFINITY ? 1ull << 44 : 0ull;
-    const double x = (static_cast<double>(l) - max) * inv;
-    if (!(x > -31.25)) return 0;  // less than half of 2^-44 (and NaN)
-    return static_cast<uint64_t>(rint(exp(x) * kOne));
+    int n;
+    return (*this)(l, n);
   }
 };
 
@@ -52,32 +90,98 @@ __device__ __forceinline__ uint64_t share(uint64_t weight, uint32_t parts) {
   return (weight >> 24) * parts + (((weight & 0xFFFFFF) * parts) >> 24);
 }
 
+template <class S>
+struct Eight {  // 8 logits as they are stored
+  u32x4 v[sizeof(typename S::storage) / 2];
+};
+
+template <class S>
+__device__ __forceinline__ Eight<S> load_eight(const typename S::storage* at) {
+  constexpr uint32_t kParts = sizeof(typename S::storage) / 2;
+  Eight<S> x;
+#pragma unroll
+  for (uint32_t c = 0; c < kParts; ++c) x.v[c] = *reinterpret_cast<const u32x4_any*>(at + c * (8 / kParts));
+  return x;
+}
+
+template <class S>
+__device__ __forceinline__ void unpack_eight(const Eight<S>& x, float (&l)[8]) {
+  if constexpr (sizeof(typename S::storage) == 2) {
+    S::unpack(x.v[0], l);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) l[e] = __uint_as_float(x.v[e / 4][e % 4]);
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) l[e] = sound(l[e]);
+}
+
 // The 8 logits of a row from index i on (-inf behind the end).
 template <class S>
 __device__ __forceinline__ void load8(const typename S::storage* row, uint32_t i, uint32_t vocab, float (&l)[8]) {
   if (i + 8 <= vocab) {
-    if constexpr (sizeof(typename S::storage) == 2) {
-      S::unpack(*reinterpret_cast<const u32x4_any*>(row + i), l);
-    } else {
-      float a[4], b[4];
-      S::unpack(*reinterpret_cast<const u32x4_any*>(row + i), a);
-      S::unpack(*reinterpret_cast<const u32x4_any*>(row + i + 4), b);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        l[e] = a[e];
-        l[4 + e] = b[e];
-      }
-    }
+    unpack_eight<S>(load_eight<S>(row + i), l);
   } else {
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) l[e] = i + e < vocab ? S::load1(row + i + e) : -INFINITY;
+    for (uint32_t e = 0; e < 8; ++e) l[e] = i + e < vocab ? sound(S::load1(row + i + e)) : -INFINITY;
   }
 }
 
-__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+template <class S, uint32_t kBatch, class F>
+__device__ __forceinline__ uint32_t walk_batches(const typename S::storage* row, uint32_t vocab, uint32_t run0, F& f) {
+  constexpr uint32_t kStep = kWaves * kRun;
+  const uint32_t lane0 = threadIdx.x % 64 * 8;
+#pragma unroll 1
+  for (; run0 + (kBatch - 1) * kStep + kRun <= vocab; run0 += kBatch * kStep) {
+    Eight<S> x[kBatch];
 #pragma unroll
-  for (int m = 32; m > 0; m /= 2) v += __shfl_xor(v, m, 64);
-  return v;
+    for (uint32_t u = 0; u < kBatch; ++u) x[u] = load_eight<S>(row + run0 + u * kStep + lane0);
+#pragma unroll
+    for (uint32_t u = 0; u < kBatch; ++u) {
+      float l[8];
+      unpack_eight<S>(x[u], l);
+      f(run0 + u * kStep + lane0, l);
+    }
+  }
+  return run0;
+}
+
+// Calls f(index of the first, logits) for the eights of a row that this lane has: wave w takes runs w, w + kWaves,
+// .. (a lane 8 tokens of each), kBatch of them loaded before the first is used, as long as there are so many. All
+// lanes of a wave make the same calls; tokens behind the end are -inf.
+template <class S, uint32_t kBatch, class F>
+__device__ __forceinline__ void walk(const typename S::storage* row, uint32_t vocab, F f) {
+  uint32_t run0 = __builtin_amdgcn_readfirstlane(threadIdx.x / 64) * kRun;
+  run0 = walk_batches<S, kBatch>(row, vocab, run0, f);
+  if constexpr (kBatch > 2) run0 = walk_batches<S, 2>(row, vocab, run0, f);
+#pragma unroll 1
+  for (; run0 < vocab; run0 += kWaves * kRun) {
+    float l[8];
+    const uint32_t i = run0 + threadIdx.x % 64 * 8;
+    load8<S>(row, i, vocab, l);
+    f(i, l);
+  }
+}
+
+// The sum over a wave, the same in all lanes: rows of 16 by data-parallel moves, the four rows in scalars.
+__device__ __forceinline__ uint64_t wave_sum(uint64_t v) {
+  const auto add = [&](auto ctrl) {
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(v), ctrl.value, 0xF, 0xF, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<uint32_t>(v >> 32), ctrl.value, 0xF, 0xF, true);
+    v += static_cast<uint64_t>(hi) << 32 | lo;
+  };
+  add(std::integral_constant<int, 0xB1>{});   // neighbours
+  add(std::integral_constant<int, 0x4E>{});   // pairs of a quad
+  add(std::integral_constant<int, 0x141>{});  // quads of a half row
+  add(std::integral_constant<int, 0x140>{});  // halves of a row
+  uint64_t sum = 0;
+#pragma unroll
+  for (int row = 0; row < 64; row += 16) {
+    const uint32_t lo = __builtin_amdgcn_readlane(static_cast<uint32_t>(v), row);
+    const uint32_t hi = __builtin_amdgcn_readlane(static_cast<uint32_t>(v >> 32), row);
+    sum += static_cast<uint64_t>(hi) << 32 | lo;
+  }
+  return sum;
 }
 
 __device__ __forceinline__ uint64_t wave_upto(uint64_t v) {  // sum over this and the lanes before
@@ -90,14 +194,26 @@ __device__ __forceinline__ uint64_t wave_upto(uint64_t v) {  // sum over this an
 }
 
 struct Lds {
-  uint64_t weight[kBuckets];
-  uint32_t count[kBuckets];
+  union {
+    struct {  // find_cut
+      uint64_t weight[kBuckets];
+      uint32_t count[kBuckets];
+    };
+    uint64_t range[kRanges];
+    float kept[4 * kThreads];  // a few logits for each thread
+    struct {
+      uint64_t list[kList];         // ~key << 32 | index: in rising order, tokens in falling order
+      uint64_t list_weight[kList];
+    };
+  };
+  double table[kSteps];
   uint64_t part_weight[kWaves];
   uint64_t part_count[kWaves];
   uint64_t run_weight[kRuns];
   uint32_t run_ties[kRuns];
+  uint32_t thread_max[kThreads];
   uint64_t before_weight, found_weight;
-  uint32_t before_count, found, found_count;
+  uint32_t before_count, found, found_count, listed, bound[2];
 };
 
 // Sums of (weight, count) over the threads before this one, and over all.
@@ -123,16 +239,143 @@ __device__ __forceinline__ void block_before(Lds& s, uint64_t w, uint64_t c, uin
   }
 }
 
-// A cut: logits with key > key are kept, of those with key == key the first `ties` by index.
+// The last token that is kept: those of a larger key are, and of the same key those up to `last`.
 struct Cut {
-  uint32_t key, ties;
-  uint64_t weight;  // of all that is kept
+  uint32_t key, last;
+  uint64_t weight;  // of all that is kept (find_cut)
+  __device__ __forceinline__ bool keeps(uint32_t k, uint32_t index) const { return k > key || (k == key && index <= last); }
 };
+
+// The index of the n-th token (from 1) of a key.
+template <class S>
+__device__ __forceinline__ uint32_t index_of_tie(Lds& s, const typename S::storage* row, uint32_t vocab, uint32_t key, uint32_t n) {
+  const uint32_t runs = (vocab + kRun - 1) / kRun;
+  for (uint32_t run = threadIdx.x / 64; run < runs; run += kWaves) {
+    float l[8];
+    load8<S>(row, run * kRun + threadIdx.x % 64 * 8, vocab, l);
+    uint32_t ties = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ties += key_of(l[e]) == key ? 1 : 0;
+    ties = static_cast<uint32_t>(wave_sum(ties));
+    if (threadIdx.x % 64 == 0) s.run_ties[run] = ties;
+  }
+  __syncthreads();
+  const uint64_t mine = threadIdx.x < runs ? s.run_ties[threadIdx.x] : 0;
+  uint64_t before, all, x, y;
+  block_before(s, 0, mine, x, before, y, all);
+  if (before < n && n <= before + mine) {  // one run of all
+    s.found = threadIdx.x;
+    s.before_count = static_cast<uint32_t>(before);
+  }
+  __syncthreads();
+  if (threadIdx.x < 64) {
+    const uint32_t i0 = s.found * kRun + threadIdx.x * 8;
+    float l[8];
+    load8<S>(row, i0, vocab, l);
+    uint32_t ties = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ties += key_of(l[e]) == key ? 1 : 0;
+    uint32_t at = s.before_count + static_cast<uint32_t>(wave_upto(ties)) - ties;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (key_of(l[e]) == key && ++at == n) s.found_count = i0 + e;
+  }
+  __syncthreads();
+  return s.found_count;
+}
+
+// Sorts the first n entries of the list (n <= kList, all different), smallest first. Up to 512 by counting for each
+// how many are smaller, with no barrier between; longer ones by a bitonic network.
+__device__ __forceinline__ void sort_list(Lds& s, uint32_t n) {
+  if (n <= 512) {
+    __syncthreads();
+    uint64_t mine = 0;
+    uint32_t rank = 0;
+    if (threadIdx.x < n) {
+      mine = s.list[threadIdx.x];
+#pragma unroll 8
+      for (uint32_t i = 0; i < n; ++i) rank += s.list[i] < mine ? 1 : 0;
+    }
+    __syncthreads();
+    if (threadIdx.x < n) s.list[rank] = mine;
+    __syncthreads();
+    return;
+  }
+  uint32_t size = 1024;
+  while (size < n) size *= 2;
+  for (uint32_t i = n + threadIdx.x; i < size; i += kThreads) s.list[i] = ~0ull;
+  for (uint32_t run = 2; run <= size; run *= 2)
+    for (uint32_t gap = run / 2; gap > 0; gap /= 2) {
+      __syncthreads();
+      for (uint32_t i = threadIdx.x; i < size / 2; i += kThreads) {
+        const uint32_t a = 2 * i - (i & (gap - 1)), b = a + gap;
+        const uint64_t x = s.list[a], y = s.list[b];
+        if ((x > y) == ((a & run) == 0)) {
+          s.list[a] = y;
+          s.list[b] = x;
+        }
+      }
+    }
+  __syncthreads();
+}
+
+// Adds the tokens of a row from logit `low` to `high` to the list; false: there are more than it holds.
+template <class S>
+__device__ __forceinline__ bool fill_list(Lds& s, const typename S::storage* row, uint32_t vocab, float low, float high) {
+  if (threadIdx.x == 0) s.listed = 0;
+  __syncthreads();
+  walk<S, 8>(row, vocab, [&](uint32_t i, const float(&l)[8]) {
+    float best = l[0];
+#pragma unroll
+    for (uint32_t e = 1; e < 8; ++e) best = fmaxf(best, l[e]);
+    if (!(best >= low)) return;  // most lanes of most waves
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      if (!(l[e] >= low && l[e] <= high) || i + e >= vocab) continue;
+      const uint32_t at = atomicAdd(&s.listed, 1u);
+      if (at < kList) s.list[at] = static_cast<uint64_t>(~key_of(l[e])) << 32 | (i + e);
+    }
+  });
+  __syncthreads();
+  return s.listed <= kList;
+}
+
+// Weighs the sorted list and finds what top-k, top-p and min-p keep of it, given the weight above it. all: weight
+// of everything that top-p shares out; 0: of the list's first k. Returns the number kept; their weights
+// are in list_weight.
+__device__ __forceinline__ uint32_t cut_list(Lds& s, uint32_t n, const Weigh& weigh, uint32_t k, uint64_t above, uint64_t all, bool by_weight, uint32_t parts,
+                             uint64_t least) {
+  constexpr uint32_t kEach = kList / kThreads;
+  uint64_t w[kEach], sum = 0;
+#pragma unroll
+  for (uint32_t j = 0; j < kEach; ++j) {
+    const uint32_t i = threadIdx.x * kEach + j;
+    w[j] = i < n && i < k ? (weigh(logit_of(~static_cast<uint32_t>(s.list[i] >> 32)))) : 0;
+    s.list_weight[i] = w[j];
+    sum += w[j];
+  }
+  uint64_t before, total, x, y;
+  block_before(s, sum, 0, before, x, total, y);
+  uint64_t need = ~0ull;
+  if (by_weight) {
+    need = share(all ? all : total, parts);
+    if (need == 0) need = 1;
+  }
+  uint32_t kept = 0;
+  before += above;
+#pragma unroll
+  for (uint32_t j = 0; j < kEach; ++j) {  // each keeps a prefix
+    if (w[j] > 0 && before < need && w[j] >= least) ++kept;
+    before += w[j];
+  }
+  block_before(s, 0, kept, x, before, y, total);
+  return static_cast<uint32_t>(total);
+}
 
 // The cut at which the count reaches `most`, or (by_weight) the weight reaches `need`, whichever is
 // asked for; false: the row's weights end before. Tokens of no weight do not count.
 template <class S>
-__device__ bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab, const Weigh& weigh, uint32_t top, bool by_weight,
+__device__ __attribute__((noinline)) bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab, const Weigh& weigh, uint32_t top, bool by_weight,
                          uint64_t need, Cut& cut) {
   uint32_t hi = top, lo = 0;
   uint64_t above_weight = 0, above_count = 0;
@@ -144,11 +387,9 @@ __device__ bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab,
       s.count[b] = 0;
     }
     __syncthreads();
-    for (uint32_t i = threadIdx.x * 8; i < vocab; i += kThreads * 8) {
-      float l[8];
-      load8<S>(row, i, vocab, l);
+    walk<S, 2>(row, vocab, [&](uint32_t, const float(&l)[8]) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
+      for (uint32_t e = 0; e < 8; ++e) {
         const uint32_t key = key_of(l[e]);
         if (key < lo || key > hi) continue;
         const uint64_t w = weigh(l[e]);
@@ -157,22 +398,25 @@ __device__ bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab,
         atomicAdd(reinterpret_cast<unsigned long long*>(&s.weight[b]), static_cast<unsigned long long>(w));
         atomicAdd(&s.count[b], 1u);
       }
-    }
+    });
     __syncthreads();
-    uint64_t w[2], c[2], w_before, c_before, w_all, c_all;
+    constexpr uint32_t kEach = kBuckets / kThreads;
+    uint64_t w[kEach], c[kEach], w_sum = 0, c_sum = 0, w_before, c_before, w_all, c_all;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      w[j] = s.weight[2 * threadIdx.x + j];
-      c[j] = s.count[2 * threadIdx.x + j];
+    for (uint32_t j = 0; j < kEach; ++j) {
+      w[j] = s.weight[kEach * threadIdx.x + j];
+      c[j] = s.count[kEach * threadIdx.x + j];
+      w_sum += w[j];
+      c_sum += c[j];
     }
-    block_before(s, w[0] + w[1], c[0] + c[1], w_before, c_before, w_all, c_all);
+    block_before(s, w_sum, c_sum, w_before, c_before, w_all, c_all);
     if ((by_weight ? above_weight + w_all : above_count + c_all) < need) return false;
     uint64_t wb = above_weight + w_before, cb = above_count + c_before;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (uint32_t j = 0; j < kEach; ++j) {
       const uint64_t was = by_weight ? wb : cb, now = was + (by_weight ? w[j] : c[j]);
       if (was < need && now >= need) {  // one bucket of all
-        s.found = 2 * threadIdx.x + j;
+        s.found = kEach * threadIdx.x + j;
         s.before_weight = wb;
         s.before_count = static_cast<uint32_t>(cb);
         s.found_weight = w[j];
@@ -195,8 +439,9 @@ __device__ bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab,
       cut.key = hi;
       uint64_t ties = by_weight ? (need - above_weight + each - 1) / each : need - above_count;
       if (ties > count) ties = count;
-      cut.ties = static_cast<uint32_t>(ties);
       cut.weight = above_weight + ties * each;
+      cut.last = vocab;
+      if (ties < count) cut.last = index_of_tie<S>(s, row, vocab, hi, static_cast<uint32_t>(ties));
       return true;
     }
   }
@@ -213,24 +458,41 @@ struct Draw {
   uint32_t vocab;
 };
 
+// The largest key that `takes` does not take, for a `takes` that takes all keys from one on, and not 0. A wave tries
+// 64 keys at a time.
+template <class F>
+__device__ __forceinline__ uint32_t last_untaken(F takes) {
+  uint32_t key = 0;
+#pragma unroll 1
+  for (int shift = 26; shift > -6; shift -= 6) {
+    const int at = shift < 0 ? 0 : shift;
+    const uint32_t trial = key + ((threadIdx.x % 64) << at);
+    const bool mine = shift >= 0 || threadIdx.x % 64 < 4;  // the last round has two bits
+    key += (__popcll(__ballot(mine && !takes(trial))) - 1) << at;
+  }
+  return key;
+}
+
 template <class S>
 __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   typedef typename S::storage T;
   __shared__ Lds s;
   const uint32_t b = blockIdx.x, vocab = a.vocab;
   const T* row = reinterpret_cast<const T*>(a.logits) + static_cast<int64_t>(b) * a.row_stride;
+  for (uint32_t i = threadIdx.x; i < kSteps; i += kThreads) s.table[i] = exp2(44.0 + static_cast<double>(i) / kSteps);
 
   // the largest logit and its lowest index
-  uint64_t best = 0;
-  for (uint32_t i = threadIdx.x * 8; i < vocab; i += kThreads * 8) {
-    float l[8];
-    load8<S>(row, i, vocab, l);
+  float mine = -INFINITY;
+  uint32_t at = 0xFFFFFFFFu;
+  walk<S, 8>(row, vocab, [&](uint32_t i, const float(&l)[8]) {
 #pragma unroll
     for (uint32_t e = 0; e < 8; ++e) {
-      const uint64_t k = static_cast<uint64_t>(key_of(l[e])) << 32 | (0xFFFFFFFFu - (i + e));
-      best = k > best ? k : best;
+      at = l[e] > mine ? i + e : at;
+      mine = l[e] > mine ? l[e] : mine;
     }
-  }
+  });
+  uint64_t best = static_cast<uint64_t>(key_of(mine)) << 32 | (0xFFFFFFFFu - at);
+  s.thread_max[threadIdx.x] = key_of(mine);
 #pragma unroll
   for (int m = 32; m > 0; m /= 2) {
     const uint64_t other = __shfl_xor(best, m, 64);
@@ -249,76 +511,159 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     }
     return;
   }
-  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature), max == INFINITY};
-
-  Cut cut{0, 0, 0};  // everything is above it
+  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature), s.table};
   const int32_t k = a.top_k ? a.top_k[b] : 0;
-  const float p = a.top_p ? a.top_p[b] : 1.0f;
-  bool cut_found = false;
-  if (k > 0 && static_cast<uint32_t>(k) < vocab)
-    cut_found = find_cut<S>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
-  if (p < 1.0f) {
-    uint64_t total = cut.weight;
-    if (!cut_found) {
-      uint64_t sum = 0;
-      for (uint32_t i = threadIdx.x * 8; i < vocab; i += kThreads * 8) {
-        float l[8];
-        load8<S>(row, i, vocab, l);
+  const float p = a.top_p ? a.top_p[b] : 1.0f, mp = a.min_p ? a.min_p[b] : 0.0f, u = a.u[b];
+  const bool by_count = k > 0 && static_cast<uint32_t>(k) < vocab, by_weight = p < 1.0f;
+  const uint32_t parts = p > 0.0f ? static_cast<uint32_t>(rint(static_cast<double>(fminf(p, 1.0f)) * 16777216.0)) : 0u;
+  const uint64_t least = mp > 0.0f ? static_cast<uint64_t>(rint(static_cast<double>(mp < 1.0f ? mp : 1.0f) * kOne)) : 1ull;
+  const uint32_t draw = !(u > 0.0f) ? 0u : u >= 1.0f ? 0xFFFFFFu : static_cast<uint32_t>(u * 16777216.0f);
+
+  if (by_count && k <= kMostK) {
+    // the upper half of the key of the k-th largest of the threads' maxima: one wave counts, 16 in each lane
+    if (threadIdx.x < 64) {
+      uint32_t m[kThreads / 64], least_max = top;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum += weigh(l[e]);
+      for (uint32_t i = 0; i < kThreads / 64; ++i) {
+        m[i] = s.thread_max[i * 64 + threadIdx.x];
+        least_max = min(least_max, m[i]);
       }
-      uint64_t x, y, z;
-      block_before(s, sum, 0, x, y, total, z);
+#pragma unroll
+      for (int i = 32; i > 0; i /= 2) least_max = min(least_max, static_cast<uint32_t>(__shfl_xor(static_cast<int>(least_max), i, 64)));
+      const uint32_t differ = top ^ least_max;  // bits above its first are the same in all
+      uint32_t bit = differ == 0 ? 0 : 0x80000000u >> __clz(differ), bound = bit == 0 ? top : top & ~(2 * bit - 1);
+      for (; bit > 0x8000u; bit /= 2) {
+        uint32_t count = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kThreads / 64; ++i) count += __popcll(__ballot(m[i] >= (bound | bit)));
+        if (count >= static_cast<uint32_t>(k)) bound |= bit;
+      }
+      if (threadIdx.x == 0) s.bound[0] = bound;
     }
-    const uint32_t parts = p > 0.0f ? static_cast<uint32_t>(rint(static_cast<double>(p) * 16777216.0)) : 0u;
+    __syncthreads();
+    // (a key below that of -inf takes everything in)
+    if (fill_list<S>(s, row, vocab, s.bound[0] > key_of(-INFINITY) ? logit_of(s.bound[0]) : -INFINITY, INFINITY)) {
+      const uint32_t n = s.listed;
+      sort_list(s, n);
+      const uint32_t kept = cut_list(s, n, weigh, static_cast<uint32_t>(k), 0, 0, by_weight, parts, least);
+      // what is kept in the order of indices, each with its place in the list
+      uint64_t entry = 0;
+      const uint32_t i = threadIdx.x;
+      if (i < kept) entry = s.list[i] << 32 | i;
+      __syncthreads();
+      if (i < kept) s.list[i] = entry;
+      sort_list(s, kept);
+      const uint64_t w = i < kept ? s.list_weight[s.list[i] & 0xFFFFFFFFu] : 0;
+      uint64_t before, all, x, y;
+      block_before(s, w, 0, before, x, all, y);
+      const uint64_t target = share(all, draw);
+      if (before <= target && target < before + w) {
+        a.tokens[b] = static_cast<int32_t>(s.list[i] >> 32);
+        if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w) / static_cast<double>(all)));
+      }
+      return;
+    }
+  }
+
+  Cut cut{0, vocab, 0};  // keeps everything
+  const bool counted = by_count && find_cut<S>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
+  if (by_weight && counted) {
+    const uint64_t need = share(cut.weight, parts);
+    find_cut<S>(s, row, vocab, weigh, top, true, need == 0 ? 1 : need, cut);
+  } else if (by_weight) {  // of all tokens that weigh anything: there are no more than k
+    __syncthreads();
+    for (uint32_t i = threadIdx.x; i < kRanges; i += kThreads) s.range[i] = 0;
+    __syncthreads();
+    walk<S, 2>(row, vocab, [&](uint32_t, const float(&l)[8]) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        int n;
+        const uint64_t w = weigh(l[e], n);
+        if (w > 0) atomicAdd(reinterpret_cast<unsigned long long*>(&s.range[-n / 16]), static_cast<unsigned long long>(w));
+      }
+    });
+    __syncthreads();
+    constexpr uint32_t kEach = (kRanges + kThreads - 1) / kThreads;
+    uint64_t w[kEach], sum = 0, before, total, x, y;
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const uint32_t i = threadIdx.x * kEach + j;
+      w[j] = i < kRanges ? s.range[i] : 0;
+      sum += w[j];
+    }
+    block_before(s, sum, 0, before, x, total, y);
     uint64_t need = share(total, parts);
     if (need == 0) need = 1;
-    Cut by_weight;
-    if (find_cut<S>(s, row, vocab, weigh, top, true, need, by_weight)) cut = by_weight;
-  }
-  const float mp = a.min_p ? a.min_p[b] : 0.0f;
-  const uint64_t least = mp > 0.0f ? static_cast<uint64_t>(rint(static_cast<double>(mp < 1.0f ? mp : 1.0f) * kOne)) : 0ull;
-
-  // weights above the cut and ties at it, of each run of 512 tokens
-  const uint32_t runs = (vocab + kRun - 1) / kRun;
-  for (uint32_t run = threadIdx.x / 64; run < runs; run += kWaves) {
-    float l[8];
-    load8<S>(row, run * kRun + threadIdx.x % 64 * 8, vocab, l);
-    uint64_t sum = 0;
-    uint32_t ties = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t key = key_of(l[e]);
-      if (key < cut.key) continue;
-      const uint64_t w = weigh(l[e]);
-      if (w < least) continue;
-      if (key > cut.key)
-        sum += w;
-      else
-        ++ties;
+    for (uint32_t j = 0; j < kEach; ++j) {
+      if (before < need && before + w[j] >= need) {  // one range of all
+        s.found = threadIdx.x * kEach + j;
+        s.before_weight = before;
+      }
+      before += w[j];
     }
-    sum = wave_sum(sum);
-    ties = static_cast<uint32_t>(wave_sum(ties));
-    if (threadIdx.x % 64 == 0) {
-      s.run_weight[run] = sum;
-      s.run_ties[run] = ties;
+    __syncthreads();
+    const int32_t found = static_cast<int32_t>(s.found);
+    const uint64_t above = s.before_weight;
+    // the keys of that range lie between the last ones that this range and the one above it do not reach
+    if (threadIdx.x < 128) {
+      const int32_t edge = threadIdx.x < 64 ? found : found - 1;
+      const uint32_t key = last_untaken([&](uint32_t key) {
+        if (key <= key_of(-INFINITY)) return false;
+        if (key >= top) return edge >= 0 || key > top;
+        int n;
+        return weigh(logit_of(key), n) > 0 && -n / 16 <= edge;
+      });
+      if (threadIdx.x % 64 == 0) s.bound[threadIdx.x / 64] = key;
+    }
+    __syncthreads();
+    if (fill_list<S>(s, row, vocab, logit_of(s.bound[0] + 1), logit_of(s.bound[1]))) {
+      const uint32_t n = s.listed;
+      sort_list(s, n);
+      const uint32_t kept = cut_list(s, n, weigh, n, above, total, true, parts, 0);
+      const uint64_t last = s.list[kept - 1];
+      cut.key = ~static_cast<uint32_t>(last >> 32);
+      cut.last = static_cast<uint32_t>(last);
+    } else {
+      find_cut<S>(s, row, vocab, weigh, top, true, need, cut);
     }
   }
+
+  __syncthreads();  // the list is read
+  // the kept weight of each run of 512 tokens
+  const uint32_t runs = (vocab + kRun - 1) / kRun;
+  walk<S, 2>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
+    uint32_t in = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) in |= cut.keeps(key_of(l[e]), i0 + e) ? 1u << e : 0u;
+    uint64_t sum = 0;
+    if (__any(__popc(in) > 4)) {
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const uint64_t w = weigh(l[e]);
+        sum += (in >> e & 1) && w >= least ? w : 0;
+      }
+    } else {  // few of the eight in any lane: those in a row of their own first
+      uint32_t kept = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e)
+        if (in >> e & 1) s.kept[kept++ * kThreads + threadIdx.x] = l[e];
+      for (uint32_t j = 0; __any(j < kept); ++j) {
+        const uint64_t w = weigh(j < kept ? s.kept[j * kThreads + threadIdx.x] : -INFINITY);
+        sum += w >= least ? w : 0;
+      }
+    }
+    const uint64_t all = wave_sum(sum);
+    if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
+  });
   __syncthreads();
-  const uint64_t tie_weight = weigh(logit_of(cut.key));
-  const uint64_t my_ties = threadIdx.x < runs ? s.run_ties[threadIdx.x] : 0;
-  uint64_t w_before, t_before, w_all, t_all, x;
-  block_before(s, 0, my_ties, x, t_before, w_all, t_all);
-  const auto kept_ties = [&](uint64_t before, uint64_t n) { return before >= cut.ties ? 0ull : n < cut.ties - before ? n : cut.ties - before; };
-  const uint64_t mine = threadIdx.x < runs ? s.run_weight[threadIdx.x] + kept_ties(t_before, my_ties) * tie_weight : 0;
-  block_before(s, mine, 0, w_before, x, w_all, t_all);
-  const float u = a.u[b];
-  const uint32_t draw = !(u > 0.0f) ? 0u : u >= 1.0f ? 0xFFFFFFu : static_cast<uint32_t>(u * 16777216.0f);
+  const uint64_t in_run = threadIdx.x < runs ? s.run_weight[threadIdx.x] : 0;
+  uint64_t w_before, w_all, x, y;
+  block_before(s, in_run, 0, w_before, x, w_all, y);
   const uint64_t target = share(w_all, draw);
-  if (w_before <= target && target < w_before + mine) {  // one run of all
+  if (w_before <= target && target < w_before + in_run) {  // one run of all
     s.found = threadIdx.x;
     s.before_weight = w_before;
-    s.before_count = static_cast<uint32_t>(t_before);
   }
   __syncthreads();
   if (threadIdx.x >= 64) return;
@@ -327,31 +672,16 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   const uint32_t i0 = s.found * kRun + threadIdx.x * 8;
   float l[8];
   load8<S>(row, i0, vocab, l);
-  uint64_t w[8];
-  uint32_t tie = 0, ties = 0;
+  uint64_t w[8], sum = 0;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t key = key_of(l[e]);
-    w[e] = key < cut.key ? 0 : weigh(l[e]);
+  for (uint32_t e = 0; e < 8; ++e) {
+    w[e] = cut.keeps(key_of(l[e]), i0 + e) ? (weigh(l[e])) : 0;
     if (w[e] < least) w[e] = 0;
-    if (key == cut.key && w[e] > 0) {
-      tie |= 1u << e;
-      ++ties;
-    }
-  }
-  uint64_t tb = s.before_count + wave_upto(ties) - ties;
-  uint64_t sum = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (tie >> e & 1) {
-      if (tb >= cut.ties) w[e] = 0;
-      ++tb;
-    }
     sum += w[e];
   }
   uint64_t upto = s.before_weight + wave_upto(sum) - sum;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
+  for (uint32_t e = 0; e < 8; ++e) {
     if (upto <= target && target < upto + w[e]) {
       a.tokens[b] = static_cast<int32_t>(i0 + e);
       if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w[e]) / static_cast<double>(w_all)));
