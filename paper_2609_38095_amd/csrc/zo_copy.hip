@@ -60,10 +60,10 @@ __global__ void __launch_bounds__(kThreads) copy_kernel(const Copy c) {
   T v[kHeads];
 #pragma unroll
   for (uint32_t h = 0; h < kHeads; ++h)
-    v[h] = *reinterpret_cast<const At*>(src + h * c.head_stride);
+    v[h] = __builtin_nontemporal_load(reinterpret_cast<const At*>(src + h * c.head_stride));
 #pragma unroll
   for (uint32_t h = 0; h < kHeads; ++h)
-    *reinterpret_cast<At*>(dst + h * c.head_stride) = v[h];
+    __builtin_nontemporal_store(v[h], reinterpret_cast<At*>(dst + h * c.head_stride));
 }
 
 template <int kVec>

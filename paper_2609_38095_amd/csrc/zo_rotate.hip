@@ -9,7 +9,7 @@
 // workgroup takes consecutive rows of one side, so that its gammas stay in registers and its few
 // tokens' sines and cosines are computed once into LDS and used by every head. A row is held by L
 // neighbouring lanes with two 16-byte vectors each, chosen so that both members of a pair are in one
-// lane: dims v and v + rotary / 2 for half pairs, 16 adjacent ones for interleaved pairs. The norm
+// lane: at dims v and v + rotary / 2 for half pairs, anywhere for interleaved pairs. The norm
 // is then a sum over L lanes by data-parallel moves, and nothing of a row passes through LDS.
 // Sizes that vectors do not divide take the same code with one element for a vector.
 //
@@ -55,28 +55,46 @@ struct Rotation {
   double turns[ZO_DIM_MAX / 2];
 };
 
-// One lane's share of a row. kVec elements make a vector; the lane holds kPairs times two vectors,
-// at dims a(n) and b(n). kInside: pairs lie inside a vector (2 i, 2 i + 1), else across the two.
+// One lane's share of a row. kVec elements make a vector; the lane holds kPairs times two vectors, at dims a(n) and
+// b(n), neighbouring lanes neighbouring vectors, so that each access of a wave covers whole lines (lanes with two
+// adjacent vectors each left every access with gaps: 16,387 fp32 tokens of 64 heads of 64, interleaved, took
+// 180 us with streaming stores). kInside: pairs lie inside a vector (2 i, 2 i + 1), else across the two.
 template <class S, int kVec, int kPairs, bool kInside>
 struct Share {
-  uint32_t a[kPairs], b[kPairs];
-  bool in_a[kPairs], in_b[kPairs], turn[kPairs];
+  uint32_t a[kPairs], b[kPairs], pair[kPairs];  // pair: of the angles, for a and b together or (inside) for a
+  bool in_a[kPairs], in_b[kPairs], turn_a[kPairs], turn_b[kPairs];
 
   __device__ void place(uint32_t lane, uint32_t lanes, uint32_t dim, uint32_t rotary, bool interleaved) {
 #pragma unroll
     for (int n = 0; n < kPairs; ++n) {
-      const uint32_t j = lane + n * lanes;  // pair of vectors
-      const uint32_t turning = rotary / (2 * kVec);
-      turn[n] = j < turning;
-      if (kInside || !turn[n] || interleaved) {
-        a[n] = 2 * kVec * j;
-        b[n] = a[n] + kVec;
-      } else {
+      const uint32_t j = lane + n * lanes, turning = rotary / (2 * kVec);
+      if (kInside) {
         a[n] = kVec * j;
+        b[n] = dim / 2 + a[n];
+        pair[n] = a[n] / 2;
+        in_a[n] = a[n] < dim / 2;
+        turn_a[n] = a[n] < rotary;
+        turn_b[n] = b[n] < rotary;
+      } else if (kVec == 1 && interleaved) {
+        a[n] = 2 * j;
+        b[n] = a[n] + 1;
+        pair[n] = j;
+        in_a[n] = a[n] < dim;
+        turn_a[n] = turn_b[n] = j < turning;
+      } else if (j < turning) {
+        a[n] = pair[n] = kVec * j;
         b[n] = a[n] + rotary / 2;
+        in_a[n] = true;
+        turn_a[n] = turn_b[n] = true;
+      } else {  // the rest of the row, in two halves (the first one longer by an element of an odd rest)
+        const uint32_t half = (dim - rotary + 1) / 2;
+        a[n] = rotary + kVec * (j - turning);
+        b[n] = a[n] + half;
+        pair[n] = 0;
+        in_a[n] = a[n] < rotary + half;
+        turn_a[n] = turn_b[n] = false;
       }
-      in_a[n] = a[n] < dim;
-      in_b[n] = b[n] < dim;
+      in_b[n] = in_a[n] && b[n] < dim;
     }
   }
 };
@@ -90,13 +108,16 @@ struct Raw<S, 1> {
   typename S::storage v;
 };
 
-template <class S, int kVec>
+// Streaming accesses (nothing is used twice) where the lanes of a row cover whole lines at a time, kWhole: 8 or more of
+// them. 8,192 packed bf16 tokens of 32 + 8 heads of 128, backward: 90 us with ordinary accesses, 62 with streaming ones;
+// 16,384 tokens of 64 heads of 64, whose accesses cover half lines: 58 and 66.
+template <class S, int kVec, bool kWhole>
 __device__ __forceinline__ Raw<S, kVec> ld(const char* base, int64_t elem) {
   const typename S::storage* p = reinterpret_cast<const typename S::storage*>(base) + elem;
   if constexpr (kVec == 1)
     return {*p};
   else
-    return {*reinterpret_cast<const u32x4_any*>(p)};
+    return {kWhole ? ld_stream(p) : *reinterpret_cast<const u32x4_any*>(p)};
 }
 
 template <class S, int kVec>
@@ -107,31 +128,39 @@ __device__ __forceinline__ void widen(const Raw<S, kVec>& r, float (&f)[kVec]) {
     S::unpack(r.v, f);
 }
 
-template <class S, int kVec>
+template <class S, int kVec, bool kWhole>
 __device__ __forceinline__ void st(char* base, int64_t elem, const float (&f)[kVec]) {
   typename S::storage* p = reinterpret_cast<typename S::storage*>(base) + elem;
   if constexpr (kVec == 1)
     S::store1(p, f[0]);
+  else if constexpr (kWhole)
+    st_stream(p, S::pack(f));
   else
     *reinterpret_cast<u32x4_any*>(p) = S::pack(f);
 }
 
-// A row's two vectors turned by the angles cs (cosine, sine of consecutive pairs); kBack: by the
-// opposite angles.
-template <int kVec, bool kInside, bool kBack>
-__device__ __forceinline__ void turn_pair(float (&a)[kVec], float (&b)[kVec], const float2* cs) {
+template <int kVec, bool kBack>
+__device__ __forceinline__ void turn_inside(float (&v)[kVec], const float2* cs) {
 #pragma unroll
-  for (int e = 0; e < kVec; ++e) {
+  for (int e = 0; e < kVec / 2; ++e) {
     const float2 t = cs[e];
-    const float s = kBack ? -t.y : t.y;
-    if constexpr (kInside) {
-      float(&v)[kVec] = e < kVec / 2 ? a : b;
-      const int i = 2 * (e % (kVec / 2));
-      const float p = v[i], q = v[i + 1];
-      v[i] = p * t.x - q * s;
-      v[i + 1] = p * s + q * t.x;
-    } else {
-      const float p = a[e], q = b[e];
+    const float s = kBack ? -t.y : t.y, p = v[2 * e], q = v[2 * e + 1];
+    v[2 * e] = p * t.x - q * s;
+    v[2 * e + 1] = p * s + q * t.x;
+  }
+}
+
+// A share's two vectors turned by the angles cs of a token (cosine and sine of each pair); kBack: by the opposite ones.
+template <int kVec, bool kInside, bool kBack, class Sh>
+__device__ __forceinline__ void turn_share(const Sh& sh, int n, float (&a)[kVec], float (&b)[kVec], const float2* cs) {
+  if constexpr (kInside) {
+    if (sh.turn_a[n]) turn_inside<kVec, kBack>(a, cs + sh.pair[n]);
+    if (sh.turn_b[n]) turn_inside<kVec, kBack>(b, cs + sh.b[n] / 2);
+  } else if (sh.turn_a[n]) {
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) {
+      const float2 t = cs[sh.pair[n] + e];
+      const float s = kBack ? -t.y : t.y, p = a[e], q = b[e];
       a[e] = p * t.x - q * s;
       b[e] = p * s + q * t.x;
     }
@@ -211,8 +240,8 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Rotation r, cons
     const int64_t at = static_cast<int64_t>(token0 + tok[i]) * sd.x_token + head[i] * sd.x_head;
 #pragma unroll
     for (int n = 0; n < kPairs; ++n) {
-      if (sh.in_a[n]) ra[i][n] = ld<S, kVec>(sd.x, at + sh.a[n]);
-      if (sh.in_b[n]) rb[i][n] = ld<S, kVec>(sd.x, at + sh.b[n]);
+      if (sh.in_a[n]) ra[i][n] = ld<S, kVec, (L >= 8)>(sd.x, at + sh.a[n]);
+      if (sh.in_b[n]) rb[i][n] = ld<S, kVec, (L >= 8)>(sd.x, at + sh.b[n]);
     }
   }
   float ga[kPairs][kVec], gb[kPairs][kVec];
@@ -220,8 +249,8 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Rotation r, cons
 #pragma unroll
     for (int n = 0; n < kPairs; ++n) {
       Raw<S, kVec> va = {}, vb = {};
-      if (sh.in_a[n]) va = ld<S, kVec>(sd.gamma, sh.a[n]);
-      if (sh.in_b[n]) vb = ld<S, kVec>(sd.gamma, sh.b[n]);
+      if (sh.in_a[n]) va = ld<S, kVec, false>(sd.gamma, sh.a[n]);
+      if (sh.in_b[n]) vb = ld<S, kVec, false>(sd.gamma, sh.b[n]);
       widen<S, kVec>(va, ga[n]);
       widen<S, kVec>(vb, gb[n]);
     }
@@ -261,15 +290,15 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const Rotation r, cons
     const bool live = t.live[tok[i]] != 0;
 #pragma unroll
     for (int n = 0; n < kPairs; ++n) {
-      if (sh.turn[n]) turn_pair<kVec, kInside, false>(a[n], b[n], t.cs + tok[i] * half + (threadIdx.x % L + n * L) * kVec);
+      turn_share<kVec, kInside, false>(sh, n, a[n], b[n], t.cs + tok[i] * half);
 #pragma unroll
       for (int e = 0; e < kVec; ++e) {
         a[n][e] = live ? a[n][e] : 0.0f;
         b[n][e] = live ? b[n][e] : 0.0f;
       }
       const int64_t at = place + head[i] * sd.y_head;
-      if (sh.in_a[n]) st<S, kVec>(sd.y, at + sh.a[n], a[n]);
-      if (sh.in_b[n]) st<S, kVec>(sd.y, at + sh.b[n], b[n]);
+      if (sh.in_a[n]) st<S, kVec, (L >= 8)>(sd.y, at + sh.a[n], a[n]);
+      if (sh.in_b[n]) st<S, kVec, (L >= 8)>(sd.y, at + sh.b[n], b[n]);
     }
   }
 }
@@ -295,8 +324,8 @@ __global__ void __launch_bounds__(kThreads) rotate_back_kernel(const Rotation r,
 #pragma unroll
   for (int n = 0; n < kPairs; ++n) {
     Raw<S, kVec> va = {}, vb = {};
-    if (sd.gamma && sh.in_a[n]) va = ld<S, kVec>(sd.gamma, sh.a[n]);
-    if (sd.gamma && sh.in_b[n]) vb = ld<S, kVec>(sd.gamma, sh.b[n]);
+    if (sd.gamma && sh.in_a[n]) va = ld<S, kVec, false>(sd.gamma, sh.a[n]);
+    if (sd.gamma && sh.in_b[n]) vb = ld<S, kVec, false>(sd.gamma, sh.b[n]);
     widen<S, kVec>(va, ga[n]);
     widen<S, kVec>(vb, gb[n]);
 #pragma unroll
@@ -321,10 +350,10 @@ __global__ void __launch_bounds__(kThreads) rotate_back_kernel(const Rotation r,
       const int64_t dat = static_cast<int64_t>(token0 + tok[i]) * sd.dy_token + head[i] * sd.dy_head;
 #pragma unroll
       for (int n = 0; n < kPairs; ++n) {
-        if (sh.in_a[n]) ya[i][n] = ld<S, kVec>(sd.dy, dat + sh.a[n]);
-        if (sh.in_b[n]) yb[i][n] = ld<S, kVec>(sd.dy, dat + sh.b[n]);
-        if (sd.gamma && sh.in_a[n]) xa[i][n] = ld<S, kVec>(sd.x, at + sh.a[n]);
-        if (sd.gamma && sh.in_b[n]) xb[i][n] = ld<S, kVec>(sd.x, at + sh.b[n]);
+        if (sh.in_a[n]) ya[i][n] = ld<S, kVec, (L >= 8)>(sd.dy, dat + sh.a[n]);
+        if (sh.in_b[n]) yb[i][n] = ld<S, kVec, (L >= 8)>(sd.dy, dat + sh.b[n]);
+        if (sd.gamma && sh.in_a[n]) xa[i][n] = ld<S, kVec, (L >= 8)>(sd.x, at + sh.a[n]);
+        if (sd.gamma && sh.in_b[n]) xb[i][n] = ld<S, kVec, (L >= 8)>(sd.x, at + sh.b[n]);
       }
     }
     __syncthreads();  // the tables of the rows before are read
@@ -340,7 +369,7 @@ __global__ void __launch_bounds__(kThreads) rotate_back_kernel(const Rotation r,
       for (int n = 0; n < kPairs; ++n) {
         widen<S, kVec>(ya[i][n], da[n]);
         widen<S, kVec>(yb[i][n], db[n]);
-        if (sh.turn[n]) turn_pair<kVec, kInside, true>(da[n], db[n], t.cs + k * half + (threadIdx.x % L + n * L) * kVec);
+        turn_share<kVec, kInside, true>(sh, n, da[n], db[n], t.cs + k * half);
       }
       if (sd.gamma) {
         float a[kPairs][kVec], b[kPairs][kVec];
@@ -378,8 +407,8 @@ __global__ void __launch_bounds__(kThreads) rotate_back_kernel(const Rotation r,
           da[n][e] = live ? da[n][e] : 0.0f;
           db[n][e] = live ? db[n][e] : 0.0f;
         }
-        if (sh.in_a[n]) st<S, kVec>(sd.y, at + sh.a[n], da[n]);
-        if (sh.in_b[n]) st<S, kVec>(sd.y, at + sh.b[n], db[n]);
+        if (sh.in_a[n]) st<S, kVec, (L >= 8)>(sd.y, at + sh.a[n], da[n]);
+        if (sh.in_b[n]) st<S, kVec, (L >= 8)>(sd.y, at + sh.b[n], db[n]);
       }
     }
   }
