@@ -208,7 +208,8 @@ int zo_cache_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensor
 
 /*
  * zo_draw -- draws a token for each row of logits from given random numbers.
- * Row b, logits l_i, i < vocab (NaN counts as -inf, +inf as the largest finite fp32 number): with
+ * Row b, logits l_i, i < vocab (NaN counts as -inf, +inf as the largest finite number of its type):
+ * with
  * m = max l_i the weight of token i is the whole number w_i = round(2^44 exp((l_i - m) / temperature[b])). In the order of falling logits, ties by index, kept are: the first
  * top_k[b] tokens (all if <= 0); of these the fewest first ones that hold floor(W P / 2^24) of their
  * weight W, P = round(2^24 top_p[b]) (at least one; all if top_p >= 1); of these those with

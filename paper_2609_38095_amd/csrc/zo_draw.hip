@@ -8,9 +8,11 @@
 //   top-k up to 512  The k-th largest of the threads' own maxima is below no more than k - 1 tokens. What
 //                    reaches it (few more than k) goes into a list in LDS, the only part that is sorted
 //                    and weighed.
-//   top-p alone      Weights are added up in 2,888 equal ranges of (l - max) / T; the range in which
+//   top-p alone      (fp32) Weights are added up in 2,888 equal ranges of (l - max) / T; the range in which
 //                    top_p's share is reached goes into the list, and tokens above it are kept anyway.
-//   otherwise        (more ties than the list holds, or a larger k) Ranges of 32-bit keys of the logits'
+//   bf16             has few values: 8 bits of each power of two between the largest logit and e^-31 of its weight. Their
+//                    tokens are counted, and each value is weighed once.
+//   otherwise        (more ties than the list holds, a larger k, or a temperature that spreads bf16 over too many values) Ranges of 32-bit keys of the logits'
 //                    order are divided until one key is left, by 2,048 counts and weights at a time.
 // The drawn token is then found in index order: weights of runs of 512 tokens, their running sums, and
 // the tokens of the run that holds the drawn share.
@@ -35,14 +37,18 @@ constexpr double kOne = 17592186044416.0;       // 2^44
 constexpr uint32_t kList = 4096;                // tokens that are sorted, at most
 constexpr int32_t kMostK = 512;                 // top-k by the threads' maxima
 constexpr uint32_t kSteps = 1024;               // of the exponential's table, for a factor of 2
+constexpr uint32_t kBins = 8192;                // values of a bf16 row that are weighed once each, at most
+constexpr uint32_t kSmall = 0x3A7F;             // bf16 below 2^-10 (of which there are very many values) share a bin
 constexpr uint32_t kRanges = 2888;              // of 16 steps, down to the smallest weight (45 halvings)
 
 
-// A logit as it counts: NaN as -inf, +inf as the largest finite number. The median of three of which one is a NaN is
+// A logit as it counts: NaN as -inf, +inf as the largest finite number of its type. The median of three of which one is a NaN is
 // the smallest; the instruction itself, since the compiler takes the median with -inf for a minimum, NaN or not.
+template <class S>
 __device__ __forceinline__ float sound(float l) {
+  const float most = __uint_as_float(sizeof(typename S::storage) == 2 ? 0x7F7F0000u : 0x7F7FFFFFu);
   float r;
-  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(l), "v"(-INFINITY), "v"(3.40282346638528860e38f));
+  asm("v_med3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(l), "v"(-INFINITY), "v"(most));
   return r;
 }
 
@@ -113,7 +119,7 @@ __device__ __forceinline__ void unpack_eight(const Eight<S>& x, float (&l)[8]) {
     for (int e = 0; e < 8; ++e) l[e] = __uint_as_float(x.v[e / 4][e % 4]);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) l[e] = sound(l[e]);
+  for (int e = 0; e < 8; ++e) l[e] = sound<S>(l[e]);
 }
 
 // The 8 logits of a row from index i on (-inf behind the end).
@@ -123,7 +129,7 @@ __device__ __forceinline__ void load8(const typename S::storage* row, uint32_t i
     unpack_eight<S>(load_eight<S>(row + i), l);
   } else {
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) l[e] = i + e < vocab ? sound(S::load1(row + i + e)) : -INFINITY;
+    for (uint32_t e = 0; e < 8; ++e) l[e] = i + e < vocab ? sound<S>(S::load1(row + i + e)) : -INFINITY;
   }
 }
 
@@ -201,6 +207,10 @@ struct Lds {
     };
     uint64_t range[kRanges];
     float kept[4 * kThreads];  // a few logits for each thread
+    struct {                   // bf16 by value
+      uint64_t bin_weight[kBins];
+      uint32_t bin_count[kBins];
+    };
     struct {
       uint64_t list[kList];         // ~key << 32 | index: in rising order, tokens in falling order
       uint64_t list_weight[kList];
@@ -212,7 +222,7 @@ struct Lds {
   uint64_t run_weight[kRuns];
   uint32_t run_ties[kRuns];
   uint32_t thread_max[kThreads];
-  uint64_t before_weight, found_weight;
+  uint64_t before_weight, found_weight, small_weight;
   uint32_t before_count, found, found_count, listed, bound[2];
 };
 
@@ -458,6 +468,106 @@ struct Draw {
   uint32_t vocab;
 };
 
+// bf16 values in their order, neighbouring values neighbouring numbers; all below 2^-10 are 0.
+__device__ __forceinline__ int code_of(float l) {
+  const uint32_t bits = __float_as_uint(l), a = (bits & 0x7FFFFFFFu) >> 16;
+  const int up = static_cast<int>(max(a, kSmall) - kSmall);
+  return bits & 0x80000000u ? -up : up;
+}
+__device__ __forceinline__ float value_of(int code) {  // not 0
+  const uint32_t a = static_cast<uint32_t>(code < 0 ? -code : code) + kSmall;
+  return __uint_as_float((code < 0 ? 0x8000u | a : a) << 16);
+}
+
+// Adds the weights of the tokens in `small` (few of a row).
+__device__ __forceinline__ void add_small(Lds& s, const float (&l)[8], uint32_t small, const Weigh& weigh) {
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e)
+    if (small >> e & 1) atomicAdd(reinterpret_cast<unsigned long long*>(&s.small_weight), static_cast<unsigned long long>(weigh(l[e])));
+}
+
+// A bf16 row by value: its weights come from one exponential for each value instead of each token, and top-k and
+// top-p from a count of each value's tokens. false: the values that weigh anything are more than the bins, or a cut falls
+// among those below 2^-10; nothing is done then.
+__device__ bool cut_by_value(Lds& s, const uint16_t* row, uint32_t vocab, const Weigh& weigh, int code_top, uint32_t bins,
+                             uint32_t k, bool by_weight, uint32_t parts, Cut& cut) {
+  const bool cuts = k > 0 || by_weight;
+  for (uint32_t i = threadIdx.x; i < bins; i += kThreads) s.bin_count[i] = 0;
+  if (threadIdx.x == 0) s.small_weight = 0;
+  __syncthreads();
+  if (cuts) {
+    walk<BF16, 4>(row, vocab, [&](uint32_t, const float(&l)[8]) {
+      uint32_t small = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {
+        const int code = code_of(l[e]);
+        const uint32_t bin = static_cast<uint32_t>(code_top - code);
+        if (bin < bins) atomicAdd(&s.bin_count[bin], 1u);
+        small |= code == 0 ? 1u << e : 0u;
+      }
+      if (small) add_small(s, l, small, weigh);
+    });
+  }
+  __syncthreads();
+  constexpr uint32_t kEach = kBins / kThreads;
+  uint64_t each[kEach], w_sum = 0, c_sum = 0, w_before, c_before, w_all, c_all;
+  uint32_t count[kEach];
+  const uint32_t i0 = threadIdx.x * kEach;
+#pragma unroll
+  for (uint32_t j = 0; j < kEach; ++j) {
+    const int code = code_top - static_cast<int>(i0 + j);
+    const bool in = i0 + j < bins;
+    each[j] = in && code != 0 ? weigh(value_of(code)) : 0;
+    count[j] = in && (code == 0 || each[j] > 0) ? s.bin_count[i0 + j] : 0;
+    s.bin_weight[i0 + j] = each[j];
+    w_sum += in && code == 0 ? s.small_weight : count[j] * each[j];
+    c_sum += count[j];
+  }
+  if (!cuts) {
+    __syncthreads();
+    return true;
+  }
+  block_before(s, w_sum, c_sum, w_before, c_before, w_all, c_all);
+  // first the count's bin, then, with the weight down to there, the weight's
+  uint64_t all = w_all;
+  bool found = false;
+  for (int round = 0; round < 2; ++round) {
+    const bool weight = round == 1;
+    if (weight ? !by_weight : k == 0 || c_all < k) continue;
+    uint64_t need = weight ? share(all, parts) : k;
+    if (need == 0) need = 1;
+    uint64_t wb = w_before, cb = c_before;
+#pragma unroll
+    for (uint32_t j = 0; j < kEach; ++j) {
+      const bool small = code_top == static_cast<int>(i0 + j);
+      const uint64_t w = small ? s.small_weight : count[j] * each[j];
+      const uint64_t was = weight ? wb : cb, now = was + (weight ? w : count[j]);
+      if (was < need && now >= need) {  // one bin of all
+        const uint64_t ties = weight ? (small ? 0 : (need - wb + each[j] - 1) / each[j]) : need - cb;
+        s.found = i0 + j;
+        s.found_count = small || ties < count[j] ? static_cast<uint32_t>(ties) : 0;  // 0: all of its tokens
+        s.before_weight = wb + ties * each[j];
+      }
+      wb += w;
+      cb += count[j];
+    }
+    __syncthreads();
+    found = true;
+    all = s.before_weight;
+    const int code = code_top - static_cast<int>(s.found);
+    const uint32_t ties = s.found_count;
+    __syncthreads();
+    if (code == 0) return false;
+    cut.key = key_of(value_of(code));
+    cut.last = ties;  // for now
+  }
+  if (found && cut.last > 0)
+    cut.last = index_of_tie<BF16>(s, row, vocab, cut.key, cut.last);
+  else
+    cut.last = vocab;
+  return true;
+}
+
 // The largest key that `takes` does not take, for a `takes` that takes all keys from one on, and not 0. A wave tries
 // 64 keys at a time.
 template <class F>
@@ -566,11 +676,24 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   }
 
   Cut cut{0, vocab, 0};  // keeps everything
-  const bool counted = by_count && find_cut<S>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
+  bool binned = false;
+  int code_top = 0;
+  uint32_t bins = 0;
+  if constexpr (sizeof(T) == 2) {
+    code_top = code_of(max);
+    const int code_low = code_of(static_cast<float>(weigh.max - 32.0 * static_cast<double>(temperature)));
+    bins = static_cast<uint32_t>(code_top - code_low) + 1;
+    __syncthreads();  // the list is read
+    if (bins <= kBins) {
+      binned = cut_by_value(s, row, vocab, weigh, code_top, bins, by_count ? static_cast<uint32_t>(k) : 0u, by_weight, parts, cut);
+      if (!binned) cut = Cut{0, vocab, 0};
+    }
+  }
+  const bool counted = !binned && by_count && find_cut<S>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
   if (by_weight && counted) {
     const uint64_t need = share(cut.weight, parts);
     find_cut<S>(s, row, vocab, weigh, top, true, need == 0 ? 1 : need, cut);
-  } else if (by_weight) {  // of all tokens that weigh anything: there are no more than k
+  } else if (!binned && by_weight) {  // of all tokens that weigh anything: there are no more than k
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kRanges; i += kThreads) s.range[i] = 0;
     __syncthreads();
@@ -632,6 +755,33 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   __syncthreads();  // the list is read
   // the kept weight of each run of 512 tokens
   const uint32_t runs = (vocab + kRun - 1) / kRun;
+  if (binned) {
+    const uint32_t cut_bin = cut.key == 0 ? bins : static_cast<uint32_t>(code_top - code_of(logit_of(cut.key)));
+    walk<S, 4>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
+      uint64_t sum = 0;
+      uint32_t small = 0;
+#pragma unroll
+      for (uint32_t e = 0; e < 8; ++e) {  // (the bin of small values weighs nothing here)
+        const int code = code_of(l[e]);
+        const uint32_t bin = static_cast<uint32_t>(code_top - code);
+        const bool in = bin < bins && (bin < cut_bin || (bin == cut_bin && i0 + e <= cut.last));
+        if (in) {
+          const uint64_t w = s.bin_weight[bin];
+          sum += w >= least ? w : 0;
+          small |= code == 0 ? 1u << e : 0u;
+        }
+      }
+      if (small) {
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e) {
+          const uint64_t w = small >> e & 1 ? weigh(l[e]) : 0;
+          sum += w >= least ? w : 0;
+        }
+      }
+      const uint64_t all = wave_sum(sum);
+      if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
+    });
+  } else
   walk<S, 2>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
     uint32_t in = 0;
 #pragma unroll
