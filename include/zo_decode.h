@@ -209,15 +209,15 @@ int zo_cache_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensor
 /*
  * zo_draw -- draws a token for each row of logits from given random numbers.
  * Row b, logits l_i, i < vocab (NaN counts as -inf, +inf as the largest finite number of its type):
- * with
- * m = max l_i the weight of token i is the whole number w_i = round(2^44 exp((l_i - m) / temperature[b])). In the order of falling logits, ties by index, kept are: the first
- * top_k[b] tokens (all if <= 0); of these the fewest first ones that hold floor(W P / 2^24) of their
- * weight W, P = round(2^24 top_p[b]) (at least one; all if top_p >= 1); of these those with
- * w_i >= round(2^44 min(min_p[b], 1)). The token is the lowest index i at which the kept weight of
- * tokens 0 .. i exceeds floor(W' U / 2^24), W' the kept weight, U = floor(2^24 u[b]) clipped to
- * [0, 2^24). Every sum is of whole numbers, so the token is exact. temperature <= 0 (or
- * NaN) takes the lowest index of the largest logit (logprob 0). A row without any weight (all -inf) gives
- * token -1 and logprob -inf.
+ * with m = max l_i the weight of token i is the whole number
+ *   w_i = round(2^44 exp((l_i - m) / temperature[b])).
+ * In the order of falling logits, ties by index, kept are: the first top_k[b] tokens (all if <= 0); of
+ * these the fewest first ones that hold floor(W P / 2^24) of their weight W, P = round(2^24 top_p[b])
+ * (at least one; all if top_p >= 1); of these those with w_i >= round(2^44 min(min_p[b], 1)). The token
+ * is the lowest index i at which the kept weight of tokens 0 .. i exceeds floor(W' U / 2^24), W' the kept
+ * weight, U = floor(2^24 u[b]) clipped to [0, 2^24). Every sum is of whole numbers, so the token is
+ * exact. temperature <= 0 (or NaN) takes the lowest index of the largest logit (logprob 0). A row
+ * without any weight (all -inf) gives token -1 and logprob -inf.
  * temperature, top_k, top_p and min_p: device arrays [rows] or NULL (1, all, all, all). u: float
  * [rows]. tokens: int32 [rows]; logprobs: float [rows] or NULL, log(w_token / W').
  * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, vocab = 0 or above 2^18), ZO_ERR_HIP.

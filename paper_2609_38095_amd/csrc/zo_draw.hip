@@ -122,14 +122,35 @@ __device__ __forceinline__ void unpack_eight(const Eight<S>& x, float (&l)[8]) {
   for (int e = 0; e < 8; ++e) l[e] = sound<S>(l[e]);
 }
 
-// The 8 logits of a row from index i on (-inf behind the end).
+// The eight of a row from index i on, -inf behind the end.
+template <class S>
+__device__ __forceinline__ Eight<S> some_eight(const typename S::storage* row, uint32_t i, uint32_t vocab) {
+  if (i + 8 <= vocab) return load_eight<S>(row + i);
+  typename S::storage tmp[8];
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    S::store1(&tmp[e], -INFINITY);
+    if (i + e < vocab) tmp[e] = row[i + e];
+  }
+  Eight<S> x;
+  __builtin_memcpy(&x, tmp, sizeof x);
+  return x;
+}
+
 template <class S>
 __device__ __forceinline__ void load8(const typename S::storage* row, uint32_t i, uint32_t vocab, float (&l)[8]) {
-  if (i + 8 <= vocab) {
-    unpack_eight<S>(load_eight<S>(row + i), l);
+  unpack_eight<S>(some_eight<S>(row, i, vocab), l);
+}
+
+// What a walk hands on of an eight: its logits, or (f takes an Eight) the eight as it is stored.
+template <class S, class F>
+__device__ __forceinline__ void hand(F& f, uint32_t i, const Eight<S>& x) {
+  if constexpr (std::is_invocable<F&, uint32_t, const Eight<S>&>::value) {
+    f(i, x);
   } else {
-#pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) l[e] = i + e < vocab ? sound<S>(S::load1(row + i + e)) : -INFINITY;
+    float l[8];
+    unpack_eight<S>(x, l);
+    f(i, l);
   }
 }
 
@@ -143,11 +164,7 @@ __device__ __forceinline__ uint32_t walk_batches(const typename S::storage* row,
 #pragma unroll
     for (uint32_t u = 0; u < kBatch; ++u) x[u] = load_eight<S>(row + run0 + u * kStep + lane0);
 #pragma unroll
-    for (uint32_t u = 0; u < kBatch; ++u) {
-      float l[8];
-      unpack_eight<S>(x[u], l);
-      f(run0 + u * kStep + lane0, l);
-    }
+    for (uint32_t u = 0; u < kBatch; ++u) hand<S>(f, run0 + u * kStep + lane0, x[u]);
   }
   return run0;
 }
@@ -162,10 +179,8 @@ __device__ __forceinline__ void walk(const typename S::storage* row, uint32_t vo
   if constexpr (kBatch > 2) run0 = walk_batches<S, 2>(row, vocab, run0, f);
 #pragma unroll 1
   for (; run0 < vocab; run0 += kWaves * kRun) {
-    float l[8];
     const uint32_t i = run0 + threadIdx.x % 64 * 8;
-    load8<S>(row, i, vocab, l);
-    f(i, l);
+    hand<S>(f, i, some_eight<S>(row, i, vocab));
   }
 }
 
@@ -209,7 +224,7 @@ struct Lds {
     float kept[4 * kThreads];  // a few logits for each thread
     struct {                   // bf16 by value
       uint64_t bin_weight[kBins];
-      uint32_t bin_count[kBins];
+      uint32_t bin_count[kBins + 1];
     };
     struct {
       uint64_t list[kList];         // ~key << 32 | index: in rising order, tokens in falling order
@@ -479,6 +494,20 @@ __device__ __forceinline__ float value_of(int code) {  // not 0
   return __uint_as_float((code < 0 ? 0x8000u | a : a) << 16);
 }
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+
+// code_top - code of two stored bf16, modulo 2^16, at most `bins`: what is larger than the largest (a NaN) or weighs
+// nothing gets `bins` too, since codes span less than 2^16.
+__device__ __forceinline__ u16x2 bins_of(uint32_t pair, int code_top, uint32_t bins) {
+  const u16x2 a = __builtin_bit_cast(u16x2, pair & 0x7FFF7FFFu);
+  const u16x2 up = __builtin_elementwise_max(a, u16x2(static_cast<unsigned short>(kSmall))) - u16x2(static_cast<unsigned short>(kSmall));
+  const i16x2 sign = __builtin_bit_cast(i16x2, pair) >> 15;
+  const i16x2 code = (__builtin_bit_cast(i16x2, up) ^ sign) - sign;
+  const u16x2 bin = __builtin_bit_cast(u16x2, i16x2(static_cast<short>(code_top)) - code);
+  return __builtin_elementwise_min(bin, u16x2(static_cast<unsigned short>(bins)));
+}
+
 // Adds the weights of the tokens in `small` (few of a row).
 __device__ __forceinline__ void add_small(Lds& s, const float (&l)[8], uint32_t small, const Weigh& weigh) {
 #pragma unroll
@@ -492,20 +521,24 @@ __device__ __forceinline__ void add_small(Lds& s, const float (&l)[8], uint32_t 
 __device__ bool cut_by_value(Lds& s, const uint16_t* row, uint32_t vocab, const Weigh& weigh, int code_top, uint32_t bins,
                              uint32_t k, bool by_weight, uint32_t parts, Cut& cut) {
   const bool cuts = k > 0 || by_weight;
-  for (uint32_t i = threadIdx.x; i < bins; i += kThreads) s.bin_count[i] = 0;
+  for (uint32_t i = threadIdx.x; i <= bins; i += kThreads) s.bin_count[i] = 0;
   if (threadIdx.x == 0) s.small_weight = 0;
   __syncthreads();
   if (cuts) {
-    walk<BF16, 4>(row, vocab, [&](uint32_t, const float(&l)[8]) {
+    walk<BF16, 4>(row, vocab, [&](uint32_t, const Eight<BF16>& x) {
       uint32_t small = 0;
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        const int code = code_of(l[e]);
-        const uint32_t bin = static_cast<uint32_t>(code_top - code);
-        if (bin < bins) atomicAdd(&s.bin_count[bin], 1u);
-        small |= code == 0 ? 1u << e : 0u;
+      for (uint32_t c = 0; c < 4; ++c) {
+        const u16x2 bin = bins_of(x.v[0][c], code_top, bins);
+        atomicAdd(&s.bin_count[bin.x], 1u);  // (`bins` is a bin of what does not count)
+        atomicAdd(&s.bin_count[bin.y], 1u);
+        small |= (bin.x == code_top ? 1u << 2 * c : 0u) | (bin.y == code_top ? 2u << 2 * c : 0u);
       }
-      if (small) add_small(s, l, small, weigh);
+      if (small) {
+        float l[8];
+        unpack_eight<BF16>(x, l);
+        add_small(s, l, small, weigh);
+      }
     });
   }
   __syncthreads();
@@ -684,7 +717,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     const int code_low = code_of(static_cast<float>(weigh.max - 32.0 * static_cast<double>(temperature)));
     bins = static_cast<uint32_t>(code_top - code_low) + 1;
     __syncthreads();  // the list is read
-    if (bins <= kBins) {
+    if (bins <= kBins && top < 0xFF7F0000u) {  // (the largest bf16 may stand for +inf)
       binned = cut_by_value(s, row, vocab, weigh, code_top, bins, by_count ? static_cast<uint32_t>(k) : 0u, by_weight, parts, cut);
       if (!binned) cut = Cut{0, vocab, 0};
     }
@@ -756,22 +789,27 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   // the kept weight of each run of 512 tokens
   const uint32_t runs = (vocab + kRun - 1) / kRun;
   if (binned) {
-    const uint32_t cut_bin = cut.key == 0 ? bins : static_cast<uint32_t>(code_top - code_of(logit_of(cut.key)));
-    walk<S, 4>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
+    // (without a cut all bins are kept, whatever the index)
+    const uint32_t cut_bin = cut.key == 0 ? bins - 1 : static_cast<uint32_t>(code_top - code_of(logit_of(cut.key)));
+    if constexpr (sizeof(T) == 2) walk<S, 4>(row, vocab, [&](uint32_t i0, const Eight<S>& x) {
       uint64_t sum = 0;
       uint32_t small = 0;
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {  // (the bin of small values weighs nothing here)
-        const int code = code_of(l[e]);
-        const uint32_t bin = static_cast<uint32_t>(code_top - code);
-        const bool in = bin < bins && (bin < cut_bin || (bin == cut_bin && i0 + e <= cut.last));
-        if (in) {
-          const uint64_t w = s.bin_weight[bin];
-          sum += w >= least ? w : 0;
-          small |= code == 0 ? 1u << e : 0u;
+      for (uint32_t c = 0; c < 4; ++c) {
+        const u16x2 two = bins_of(x.v[0][c], code_top, bins);
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {
+          const uint32_t bin = h ? two.y : two.x;
+          if (bin < cut_bin || (bin == cut_bin && i0 + 2 * c + h <= cut.last)) {
+            const uint64_t w = s.bin_weight[bin];  // (the bin of small values weighs nothing here)
+            sum += w >= least ? w : 0;
+            small |= static_cast<int>(bin) == code_top ? 1u << (2 * c + h) : 0u;
+          }
         }
       }
       if (small) {
+        float l[8];
+        unpack_eight<S>(x, l);
 #pragma unroll
         for (uint32_t e = 0; e < 8; ++e) {
           const uint64_t w = small >> e & 1 ? weigh(l[e]) : 0;
