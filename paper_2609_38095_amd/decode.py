@@ -1,7 +1,8 @@
 """Python binding of libzo's decode-step operators (include/zo_decode.h): from trained weights to
 answers.
 
-Argument marshalling only, as in the package itself, under the C names:
+Argument marshalling only, as in the package itself (in _tensors.so for the calls that take tensors), under
+the C names:
 
   zo_rotary_turns(rotary, base, kind, factor, ...)      rotation frequencies (host, float64)
   zo_norm_rotate(q, k, positions, turns, ...)           head norms and rotation, one pass
@@ -19,14 +20,14 @@ stream of its own allocates on that stream, and waiting for tensors that other s
 is the caller's.
 """
 
-import array
+import contextlib
 import ctypes
-import struct
+import os
 
 import numpy as np
 import torch
 
-from . import ZO_BF16, ZO_F32, _check, _lib as _base_lib, _stream
+from . import PKG_DIR, ZoLibraryMissing, _check, _lib as _base_lib, _stream
 
 ZO_ERR_MEMORY, ZO_ERR_FULL = -5, -6
 ZO_DIM_MAX = 256
@@ -36,20 +37,12 @@ EXPORTS = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_r
            "zo_norm_rotate_back_work", "zo_cache_attend", "zo_cache_attend_work", "zo_cache_copy", "zo_draw",
            "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork", "zo_pages_extend", "zo_pages_drop",
            "zo_pages_left", "zo_pages_length", "zo_pages_table", "zo_pages_compact")
+# entry points that _tensors.so calls, in the order that it takes their addresses in
+_CALLED = ("zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_norm_rotate_back_work", "zo_cache_attend",
+           "zo_cache_attend_work", "zo_cache_copy", "zo_draw")
 
-# the argument structs of zo_decode.h, packed by one call each (a ctypes structure takes longer to
-# fill than a small kernel to run)
-_ROTATE = struct.Struct("Qqq Qqq Qqq Qqq QQQQ IIIIII ff i4x".replace(" ", ""))
-_PUT = struct.Struct(_ROTATE.format + "Qqq QQqqqIIII QqII Q".replace(" ", ""))
-_BACK = struct.Struct(_ROTATE.format + "Qqq Qqq QQQQ".replace(" ", ""))
-_ATTEND = struct.Struct("Qqq Qqq QQqqqIIII QqII QQQQ If i4x".replace(" ", ""))
-_DRAW = struct.Struct("QqQQQQQQQIIi4x")
-_CACHE = struct.Struct("QQqqqIIII")
-_NO_ROWS = (0, 0, 0)
-_TYPES = {torch.float32: ZO_F32, torch.bfloat16: ZO_BF16}
-
-_TENSORS = {torch.Tensor, torch.nn.Parameter}
 _READY = None
+_TENSORS = None
 
 
 class ZoPageMove(ctypes.Structure):
@@ -81,99 +74,59 @@ def _lib():
     return _READY
 
 
+def _tensors():
+    global _TENSORS
+    if _TENSORS is None:
+        lib = _lib()
+        if not os.path.exists(os.path.join(PKG_DIR, "_tensors.so")):
+            raise ZoLibraryMissing(f"{os.path.join(PKG_DIR, '_tensors.so')} is not built; run __graft_entry__.build()")
+        from . import _tensors as module
+        module.bind(*[ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _CALLED])
+        _TENSORS = module
+    return _TENSORS
+
+
 def _on(stream):
     """Allocations of a call with a stream of its own belong to that stream."""
+    if stream is None:
+        return contextlib.nullcontext()
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)))
     return torch.cuda.stream(stream)
 
 
-def _new(like, shape, stream, dtype=None):
-    """A tensor on `like`'s device for a result or a workspace."""
+_INITIALIZED = False
+
+
+def _initialized():
+    global _INITIALIZED
+    _INITIALIZED = torch.cuda.is_initialized()
+    return _INITIALIZED
+
+
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
+def _call(f, stream, like, *args):
+    """f on the current device and stream, or on the stream given, which must belong to like's device."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-    with _on(stream):
-        return torch.empty(shape, dtype=dtype or like.dtype, device=like.device)
-
-
-def _launch_stream(like, stream):
-    """The hipStream_t to launch on, torch's current one by default; the tensors are on the current device."""
-    if stream is None:
-        index = like.get_device()
-        if index == torch._C._cuda_getDevice():
-            return torch._C._cuda_getCurrentRawStream(index)
-    return _stream(like, stream)
-
-
-# Each check is one expression over what a sound argument has; what it does not take is named by _refuse. (A
-# call on a few tokens takes less time on the GPU than ten tensors' checks one by one take here.)
-
-def _refuse(t, name, dtype, like, shape, what):
-    """Raises what is wrong with an argument."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.get_device() != like.get_device():
-        raise ValueError(f"{name} lives on {t.device}, the other tensors on {like.device}")
-    if t.shape != shape:
-        raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
-    raise ValueError(f"{name}: {what}")
-
-
-def _dtype(t, name, dims):
-    """The library's name of a tensor's type; the tensor that a call's others are compared with."""
-    dtype = _TYPES.get(getattr(t, "dtype", None))
-    if dtype is None:
-        raise TypeError(f"{name} must be a float32 or bfloat16 tensor")
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA (HIP) torch tensor")
-    if t.dim() != dims:
-        raise ValueError(f"{name} must have {dims} dimensions")
-    return dtype
-
-
-def _rows(t, name, like, shape):
-    """(address, token stride, head stride) of a tensor [tokens, heads, dim]."""
-    if type(t) in _TENSORS and t.dtype is like.dtype and t.shape == shape and t.get_device() == like.get_device():
-        a, b, c = t.stride()
-        if c == 1 or shape[2] == 1:
-            return t.data_ptr(), a, b
-    _refuse(t, name, like.dtype, like, shape, "the last dimension must be contiguous")
-
-
-def _vector(t, name, dtype, like, n):
-    """The address of a contiguous tensor of n elements; 0 for None."""
-    if t is None:
-        return 0
-    if type(t) in _TENSORS and t.dtype is dtype and t.shape == (n,) and t.get_device() == like.get_device() \
-            and (n < 2 or t.stride(0) == 1):
-        return t.data_ptr()
-    _refuse(t, name, dtype, like, (n,), "must be contiguous")
-
-
-def _cache(k, v, like):
-    """The fields of a cache [pages, heads, page_tokens, dim]."""
-    shape = getattr(k, "shape", None)
-    if shape is not None and len(shape) == 4:
-        strides = k.stride()
-        if type(v) in _TENSORS and k.dtype is like.dtype and v.dtype is like.dtype and v.shape == shape \
-                and v.stride() == strides and k.get_device() == like.get_device() == v.get_device() \
-                and (strides[3] == 1 or shape[3] == 1):
-            return (k.data_ptr(), v.data_ptr(), *strides[:3], *shape)
+        if _INITIALIZED or _initialized():
+            device = _device()
+            got = f(device, _raw_stream(device), *args)
+        else:  # then no argument is on a device, and f says so
+            got = f(-1, 0, *args)
     else:
-        raise ValueError("k_cache must be a tensor [pages, heads, page_tokens, dim]")
-    _refuse(k, "k_cache", like.dtype, like, shape, "") if k.dtype != like.dtype or k.get_device() != like.get_device() else \
-        _refuse(v, "v_cache", like.dtype, like, shape, "the strides of k_cache, the last dimension contiguous, are needed")
+        handle = _stream(like, stream).value or 0
+        with _on(stream):
+            got = f(_device(), handle, *args)
+    if type(got) is int:
+        _check(got, "zo_" + f.__name__)
+    return got
 
 
-def _table(table, like):
-    if type(table) in _TENSORS and table.dtype is torch.int32 and table.get_device() == like.get_device() and table.dim() == 2:
-        n, width = table.shape
-        a, b = table.stride()
-        if b == 1 or width < 2:
-            return table.data_ptr(), a, n, width
-    _refuse(table, "table", torch.int32, like, getattr(table, "shape", ()), "must be [sequences, pages], its rows contiguous")
+def _doubles(turns):
+    """Frequencies as an array of float64; None for none."""
+    return turns if turns is None or type(turns) is np.ndarray and turns.dtype == np.float64 else np.array(turns, np.float64)
 
 
 def zo_rotary_turns(rotary, base=10000.0, kind=ZO_ROTARY_LINEAR, factor=1.0, original=0.0, low=1.0, high=4.0):
@@ -183,182 +136,54 @@ def zo_rotary_turns(rotary, base=10000.0, kind=ZO_ROTARY_LINEAR, factor=1.0, ori
     return out
 
 
-def _sides(q, k):
-    like = q if q is not None else k
-    if like is None:
-        raise ValueError("queries or keys are needed")
-    dtype = _dtype(like, "q and k", 3)
-    tokens, heads, dim = like.shape
-    if k is None:
-        return like, dtype, tokens, dim, heads, 0
-    if not isinstance(k, torch.Tensor) or k.dim() != 3:
-        raise TypeError("k must be a CUDA (HIP) torch tensor [tokens, heads, dim]")
-    return like, dtype, tokens, dim, 0 if q is None else heads, k.shape[1]
-
-
-def _turns(turns):
-    """(the frequencies as float64, their address, the rotated dims)."""
-    if turns is None:
-        return None, 0, 0
-    if not (isinstance(turns, np.ndarray) and turns.dtype == np.float64 and turns.ndim == 1 and turns.flags.c_contiguous):
-        turns = np.ascontiguousarray(np.asarray(turns, dtype=np.float64)).reshape(-1)
-    return turns, turns.__array_interface__["data"][0], 2 * len(turns)
-
-
 def zo_norm_rotate(q, k, positions, turns=None, interleaved=False, magnitude=1.0, q_gamma=None, k_gamma=None,
                    norm_eps=1e-6, q_out=None, k_out=None, stream=None):
     """(q_out, k_out): each head of q and k [tokens, heads, dim] normed (where it has a gamma) and its first
     2 len(turns) dims rotated by its token's position. q or k may be None. In place: q_out = q."""
-    like, dtype, tokens, dim, hq, hk = _sides(q, k)
-    if q is not None and q_out is None:
-        q_out = _new(like, (tokens, hq, dim), stream)
-    if k is not None and k_out is None:
-        k_out = _new(like, (tokens, hk, dim), stream)
-    qs = ks = qo = ko = _NO_ROWS
-    if q is not None:
-        qs, qo = _rows(q, "q", like, q.shape), _rows(q_out, "q_out", like, q.shape)
-    if k is not None:
-        shape = (tokens, hk, dim)
-        ks, ko = _rows(k, "k", like, shape), _rows(k_out, "k_out", like, shape)
-    turns, at, rotary = _turns(turns)
-    args = _ROTATE.pack(*qs, *ks, *qo, *ko, _vector(q_gamma, "q_gamma", like.dtype, like, dim),
-                        _vector(k_gamma, "k_gamma", like.dtype, like, dim),
-                        _vector(positions, "positions", torch.int32, like, tokens), at, tokens, hq, hk, dim, rotary,
-                        interleaved, norm_eps, magnitude, dtype)
-    _check(_lib().zo_norm_rotate(args, _launch_stream(like, stream)), "zo_norm_rotate")
-    return q_out, k_out
+    return _call((_TENSORS or _tensors()).norm_rotate, stream, q if q is not None else k, q, k, positions, _doubles(turns),
+                 interleaved, magnitude, q_gamma, k_gamma, norm_eps, q_out, k_out)
 
 
 def zo_norm_rotate_put(q, k, v, k_cache, v_cache, table, positions, turns=None, interleaved=False, magnitude=1.0,
                        q_gamma=None, k_gamma=None, norm_eps=1e-6, seqs=None, q_out=None, stream=None):
     """zo_norm_rotate whose keys, with the values v, are put at token positions[t] of sequence seqs[t] (t itself
     where seqs is None) of the paged cache. Returns q_out. q may be None."""
-    like, dtype, tokens, dim, hq, hk = _sides(q, k)
-    qs = qo = _NO_ROWS
-    if q is not None:
-        qs = _rows(q, "q", like, q.shape)
-        if q_out is None:
-            q_out = _new(like, (tokens, hq, dim), stream)
-        qo = _rows(q_out, "q_out", like, q.shape)
-    shape = (tokens, hk, dim)
-    turns, at, rotary = _turns(turns)
-    args = _PUT.pack(*qs, *_rows(k, "k", like, shape), *qo, *_NO_ROWS, _vector(q_gamma, "q_gamma", like.dtype, like, dim),
-                     _vector(k_gamma, "k_gamma", like.dtype, like, dim),
-                     _vector(positions, "positions", torch.int32, like, tokens), at, tokens, hq, hk, dim, rotary,
-                     interleaved, norm_eps, magnitude, dtype, *_rows(v, "v", like, shape), *_cache(k_cache, v_cache, like),
-                     *_table(table, like), _vector(seqs, "seqs", torch.int32, like, tokens))
-    _check(_lib().zo_norm_rotate_put(args, _launch_stream(like, stream)), "zo_norm_rotate_put")
-    return q_out
+    return _call((_TENSORS or _tensors()).norm_rotate_put, stream, k, q, k, v, k_cache, v_cache, table, positions, _doubles(turns),
+                 interleaved, magnitude, q_gamma, k_gamma, norm_eps, seqs, q_out)
 
 
 def zo_norm_rotate_back(dq_out, dk_out, q, k, positions, turns=None, interleaved=False, magnitude=1.0, q_gamma=None,
                         k_gamma=None, norm_eps=1e-6, dq=None, dk=None, work=None, stream=None):
     """(dq, dk, dq_gamma, dk_gamma) of zo_norm_rotate(q, k, ...) for the gradients of its outputs; the gammas'
     are float32 (None without the gamma). q and k are read only where there is a gamma."""
-    like, dtype, tokens, dim, hq, hk = _sides(dq_out, dk_out)
-    lib = _lib()
-    if dq_out is not None and dq is None:
-        dq = _new(like, (tokens, hq, dim), stream)
-    if dk_out is not None and dk is None:
-        dk = _new(like, (tokens, hk, dim), stream)
-    dq_gamma = _new(like, (dim,), stream, torch.float32) if q_gamma is not None and hq else None
-    dk_gamma = _new(like, (dim,), stream, torch.float32) if k_gamma is not None and hk else None
-    if work is None and (dq_gamma is not None or dk_gamma is not None):
-        work = _new(like, (max(lib.zo_norm_rotate_back_work(tokens, hq, hk, dim), 16),), stream, torch.uint8)
-    sq, sk = (tokens, hq, dim), (tokens, hk, dim)
-    rows = lambda t, name, shape, on: _rows(t, name, like, shape) if on else _NO_ROWS  # noqa: E731
-    turns, at, rotary = _turns(turns)
-    args = _BACK.pack(*rows(q, "q", sq, dq_gamma is not None), *rows(k, "k", sk, dk_gamma is not None),
-                      *rows(dq_out, "dq_out", sq, hq), *rows(dk_out, "dk_out", sk, hk),
-                      _vector(q_gamma, "q_gamma", like.dtype, like, dim), _vector(k_gamma, "k_gamma", like.dtype, like, dim),
-                      _vector(positions, "positions", torch.int32, like, tokens), at, tokens, hq, hk, dim, rotary,
-                      interleaved, norm_eps, magnitude, dtype, *rows(dq, "dq", sq, hq), *rows(dk, "dk", sk, hk),
-                      0 if dq_gamma is None else dq_gamma.data_ptr(), 0 if dk_gamma is None else dk_gamma.data_ptr(),
-                      *_work(work, like))
-    _check(lib.zo_norm_rotate_back(args, _launch_stream(like, stream)), "zo_norm_rotate_back")
-    return dq, dk, dq_gamma, dk_gamma
-
-
-def _work(work, like):
-    """(address, bytes) of a workspace; (0, 0) for None."""
-    if work is None:
-        return 0, 0
-    if not isinstance(work, torch.Tensor) or not work.is_cuda or not work.is_contiguous() or work.get_device() != like.get_device():
-        raise TypeError("work must be a contiguous CUDA (HIP) tensor on the other tensors' device")
-    return work.data_ptr(), work.numel() * work.element_size()
+    return _call((_TENSORS or _tensors()).norm_rotate_back, stream, dq_out if dq_out is not None else dk_out, dq_out, dk_out, q, k,
+                 positions, _doubles(turns), interleaved, magnitude, q_gamma, k_gamma, norm_eps, dq, dk, work)
 
 
 def zo_cache_attend(q, k_cache, v_cache, table, lengths, scale=None, out=None, lse=False, work=None, stream=None):
     """out [sequences, heads, dim] of one new token of each sequence: attention of its queries q over the first
     lengths[s] tokens of its pages table[s]. scale: dim ** -0.5 by default. lse: also returns log sum exp
     of the scores, float32 [sequences, heads]. work: a tensor of zo_cache_attend_work() bytes (allocated if None)."""
-    dtype = _dtype(q, "q", 3)
-    seqs, heads, dim = shape = q.shape
-    qs = _rows(q, "q", q, shape)
-    cache = _cache(k_cache, v_cache, q)
-    if cache[8] != dim:
-        raise ValueError(f"the cache's heads hold {cache[8]} dims, the queries' {dim}")
-    ids = _table(table, q)
-    if ids[2] != seqs:
-        raise ValueError("the table has one row for each sequence")
-    lib = _lib()
-    if out is None:
-        out = _new(q, shape, stream)
-    sums = _new(q, (seqs, heads), stream, torch.float32) if lse else None
-    if work is None:
-        work = _new(q, (lib.zo_cache_attend_work(seqs, heads, cache[6], dim),), stream, torch.uint8)
-    args = _ATTEND.pack(*qs, *_rows(out, "out", q, shape), *cache, *ids,
-                        _vector(lengths, "lengths", torch.int32, q, seqs), 0 if sums is None else sums.data_ptr(),
-                        *_work(work, q), heads, dim ** -0.5 if scale is None else scale, dtype)
-    _check(lib.zo_cache_attend(args, _launch_stream(q, stream)), "zo_cache_attend")
-    return (out, sums) if lse else out
+    return _call((_TENSORS or _tensors()).cache_attend, stream, q, q, k_cache, v_cache, table, lengths, scale, out, lse, work)
+
+
+def _int32s(x):
+    return x if x is None or type(x) is np.ndarray and x.dtype == np.int32 else np.array(x, np.int32)
 
 
 def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):
     """In each layer's cache: tokens 0 .. rows[i] - 1 (all if None) of page src[i] to page dst[i]. src, dst and rows
     are host arrays; no dst is repeated or a src of the same call."""
-    k_caches, v_caches = list(k_caches), list(v_caches)
-    if len(k_caches) != len(v_caches):
-        raise ValueError("one v_cache for each k_cache")
-    if not k_caches:
-        return
-    like = k_caches[0]
-    dtype = _dtype(like, "k_cache", 4)
-    fields = _cache(like, v_caches[0], like)
-    kind, device, shape, strides = like.dtype, like.get_device(), like.shape, like.stride()
-    at = []
-    for t in k_caches + v_caches:
-        if not (type(t) in _TENSORS and t.dtype is kind and t.get_device() == device and t.shape == shape
-                and t.stride() == strides):
-            _refuse(t, "each cache", kind, like, shape, "must have the strides of the first")
-        at.append(t.data_ptr())
-    src = np.asarray(src, dtype=np.int32)
-    moves = np.empty((src.size, 3), np.int32)
-    moves[:, 0], moves[:, 1] = src, dst
-    moves[:, 2] = shape[2] if rows is None else rows
-    _check(_lib().zo_cache_copy(_CACHE.pack(*fields), array.array("Q", at).tobytes(), len(at), moves.ctypes.data, len(moves),
-                                dtype, _launch_stream(like, stream)), "zo_cache_copy")
+    k_caches = list(k_caches)
+    _call((_TENSORS or _tensors()).cache_copy, stream, k_caches[0] if k_caches else None, k_caches, list(v_caches), _int32s(src),
+          _int32s(dst), _int32s(rows))
 
 
 def zo_draw(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=False, tokens=None, stream=None):
     """int32 tokens [rows] drawn from logits [rows, vocab] with the random numbers u [rows] in [0, 1), each row with
     its temperature, top_k (int32), top_p and min_p (device tensors [rows] or None). logprobs: also returns
     the drawn tokens' log probabilities among what was kept, float32."""
-    dtype = _dtype(logits, "logits", 2)
-    rows, vocab = logits.shape
-    if vocab > 1 and logits.stride(1) != 1:
-        raise ValueError("rows of logits must be contiguous")
-    if tokens is None:
-        tokens = _new(logits, (rows,), stream, torch.int32)
-    probs = _new(logits, (rows,), stream, torch.float32) if logprobs else None
-    f32 = torch.float32
-    args = _DRAW.pack(logits.data_ptr(), logits.stride(0), _vector(u, "u", f32, logits, rows),
-                      _vector(temperature, "temperature", f32, logits, rows), _vector(top_k, "top_k", torch.int32, logits, rows),
-                      _vector(top_p, "top_p", f32, logits, rows), _vector(min_p, "min_p", f32, logits, rows),
-                      _vector(tokens, "tokens", torch.int32, logits, rows), 0 if probs is None else probs.data_ptr(),
-                      rows, vocab, dtype)
-    _check(_lib().zo_draw(args, _launch_stream(logits, stream)), "zo_draw")
-    return (tokens, probs) if logprobs else tokens
+    return _call((_TENSORS or _tensors()).draw, stream, logits, logits, u, temperature, top_k, top_p, min_p, logprobs, tokens)
 
 
 class ZoPages:

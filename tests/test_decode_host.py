@@ -6,6 +6,7 @@ import math
 import os
 import re
 import shutil
+import struct
 import subprocess
 
 import numpy as np
@@ -38,17 +39,17 @@ def test_header_declares_what_the_binding_names():
         assert b"unknown" not in lib.zo_strerror(status)
 
 
-def test_argument_structs_have_the_headers_sizes(tmp_path):
-    names = ("zo_rotate", "zo_rotate_put", "zo_rotate_back", "zo_attend", "zo_draw_args", "zo_cache", "zo_page_move")
-    src = tmp_path / "sizes.c"
-    src.write_text('#include <stdio.h>\n#include "zo_decode.h"\nint main(void) {\n'
-                   + "".join(f'  printf("%u ", (unsigned)sizeof({n}));\n' for n in names) + "  return 0;\n}\n")
-    exe = tmp_path / "sizes"
-    subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)],
-                   check=True)
-    sizes = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
-    assert sizes == [s.size for s in (decode._ROTATE, decode._PUT, decode._BACK, decode._ATTEND, decode._DRAW, decode._CACHE)] \
-        + [ctypes.sizeof(decode.ZoPageMove)]
+def test_binding_module_is_built_and_bound():
+    """The module that marshals tensors is in the tree, takes the entry points' addresses and refuses anything else."""
+    module = decode._tensors()
+    assert os.path.exists(os.path.join(ROOT, "paper_2609_38095_amd", "_tensors.so"))
+    for args in ((), (0,) * 8, (1, 2)):
+        with pytest.raises((TypeError, ValueError)):
+            module.bind(*args)
+    with pytest.raises(TypeError):
+        module.norm_rotate(0, 0)
+    with pytest.raises(TypeError):
+        module.cache_attend("x", 0, *[None] * 9)
 
 
 def test_host_code_under_asan_ubsan(tmp_path):
@@ -99,13 +100,14 @@ def test_null_and_invalid_structs_are_refused():
     lib = decode._lib()
     for name in ("zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_cache_attend", "zo_draw"):
         assert getattr(lib, name)(None, None) == zo.ZO_ERR_NULL
-    draw = lambda **kw: lib.zo_draw(decode._DRAW.pack(*{**dict(  # noqa: E731
+    packed = struct.Struct("QqQQQQQQQIIi4x")  # zo_draw_args
+    draw = lambda **kw: lib.zo_draw(packed.pack(*{**dict(  # noqa: E731
         logits=0x1000, stride=100, u=0x2000, t=0, k=0, p=0, m=0, tokens=0x3000, lp=0, rows=4, vocab=100, dtype=0), **kw}.values()), None)
     assert draw(vocab=0) == draw(vocab=(1 << 18) + 1) == draw(dtype=5) == draw(stride=-1) == draw(logits=0x1002) == zo.ZO_ERR_ARG
     assert draw(u=0x2001) == draw(t=0x2002) == draw(tokens=0x3001) == draw(lp=0x3002) == zo.ZO_ERR_ARG
     assert draw(logits=0) == draw(u=0) == draw(tokens=0) == zo.ZO_ERR_NULL
     assert draw(rows=0, logits=0, u=0, tokens=0) == zo.ZO_OK
-    cache = decode._CACHE.pack(0x1000, 0x9000, 64, 64, 8, 4, 1, 8, 8)
+    cache = struct.pack("QQqqqIIII", 0x1000, 0x9000, 64, 64, 8, 4, 1, 8, 8)
     moves = np.array([[0, 1, 8]], np.int32)
     two = np.array([0x1000, 0x9000], np.uint64).tobytes()
     at = moves.ctypes.data
