@@ -116,7 +116,8 @@ def _call(f, stream, like, *args):
         else:  # then no argument is on a device, and f says so
             got = f(-1, 0, *args)
     else:
-        handle = _stream(like, stream).value or 0
+        # f itself refuses what is on no device, as it does without a stream
+        handle = _stream(like if getattr(like, "is_cuda", False) else None, stream).value or 0
         with _on(stream):
             got = f(_device(), handle, *args)
     if type(got) is int:

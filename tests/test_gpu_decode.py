@@ -561,3 +561,94 @@ def test_streams_and_graphs():
         for a, b in zip(held, want):
             assert torch.equal(a, b)
         assert torch.equal(step()[1], want[1])
+
+
+def test_refusals():
+    """Wrong arguments raise and leave the outputs as they were."""
+    q, k, v = rows_of("own", 1, 4, 6, 2, 64, "bf16")
+    kc, vc = cache_of("heads", 2, 8, 2, 16, 64, "bf16")
+    at = torch.arange(4, dtype=torch.int32, device="cuda")
+    table = torch.arange(8, dtype=torch.int32, device="cuda").reshape(4, 2)
+    lengths = at + 1
+    out = torch.full_like(q, 7.0)
+    turns = zo.zo_rotary_turns(64)
+
+    def rejects(error, call, *args, **kw):
+        with pytest.raises(error):
+            call(*args, **kw)
+
+    rotate = zo.zo_norm_rotate
+    rejects(TypeError, rotate, q, k.float(), at)
+    rejects(TypeError, rotate, q, k, at.long())
+    rejects(TypeError, rotate, q, k, at, turns.astype(np.float32).reshape(2, -1))
+    rejects(TypeError, rotate, q, k.cpu(), at)
+    rejects(TypeError, rotate, q, k, at, q_gamma=torch.ones(64, device="cuda"))
+    rejects(ValueError, rotate, q, k[:, :, :32], at)
+    rejects(ValueError, rotate, q, k[:3], at)
+    rejects(ValueError, rotate, q, k, at[:3])
+    rejects(ValueError, rotate, q.transpose(1, 2), None, at)
+    rejects(ValueError, rotate, q, k, at, q_out=out[:3])
+    rejects(ValueError, rotate, None, None, at)
+    for bad, code in ((dict(turns=zo.zo_rotary_turns(66)), zo.ZO_ERR_ARG), (dict(norm_eps=float("nan")), zo.ZO_ERR_NONFINITE),
+                      (dict(q_out=out.expand(4, 6, 64)[:1].expand(4, 6, 64)), zo.ZO_ERR_ARG),  # rows that overlap
+                      (dict(q_out=q[:, :, :].flip(1).flip(1).as_strided((4, 6, 64), (384, 64, 1)), turns=turns * np.inf), zo.ZO_ERR_NONFINITE)):
+        with pytest.raises(zo.ZoError) as e:
+            rotate(q, k, at, **bad)
+        assert e.value.status == code
+    shifted = torch.zeros(4 * 6 * 64 + 1, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(zo.ZoError):  # an output that begins an element behind its input
+        rotate(shifted[:-1].view(4, 6, 64), None, at, q_out=shifted[1:].view(4, 6, 64))
+    attend = zo.zo_cache_attend
+    rejects(TypeError, attend, q.float(), kc, vc, table, lengths)
+    rejects(TypeError, attend, q, kc, vc, table.long(), lengths)
+    rejects(ValueError, attend, q, kc, vc[:4], table, lengths)
+    rejects(ValueError, attend, q, kc, vc, table[:2], lengths)
+    rejects(ValueError, attend, q, kc, vc, table, lengths[:2])
+    rejects(ValueError, attend, q[:, :, :32], kc, vc, table, lengths)
+    rejects(zo.ZoError, attend, q[:, :3], kc, vc, table, lengths)  # 3 query heads for 2 key heads
+    rejects(zo.ZoError, attend, q, kc, vc, table, lengths, float("inf"), out=out)
+    rejects(zo.ZoError, attend, q, kc, vc, table, lengths, out=out, work=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    rejects(zo.ZoError, attend, q, kc, vc, table, lengths, out=q)
+    rejects(ValueError, zo.zo_norm_rotate_put, q, k, v, kc, vc.transpose(0, 1), table, at)
+    rejects(zo.ZoError, zo.zo_norm_rotate_put, q, k[:, :1], v[:, :1], kc, vc, table, at)  # another count of heads
+    back = zo.zo_norm_rotate_back
+    gamma = torch.ones(64, dtype=torch.bfloat16, device="cuda")
+    rejects(TypeError, back, out, None, None, None, at, q_gamma=gamma)  # the input is needed with a gamma
+    rejects(zo.ZoError, back, out, None, q, None, at, q_gamma=gamma, work=torch.empty(16, dtype=torch.uint8, device="cuda"))
+    rejects(zo.ZoError, zo.zo_cache_copy, [kc], [vc], [0, 1], [1, 2])
+    rejects(zo.ZoError, zo.zo_cache_copy, [kc], [vc], [0], [8])
+    rejects(ValueError, zo.zo_cache_copy, [kc], [vc], [0, 1], [2])
+    rejects(ValueError, zo.zo_cache_copy, [kc, kc[:4]], [vc, vc[:4]], [0], [1])
+    logits, u = normal(1, (4, 100), "f32"), torch.rand(4, device="cuda")
+    rejects(TypeError, zo.zo_draw, logits, u.double())
+    rejects(TypeError, zo.zo_draw, logits, u, top_k=torch.ones(4, device="cuda"))
+    rejects(ValueError, zo.zo_draw, logits, u[:3])
+    rejects(ValueError, zo.zo_draw, logits.T, u)
+    rejects(zo.ZoError, zo.zo_draw, logits[:, :0], u)
+    if torch.cuda.device_count() == 1:
+        stream = torch.cuda.Stream()
+        rejects(TypeError, zo.zo_draw, logits.cpu(), u, stream=stream)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
+
+
+def test_work_and_outputs_given():
+    """Results in given tensors, with given workspaces, are those of the allocated ones."""
+    q, k, _ = rows_of("fused", 5, 9, 4, 2, 64, "f32")
+    kc, vc = cache_of("tokens", 6, 40, 2, 16, 64, "f32")
+    table = torch.arange(36, dtype=torch.int32, device="cuda").reshape(9, 4)
+    lengths = torch.tensor([64, 1, 0, 17, 33, 2, 50, 63, 5], dtype=torch.int32, device="cuda")
+    want, lse = zo.zo_cache_attend(q, kc, vc, table, lengths, lse=True)
+    from paper_2609_38095_amd import decode
+    work = torch.full((decode._lib().zo_cache_attend_work(9, 4, 2, 64),), 255, dtype=torch.uint8, device="cuda")  # NaN everywhere
+    out = torch.zeros(9, 64, 4, device="cuda").transpose(1, 2).contiguous()
+    wide_out = torch.zeros(9, 4, 80, device="cuda")
+    for o in (out, wide_out[:, :, 3:67]):
+        got = zo.zo_cache_attend(q, kc, vc, table, lengths, out=o, work=work)
+        assert got.data_ptr() == o.data_ptr() and torch.equal(o, want)
+    assert not wide_out[:, :, :3].any() and not wide_out[:, :, 67:].any()
+    tokens = torch.full((3,), -5, dtype=torch.int32, device="cuda")
+    logits, u = normal(1, (3, 100), "bf16"), torch.rand(3, device="cuda")
+    assert zo.zo_draw(logits, u, tokens=tokens) is not None and torch.equal(tokens, zo.zo_draw(logits, u))
+    assert zo.zo_draw(logits[:0], u[:0]).shape == (0,)
+    assert zo.zo_cache_attend(q[:0], kc, vc, table[:0], lengths[:0]).shape == (0, 4, 64)
