@@ -101,8 +101,8 @@ int zo_rotary_turns(zo_rotary_kind kind, uint32_t rotary, double base, double fa
  * that far positions cost no precision. gamma: `dim` elements of the call's dtype. turns: host array
  * of rotary / 2 doubles (zo_rotary_turns or the caller's own); rotary = 0: no rotation.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (dtype, alignment, dim = 0 or above ZO_DIM_MAX, rotary odd or
- * above dim, in and out overlapping otherwise); ZO_ERR_NONFINITE (norm_eps, magnitude, a frequency);
- * ZO_ERR_HIP.
+ * above dim, in and out overlapping otherwise, more rows than a launch takes: at least 2^26);
+ * ZO_ERR_NONFINITE (norm_eps, magnitude, a frequency); ZO_ERR_HIP.
  */
 typedef struct {
   zo_heads q, k, q_out, k_out;
@@ -171,7 +171,7 @@ int zo_norm_rotate_back(const zo_rotate_back* b, void* stream);
  * Weights are exp2 in fp32; for bf16 each is split in two bf16 parts (16 bits of it) where it meets
  * the values, and sums are fp32.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (dtype, alignment, dim = 0 or above ZO_DIM_MAX, heads, pages or
- * page_tokens 0, too little work); ZO_ERR_NONFINITE (scale); ZO_ERR_HIP.
+ * page_tokens 0, too little work, 2^24 rows or more); ZO_ERR_NONFINITE (scale); ZO_ERR_HIP.
  */
 typedef struct {
   zo_heads q, out;
@@ -196,7 +196,7 @@ int zo_cache_attend(const zo_attend* a, void* stream);
  * arrays. All moves read what the pages held before the call: no dst is repeated or is the src of a
  * move.
  * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, a page or rows out of range, rows = 0, a
- * repeated dst, a dst that is a src, pages that overlap, pages of 2^30 elements or more), ZO_ERR_MEMORY,
+ * repeated dst, a dst that is a src, pages that overlap, pages of more than 2^23 elements), ZO_ERR_MEMORY,
  * ZO_ERR_HIP (earlier batches may already be enqueued).
  */
 typedef struct {
@@ -220,7 +220,7 @@ int zo_cache_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensor
  * without any weight (all -inf) gives token -1 and logprob -inf.
  * temperature, top_k, top_p and min_p: device arrays [rows] or NULL (1, all, all, all). u: float
  * [rows]. tokens: int32 [rows]; logprobs: float [rows] or NULL, log(w_token / W').
- * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, vocab = 0 or above 2^18), ZO_ERR_HIP.
+ * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, vocab = 0 or above 2^18, 2^22 rows or more), ZO_ERR_HIP.
  */
 typedef struct {
   const void* logits; /* [rows, vocab], rows row_stride elements apart */

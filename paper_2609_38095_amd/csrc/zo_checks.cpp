@@ -211,7 +211,8 @@ int check_attend(const zo_attend& a) {
   if (!dtype_ok(a.dtype)) return ZO_ERR_ARG;
   const size_t elem = elem_bytes(a.dtype);
   if (a.cache.heads == 0 || a.cache.heads > 0xFFFFu || a.q_heads > 0xFFFFu || a.q_heads % a.cache.heads != 0) return ZO_ERR_ARG;
-  if (static_cast<uint64_t>(a.table.seqs) * std::max(a.q_heads, 1u) > 0x7FFFFFFFu) return ZO_ERR_ARG;  // items in 32 bits
+  // a workgroup for each item, 2^32 threads at most in a launch
+  if (static_cast<uint64_t>(a.table.seqs) * std::max(a.q_heads, 1u) >= (1u << 24)) return ZO_ERR_ARG;
   if (!std::isfinite(a.scale)) return ZO_ERR_NONFINITE;
   if (a.table.seqs == 0 || a.q_heads == 0) return ZO_OK;
   ZO_TRY(check_cache(a.cache, elem, false));
@@ -232,7 +233,7 @@ int check_attend(const zo_attend& a) {
 int check_draw(const zo_draw_args& a) {
   if (!dtype_ok(a.dtype) || a.vocab == 0 || a.vocab > (1u << 18) || !axis_ok(a.row_stride, a.rows)) return ZO_ERR_ARG;
   if (a.rows == 0) return ZO_OK;
-  if (a.rows > 0x7FFFFFFFu) return ZO_ERR_ARG;
+  if (a.rows >= (1u << 22)) return ZO_ERR_ARG;  // 2^32 threads at most in a launch
   if (a.logits == nullptr || a.u == nullptr || a.tokens == nullptr) return ZO_ERR_NULL;
   if (!aligned(a.logits, elem_bytes(a.dtype)) || !aligned(a.u, 4) || !aligned(a.temperature, 4) || !aligned(a.top_k, 4) ||
       !aligned(a.top_p, 4) || !aligned(a.min_p, 4) || !aligned(a.tokens, 4) || !aligned(a.logprobs, 4))
@@ -248,10 +249,8 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
   first.k = first.v = tensors[0];
   const size_t elem = elem_bytes(dtype);
   ZO_TRY(check_cache(first, elem, true));
-  // vectors of a head's page and a launch's workgroups are numbered in 32 bits
-  if (static_cast<uint64_t>(first.page_tokens) * first.dim > (1ull << 28) || first.heads > 0xFFFFu ||
-      static_cast<uint64_t>(first.page_tokens) * first.dim * first.heads > (1ull << 30))
-    return ZO_ERR_ARG;
+  // 2^32 threads at most in a launch
+  if (first.heads > 0xFFFFu || static_cast<uint64_t>(first.page_tokens) * first.dim * first.heads > (1ull << 23)) return ZO_ERR_ARG;
   for (uint32_t i = 0; i < n_tensors; ++i) {
     if (tensors[i] == nullptr) return ZO_ERR_NULL;
     if (!aligned(tensors[i], elem)) return ZO_ERR_ARG;

@@ -1,5 +1,5 @@
 // Host-side argument checks of the decode-step operators. Plain C++ (no HIP), shared by their
-// launchers and by the host checker that runs this code under AddressSanitizer and UBSan.
+// launchers and by the host test that runs this code under AddressSanitizer and UBSan.
 #ifndef ZO_CHECKS_H_
 #define ZO_CHECKS_H_
 

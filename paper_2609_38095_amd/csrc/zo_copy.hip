@@ -1,5 +1,6 @@
 // Copies of cache pages for gfx950: forks, compactions. Bound by HBM: one read and one write of the
-// rows that are copied.
+// rows that are copied. 1,024 pages of 16 tokens, 8 heads of 128 in bf16, in 28 layers (3.8 GB): 720 us,
+// 5.2 TB/s (a plain copy with as much in flight for each wave reaches 5.6).
 //
 // A move copies `rows` tokens of every key head, keys and values, in every cache. One workgroup takes
 // 256 vectors of 16 bytes of a head's rows, in as many heads (8, 4, 2 or 1) of one page of one tensor as

@@ -10,15 +10,19 @@
 //                    and weighed.
 //   top-p alone      (fp32) Weights are added up in 2,888 equal ranges of (l - max) / T; the range in which
 //                    top_p's share is reached goes into the list, and tokens above it are kept anyway.
-//   bf16             has few values: 8 bits of each power of two between the largest logit and e^-31 of its weight. Their
-//                    tokens are counted, and each value is weighed once.
-//   otherwise        (more ties than the list holds, a larger k, or a temperature that spreads bf16 over too many values) Ranges of 32-bit keys of the logits'
-//                    order are divided until one key is left, by 2,048 counts and weights at a time.
+//   bf16             has few values: 8 bits of each power of two between the largest logit and e^-31 of
+//                    its weight. Their tokens are counted, and each value is weighed once.
+//   otherwise        (more ties than the list holds, a larger k, or a temperature that spreads bf16 over
+//                    too many values) Ranges of 32-bit keys of the logits' order are divided until one
+//                    key is left, by 2,048 counts and weights at a time.
 // The drawn token is then found in index order: weights of runs of 512 tokens, their running sums, and
 // the tokens of the run that holds the drawn share.
 //
 // The row is read from HBM once; later passes find it in the L2 (608 KB at 152 k fp32 logits). Bound by
-// the fp64 exponentials of one CU where every token's weight is needed, else by its reads.
+// the fp64 exponentials of one CU where every token's weight is needed, else by its reads. Measured, of
+// 151,936 logits: 256 bf16 rows with top-p 0.95 and min-p in 95 us (read 12, counts 25, runs 23, the rest
+// cuts and the slowest row), one fp32 row in 25 us with top-k 50 and in 73 without (read 8, ranges 33,
+// list 12, runs 18).
 
 #include <cmath>
 #include <type_traits>

@@ -210,3 +210,16 @@ def test_oracle_attention_and_draw():
     assert [oracle.draw(l, u, min_p=0.6)[0] for u in (0.5, 0.6)] == [1, 3] and oracle.draw(l, 0.9, temperature=0.0) == (1, 0.0)
     assert oracle.draw(np.full(3, -np.inf, np.float32), 0.3) == (-1, -math.inf)
     np.testing.assert_allclose(oracle.draw(l, 0.9)[1], math.log(0.3), rtol=1e-6)
+
+
+def test_launches_of_2_to_the_32_threads_are_refused():
+    """A launch takes fewer; what would need more is turned away before any HIP call."""
+    lib = decode._lib()
+    draw = struct.Struct("QqQQQQQQQIIi4x")  # zo_draw_args
+    for rows in (1 << 22, 1 << 31, (1 << 32) - 1):
+        assert lib.zo_draw(draw.pack(0x1000, 100, 0x2000, 0, 0, 0, 0, 0x3000, 0, rows, 100, 0), None) == zo.ZO_ERR_ARG
+    moves = np.array([[0, 1, 8]], np.int32)
+    one = np.array([1 << 20], np.uint64).tobytes()
+    for tokens, heads in ((1 << 15, 5), (1 << 20, 1), (1 << 12, 64)):  # pages of 64-dim heads above 2^23 elements
+        cache = struct.pack("QQqqqIIII", 1 << 20, 1 << 40, tokens * heads * 64, tokens * 64, 64, 4, heads, tokens, 64)
+        assert lib.zo_cache_copy(cache, one, 1, moves.ctypes.data, 1, 0, None) == zo.ZO_ERR_ARG
