@@ -237,6 +237,15 @@ typedef struct {
 int zo_draw(const zo_draw_args* a, void* stream);
 
 /*
+ * zo_draw_split -- zo_draw, its rows split over workgroups where they are few and long: the same
+ * tokens sooner. work: zo_draw_work() bytes (top_k: whether the call has any), aligned to 16, contents irrelevant,
+ * one for each call in flight; with 0 bytes (many or short rows) work is not used and the call is zo_draw.
+ * Errors: as zo_draw; ZO_ERR_ARG, ZO_ERR_NULL for the workspace.
+ */
+int zo_draw_split(const zo_draw_args* a, void* work, uint64_t work_bytes, void* stream);
+uint64_t zo_draw_work(uint32_t rows, uint32_t vocab, int top_k);
+
+/*
  * The page book -- host bookkeeping of a cache's pages: which pages each sequence holds, which are
  * shared, which are free. It holds no device memory and never touches the GPU; what has to be copied
  * on the device it hands out as moves for zo_cache_copy (of every layer, before the next put). A book

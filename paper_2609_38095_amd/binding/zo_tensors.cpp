@@ -30,7 +30,8 @@ struct Entry {
   decltype(&zo_cache_attend) cache_attend;
   decltype(&zo_cache_attend_work) cache_attend_work;
   decltype(&zo_cache_copy) cache_copy;
-  decltype(&zo_draw) draw;
+  decltype(&zo_draw_split) draw_split;
+  decltype(&zo_draw_work) draw_work;
 } entry = {};
 
 struct Refusal {  // a Python exception to raise
@@ -403,12 +404,12 @@ PyObject* cache_copy(PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* draw(PyObject* const* args, Py_ssize_t n) {
-  Args a(args, n, 10);
+  Args a(args, n, 11);
   const at::Tensor* logits = a.tensor("logits");
   const at::Tensor *u = a.tensor("u"), *temperature = a.tensor("temperature"), *top_k = a.tensor("top_k"), *top_p = a.tensor("top_p");
   const at::Tensor* min_p = a.tensor("min_p");
   const bool logprobs = a.flag();
-  const at::Tensor* given = a.tensor("tokens");
+  const at::Tensor *given = a.tensor("tokens"), *work = a.tensor("work");
   if (logits == nullptr || u == nullptr) refuse(PyExc_TypeError, "logits and u must be CUDA (HIP) torch tensors");
   zo_draw_args p = {};
   p.dtype = type_of(*logits, "logits");
@@ -431,7 +432,11 @@ PyObject* draw(PyObject* const* args, Py_ssize_t n) {
     probs = fresh(*logits, {count}, at::kFloat);
     p.logprobs = static_cast<float*>(probs.data_ptr());
   }
-  const int rc = entry.draw(&p, a.stream);
+  at::Tensor hold;
+  void* at = nullptr;
+  uint64_t bytes = 0;
+  if (const uint64_t needed = entry.draw_work(p.rows, p.vocab, p.top_k != nullptr)) work_of(work, *logits, needed, hold, at, bytes);
+  const int rc = entry.draw_split(&p, at, bytes, a.stream);
   if (rc != ZO_OK) return status(rc);
   return logprobs ? tuple_of({tokens, probs}) : THPVariable_Wrap(tokens);
 }

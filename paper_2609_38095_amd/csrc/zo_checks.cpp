@@ -241,6 +241,14 @@ int check_draw(const zo_draw_args& a) {
   return ZO_OK;
 }
 
+int check_draw_split(const zo_draw_args& a, const void* work, uint64_t work_bytes) {
+  ZO_TRY(check_draw(a));
+  const uint64_t bytes = zo_draw_work(a.rows, a.vocab, a.top_k != nullptr);
+  if (bytes == 0) return ZO_OK;
+  if (work == nullptr) return ZO_ERR_NULL;
+  return aligned(work, 16) && work_bytes >= bytes ? ZO_OK : ZO_ERR_ARG;
+}
+
 int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype) {
   if (!dtype_ok(dtype)) return ZO_ERR_ARG;
   if (n_tensors == 0 || n_moves == 0) return ZO_OK;
@@ -288,6 +296,18 @@ uint64_t zo_cache_attend_work(uint32_t seqs, uint32_t q_heads, uint32_t heads, u
   const uint64_t group = q_heads / heads < 16 ? q_heads / heads : 16;
   const uint64_t row = (dim + 3) / 4 * 4 + 4;
   return zo::attend_items_bytes(seqs, q_heads, heads) + 2ull * zo::attend_workers(dim) * group * row * sizeof(float);
+}
+
+// Rows are split where that is sooner. us for fp32 (bf16) rows, one workgroup each | split: with top-p alone 16,384
+// logits 27 (25) | 27, 32,000 38 (33) | 28, 151,936 108 (75) | 33 for 4 rows, 43 for 16 and 57 for 32; without settings
+// 14 (17) | 12 and 56 (48) | 13 for 4 rows, 21 for 32. A top-k that counts ends early in one workgroup: 16,384 logits
+// 17 | 24, 151,936 25 | 23 for 4 rows, 28 for 16 and 36 for 32. Rows whose top_k is 0 are as above and may lie in the
+// same batch, so one with a top_k is split from where its other rows lose no more than a few us.
+uint64_t zo_draw_work(uint32_t rows, uint32_t vocab, int top_k) {
+  const uint32_t most_rows = top_k ? 16 : 32, least_vocab = top_k ? 1u << 16 : 4 * zo::kDrawPart;
+  if (rows > most_rows || vocab < least_vocab || vocab > (1u << 18)) return 0;
+  const uint64_t parts = (vocab + zo::kDrawPart - 1) / zo::kDrawPart;
+  return rows * (parts * zo::kDrawPartWords + zo::kDrawRowWords) * 8;
 }
 
 int zo_rotary_turns(zo_rotary_kind kind, uint32_t rotary, double base, double factor, double original, double low,

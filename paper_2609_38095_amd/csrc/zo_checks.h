@@ -17,6 +17,7 @@ int check_put(const zo_rotate_put& p);
 int check_back(const zo_rotate_back& b);
 int check_attend(const zo_attend& a);
 int check_draw(const zo_draw_args& a);
+int check_draw_split(const zo_draw_args& a, const void* work, uint64_t work_bytes);
 int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype);
 
 // Whether two sets of rows may share an element. Exact for rows of one interleaved buffer (equal
@@ -30,6 +31,9 @@ constexpr uint32_t kBackBlocks = 512;
 uint32_t back_blocks(uint32_t tokens, uint32_t heads);
 uint64_t attend_items_bytes(uint32_t seqs, uint32_t q_heads, uint32_t heads);  // the parts' whereabouts
 uint32_t attend_workers(uint32_t dim);  // at most
+
+// zo_draw_split: tokens of a workgroup's part, and words of 8 bytes that a part and a row keep.
+constexpr uint32_t kDrawPart = 4096, kDrawPartWords = 4074, kDrawRowWords = 2;
 
 }  // namespace zo
 

@@ -1,4 +1,4 @@
-// The draw of a token from each row of logits, for gfx950: one workgroup for a row.
+// The draw of a token from each row of logits, for gfx950: one workgroup for a row, more for few long rows.
 //
 // Mathematics. Weights are whole numbers, w_i = round(2^44 exp((l_i - max) / T)), from fp64 exponentials;
 // their sums (below 2^62 for 2^18 tokens) are exact in any order, so the token is the same whatever the
@@ -21,8 +21,8 @@
 // The row is read from HBM once; later passes find it in the L2 (608 KB at 152 k fp32 logits). Bound by
 // the fp64 exponentials of one CU where every token's weight is needed, else by its reads. Measured, of
 // 151,936 logits: 256 bf16 rows with top-p 0.95 and min-p in 95 us (read 12, counts 25, runs 23, the rest
-// cuts and the slowest row), one fp32 row in 25 us with top-k 50 and in 73 without (read 8, ranges 33,
-// list 12, runs 18).
+// cuts and the slowest row), one fp32 row in 25 us with top-k 50 and in 108 with top-p 0.95 alone. Few
+// long rows are therefore split over workgroups where the caller gives a workspace: 33 us.
 
 #include <cmath>
 #include <type_traits>
@@ -69,9 +69,10 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
 // with r = f ln 2 / 1024 below 3.4e-4, where the third-degree Taylor polynomial is off by 6e-16; with the rounding of
 // x - r times its weight, the weight is off by less than 2^-49 where its last place is 2^-44. The whole number
 // n = 1024 q + j also gives the token's range, counted down from the largest logit.
+typedef const __attribute__((address_space(3))) double* LdsTable;  // said, not left to be found out: it is read for each token
 struct Weigh {
   double max, inv;  // 1 / temperature
-  const double* table;  // 2^(44 + j / 1024), LDS
+  LdsTable table;   // 2^(44 + j / 1024)
   // n: 0 .. -16 kRanges (of a weight that is not 0). Straight-line code, so that several tokens' chains of
   // operations overlap. Rounding to whole numbers is the addition of a power of two whose last place is 1,
   // and scaling by 2^q an addition to the exponent: fp64 operations take twice as long as others, its
@@ -314,19 +315,23 @@ __device__ __forceinline__ uint32_t index_of_tie(Lds& s, const typename S::stora
 }
 
 // Sorts the first n entries of the list (n <= kList, all different), smallest first. Up to 512 by counting for each
-// how many are smaller, with no barrier between; longer ones by a bitonic network.
+// how many are smaller, an entry's count shared by as many waves as there are; longer ones by a bitonic network.
 __device__ __forceinline__ void sort_list(Lds& s, uint32_t n) {
   if (n <= 512) {
+    const uint32_t size = n <= 64 ? 64 : (n + 63) / 64 * 64, copies = kThreads / size, copy = threadIdx.x / size;
+    const uint32_t i = threadIdx.x - copy * size;
+    if (threadIdx.x < n) s.thread_max[threadIdx.x] = 0;  // ranks
     __syncthreads();
-    uint64_t mine = 0;
-    uint32_t rank = 0;
-    if (threadIdx.x < n) {
-      mine = s.list[threadIdx.x];
+    const uint64_t mine = i < n ? s.list[i] : 0;
+    if (i < n && copy < copies) {
+      uint32_t rank = 0;
+      const uint32_t end = (copy + 1) * n / copies;
 #pragma unroll 8
-      for (uint32_t i = 0; i < n; ++i) rank += s.list[i] < mine ? 1 : 0;
+      for (uint32_t j = copy * n / copies; j < end; ++j) rank += s.list[j] < mine ? 1 : 0;
+      atomicAdd(&s.thread_max[i], rank);
     }
     __syncthreads();
-    if (threadIdx.x < n) s.list[rank] = mine;
+    if (threadIdx.x < n) s.list[s.thread_max[threadIdx.x]] = mine;
     __syncthreads();
     return;
   }
@@ -403,9 +408,12 @@ __device__ __forceinline__ uint32_t cut_list(Lds& s, uint32_t n, const Weigh& we
 
 // The cut at which the count reaches `most`, or (by_weight) the weight reaches `need`, whichever is
 // asked for; false: the row's weights end before. Tokens of no weight do not count.
-template <class S>
-__device__ __attribute__((noinline)) bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab, const Weigh& weigh, uint32_t top, bool by_weight,
-                         uint64_t need, Cut& cut) {
+// kSplit: the kernel that calls it. A function of its own for each lets the compiler see where its arguments come
+// from; shared by two kernels, `weigh` and `cut` are kept in memory and read from there for each token (fp32 rows without
+// settings: 77 -> 141 us).
+template <class S, bool kSplit>
+__device__ __attribute__((noinline)) bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab, const Weigh& weigh, uint32_t top,
+                                                   bool by_weight, uint64_t need, Cut& cut) {
   uint32_t hi = top, lo = 0;
   uint64_t above_weight = 0, above_count = 0;
   for (;;) {
@@ -522,6 +530,7 @@ __device__ __forceinline__ void add_small(Lds& s, const float (&l)[8], uint32_t 
 // A bf16 row by value: its weights come from one exponential for each value instead of each token, and top-k and
 // top-p from a count of each value's tokens. false: the values that weigh anything are more than the bins, or a cut falls
 // among those below 2^-10; nothing is done then.
+template <bool kSplit>
 __device__ bool cut_by_value(Lds& s, const uint16_t* row, uint32_t vocab, const Weigh& weigh, int code_top, uint32_t bins,
                              uint32_t k, bool by_weight, uint32_t parts, Cut& cut) {
   const bool cuts = k > 0 || by_weight;
@@ -620,13 +629,389 @@ __device__ __forceinline__ uint32_t last_untaken(F takes) {
   return key;
 }
 
+// The largest key whose weight does not reach range `edge`.
+__device__ __forceinline__ uint32_t range_edge(const Weigh& weigh, uint32_t top, int32_t edge) {
+  return last_untaken([&](uint32_t key) {
+    if (key <= key_of(-INFINITY)) return false;
+    if (key >= top) return edge >= 0 || key > top;
+    int n;
+    return weigh(logit_of(key), n) > 0 && -n / 16 <= edge;
+  });
+}
+
+// What a row is drawn with.
+__device__ __forceinline__ float temperature_of(const Draw& a, uint32_t b) { return a.temperature ? a.temperature[b] : 1.0f; }
+struct Asked {
+  int32_t k;
+  bool by_count, by_weight;
+  uint32_t parts, draw;  // of 2^24
+  uint64_t least;        // weight
+  __device__ __forceinline__ Asked(const Draw& a, uint32_t b) {
+    const float p = a.top_p ? a.top_p[b] : 1.0f, mp = a.min_p ? a.min_p[b] : 0.0f, u = a.u[b];
+    k = a.top_k ? a.top_k[b] : 0;
+    by_count = k > 0 && static_cast<uint32_t>(k) < a.vocab;
+    by_weight = p < 1.0f;
+    parts = p > 0.0f ? static_cast<uint32_t>(rint(static_cast<double>(fminf(p, 1.0f)) * 16777216.0)) : 0u;
+    least = mp > 0.0f ? static_cast<uint64_t>(rint(static_cast<double>(mp < 1.0f ? mp : 1.0f) * kOne)) : 1ull;
+    draw = !(u > 0.0f) ? 0u : u >= 1.0f ? 0xFFFFFFu : static_cast<uint32_t>(u * 16777216.0f);
+  }
+};
+
+// The draw of a row that has no weight, or takes its largest logit.
+__device__ __forceinline__ void draw_largest(const Draw& a, uint32_t b, float max, uint32_t first) {
+  if (threadIdx.x != 0) return;
+  a.tokens[b] = max == -INFINITY ? -1 : static_cast<int32_t>(first);
+  if (a.logprobs) a.logprobs[b] = max == -INFINITY ? -INFINITY : 0.0f;
+}
+
+// The draw of a row with top-k from the list of n tokens that hold its first k.
+__device__ __forceinline__ void draw_listed(Lds& s, const Draw& a, uint32_t b, uint32_t n, const Weigh& weigh, const Asked& asked) {
+  sort_list(s, n);
+  const uint32_t kept = cut_list(s, n, weigh, static_cast<uint32_t>(asked.k), 0, 0, asked.by_weight, asked.parts, asked.least);
+  // what is kept in the order of indices, each with its place in the list
+  uint64_t entry = 0;
+  const uint32_t i = threadIdx.x;
+  if (i < kept) entry = s.list[i] << 32 | i;
+  __syncthreads();
+  if (i < kept) s.list[i] = entry;
+  sort_list(s, kept);
+  const uint64_t w = i < kept ? s.list_weight[s.list[i] & 0xFFFFFFFFu] : 0;
+  uint64_t before, all, x, y;
+  block_before(s, w, 0, before, x, all, y);
+  const uint64_t target = share(all, asked.draw);
+  if (before <= target && target < before + w) {
+    a.tokens[b] = static_cast<int32_t>(s.list[i] >> 32);
+    if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w) / static_cast<double>(all)));
+  }
+}
+
+// The draw of a row from the kept weight of each of its runs.
 template <class S>
-__global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
+__device__ __forceinline__ void draw_from_runs(Lds& s, const Draw& a, uint32_t b, const typename S::storage* row, const Weigh& weigh,
+                                               const Asked& asked, const Cut& cut) {
+  const uint32_t runs = (a.vocab + kRun - 1) / kRun;
+  const uint64_t in_run = threadIdx.x < runs ? s.run_weight[threadIdx.x] : 0;
+  uint64_t w_before, w_all, x, y;
+  block_before(s, in_run, 0, w_before, x, w_all, y);
+  const uint64_t target = share(w_all, asked.draw);
+  if (w_before <= target && target < w_before + in_run) {  // one run of all
+    s.found = threadIdx.x;
+    s.before_weight = w_before;
+  }
+  __syncthreads();
+  if (threadIdx.x >= 64) return;
+
+  // the token inside the run
+  const uint32_t i0 = s.found * kRun + threadIdx.x * 8;
+  float l[8];
+  load8<S>(row, i0, a.vocab, l);
+  uint64_t w[8], sum = 0;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    w[e] = cut.keeps(key_of(l[e]), i0 + e) ? (weigh(l[e])) : 0;
+    if (w[e] < asked.least) w[e] = 0;
+    sum += w[e];
+  }
+  uint64_t upto = s.before_weight + wave_upto(sum) - sum;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    if (upto <= target && target < upto + w[e]) {
+      a.tokens[b] = static_cast<int32_t>(i0 + e);
+      if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w[e]) / static_cast<double>(w_all)));
+    }
+    upto += w[e];
+  }
+}
+
+// Few long rows, each split over workgroups of 8 runs, a run for each wave and 8 tokens for each lane. Sums are exact in
+// any order, so this gives the token that one workgroup gives; what it cannot serve (a larger k, lists that do not
+// hold a part's or the row's tokens) is left to that code.
+//   1. the largest logit of each part, and of each 64 tokens of it
+//   2. top-p without top-k: the part's weights by ranges, and these by 64 to the halving
+//   3. top-k: the bound from the maxima of 64 tokens, by counting; top-p: the halving and the range in it at which
+//      the share is reached, from the parts' sums; then the part's list, and the weights of its runs above it
+//   4. one workgroup for a row sorts the joined list, cuts it and draws
+// 4 fp32 rows of 151,936 with top-p 0.95: 5, 7, 10 and 19 us (one workgroup for each: 108); with top-k 50 4, 2, 8 and 14 (25).
+constexpr uint32_t kPartThreads = 512, kPartWaves = kPartThreads / 64;
+constexpr uint32_t kHalvings = (kRanges + 63) / 64, kAllRanges = 64 * kHalvings;
+constexpr uint32_t kPartList = 1024;
+constexpr uint32_t kPartGroups = kDrawPart / 64;
+static_assert(kPartThreads * 8 == kDrawPart && kPartWaves * kRun == kDrawPart, "a run for each wave");
+static_assert(kDrawPart * 64ull >= 1u << 18, "a lane for each part");
+static_assert(kDrawPartWords == 2 + kPartGroups / 2 + 64 + kAllRanges + kPartList + kPartWaves, "words of a part");
+
+struct Split {
+  uint64_t *best, *listed, *halving, *range, *list, *run, *sums;
+  uint32_t* group_max;
+  uint32_t parts;
+  __device__ __forceinline__ Split(uint64_t* work, uint32_t b, uint32_t vocab) {
+    parts = (vocab + kDrawPart - 1) / kDrawPart;
+    best = work + static_cast<size_t>(b) * (parts * kDrawPartWords + kDrawRowWords);
+    listed = best + parts;
+    halving = listed + parts;
+    range = halving + parts * 64;
+    list = range + parts * kAllRanges;
+    run = list + parts * kPartList;
+    group_max = reinterpret_cast<uint32_t*>(run + parts * kPartWaves);
+    sums = run + parts * (kPartWaves + kPartGroups / 2);
+  }
+  // The row's largest key << 32 | ~its lowest index; every wave for itself.
+  __device__ __forceinline__ uint64_t largest() const {
+    uint64_t v = threadIdx.x % 64 < parts ? best[threadIdx.x % 64] : 0;
+#pragma unroll
+    for (int m = 32; m > 0; m /= 2) {
+      const uint64_t other = __shfl_xor(v, m, 64);
+      v = other > v ? other : v;
+    }
+    return v;
+  }
+};
+
+enum class Way { kLargest, kCount, kWeight, kAll, kOther };
+__device__ __forceinline__ Way way_of(const Draw& a, uint32_t b, const Asked& asked, float max) {
+  if (max == -INFINITY || !(temperature_of(a, b) > 0.0f)) return Way::kLargest;
+  if (asked.by_count) return asked.k <= kMostK ? Way::kCount : Way::kOther;
+  return asked.by_weight ? Way::kWeight : Way::kAll;
+}
+
+template <class S>
+__device__ __forceinline__ const typename S::storage* row_of(const Draw& a, uint32_t b) {
+  return reinterpret_cast<const typename S::storage*>(a.logits) + static_cast<int64_t>(b) * a.row_stride;
+}
+
+template <class S>
+__global__ void __launch_bounds__(kPartThreads) split_max_kernel(const Draw a, uint64_t* work) {
+  __shared__ uint64_t wave_best[kPartWaves];
+  const uint32_t b = blockIdx.y, part = blockIdx.x;
+  const Split to(work, b, a.vocab);
+  const uint32_t i = part * kDrawPart + threadIdx.x * 8;
+  float l[8], mine = -INFINITY;
+  load8<S>(row_of<S>(a, b), i, a.vocab, l);
+  uint32_t at = 0xFFFFFFFFu;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    at = l[e] > mine ? i + e : at;
+    mine = l[e] > mine ? l[e] : mine;
+  }
+  uint64_t best = static_cast<uint64_t>(key_of(mine)) << 32 | (0xFFFFFFFFu - at);
+#pragma unroll
+  for (int m = 1; m < 64; m *= 2) {
+    const uint64_t other = __shfl_xor(best, m, 64);
+    best = other > best ? other : best;
+    if (m == 4 && threadIdx.x % 8 == 0) to.group_max[part * kPartGroups + threadIdx.x / 8] = static_cast<uint32_t>(best >> 32);
+  }
+  if (threadIdx.x % 64 == 0) wave_best[threadIdx.x / 64] = best;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (uint32_t w = 1; w < kPartWaves; ++w) best = wave_best[w] > best ? wave_best[w] : best;
+  to.best[part] = best;
+}
+
+template <class S>
+__global__ void __launch_bounds__(kPartThreads) split_ranges_kernel(const Draw a, uint64_t* work) {
+  __shared__ double table[kSteps];
+  __shared__ uint64_t range[kAllRanges];
+  const uint32_t b = blockIdx.y, part = blockIdx.x;
+  const Split to(work, b, a.vocab);
+  const float max = logit_of(static_cast<uint32_t>(to.largest() >> 32));
+  if (way_of(a, b, Asked(a, b), max) != Way::kWeight) return;  // all of the workgroup
+  float l[8];
+  load8<S>(row_of<S>(a, b), part * kDrawPart + threadIdx.x * 8, a.vocab, l);
+  for (uint32_t i = threadIdx.x; i < kSteps; i += kPartThreads) table[i] = exp2(44.0 + static_cast<double>(i) / kSteps);
+  for (uint32_t i = threadIdx.x; i < kAllRanges; i += kPartThreads) range[i] = 0;
+  __syncthreads();
+  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature_of(a, b)), (LdsTable)table};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    int n;
+    const uint64_t w = weigh(l[e], n);
+    if (w > 0) atomicAdd(reinterpret_cast<unsigned long long*>(&range[-n / 16]), static_cast<unsigned long long>(w));
+  }
+  __syncthreads();
+  for (uint32_t h = threadIdx.x / 64; h < 64; h += kPartWaves) {
+    uint64_t sum = 0;
+    if (h < kHalvings) {
+      const uint64_t w = range[h * 64 + threadIdx.x % 64];
+      to.range[part * kAllRanges + h * 64 + threadIdx.x % 64] = w;
+      sum = wave_sum(w);
+    }
+    if (threadIdx.x % 64 == 0) to.halving[part * 64 + h] = sum;
+  }
+}
+
+// The sums of 64 numbers over the parts, `stride` apart, and the first of them with which `need` is reached: its index, and the
+// sum before it. The same in all waves.
+struct Reached {
+  uint32_t index;
+  uint64_t before, all;
+};
+template <class F>
+__device__ __forceinline__ Reached reach(uint64_t (*sums)[64], const uint64_t* from, uint32_t stride, uint32_t parts, F need_of) {
+  const uint32_t lane = threadIdx.x % 64;
+  uint64_t sum = 0;
+#pragma unroll 4
+  for (uint32_t part = threadIdx.x / 64; part < parts; part += kPartWaves) sum += from[static_cast<size_t>(part) * stride + lane];
+  __syncthreads();  // earlier sums are read
+  sums[threadIdx.x / 64][lane] = sum;
+  __syncthreads();
+  sum = 0;
+  for (uint32_t w = 0; w < kPartWaves; ++w) sum += sums[w][lane];
+  const uint64_t upto = wave_upto(sum), all = __shfl(upto, 63, 64), need = need_of(all);
+  const uint64_t there = __ballot(upto >= need);
+  const uint32_t index = there == 0 ? 0 : static_cast<uint32_t>(__builtin_ctzll(there));  // (need is never above all)
+  return Reached{index, __shfl(upto - sum, static_cast<int>(index), 64), all};
+}
+
+template <class S>
+__global__ void __launch_bounds__(kPartThreads) split_list_kernel(const Draw a, uint64_t* work) {
+  __shared__ double table[kSteps];
+  __shared__ uint64_t sums[kPartWaves][64];
+  __shared__ uint32_t counts[16], bound[2], listed;
+  const uint32_t b = blockIdx.y, part = blockIdx.x;
+  const Split to(work, b, a.vocab);
+  const uint32_t top = static_cast<uint32_t>(to.largest() >> 32);
+  const float max = logit_of(top);
+  const Asked asked(a, b);
+  const Way way = way_of(a, b, asked, max);
+  if (way == Way::kLargest || way == Way::kOther) return;  // all of the workgroup
+  const uint32_t i0 = part * kDrawPart + threadIdx.x * 8;
+  float l[8];
+  load8<S>(row_of<S>(a, b), i0, a.vocab, l);
+  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature_of(a, b)), (LdsTable)table};
+  if (threadIdx.x == 0) listed = 0;
+
+  float low = INFINITY, high = INFINITY;  // of the list
+  uint32_t above = 0;                     // keys above this are kept, whatever the list says
+  if (way == Way::kCount) {
+    // the upper half of the key of the k-th largest of the maxima of 64 tokens
+    const uint32_t groups = to.parts * kPartGroups;
+    uint32_t m[64 * kPartGroups / kPartThreads];
+#pragma unroll
+    for (uint32_t j = 0; j < 64 * kPartGroups / kPartThreads; ++j) {
+      const uint32_t g = j * kPartThreads + threadIdx.x;
+      m[j] = g < groups ? to.group_max[g] : 0;
+    }
+    if (threadIdx.x < 16) counts[threadIdx.x] = 0;
+    __syncthreads();
+    uint32_t key = 0;
+    for (uint32_t bit = 0x80000000u, turn = 0; turn < 16; bit /= 2, ++turn) {
+      uint32_t count = 0;
+#pragma unroll
+      for (uint32_t j = 0; j < 64 * kPartGroups / kPartThreads; ++j) count += __popcll(__ballot(m[j] >= (key | bit)));
+      if (threadIdx.x % 64 == 0) atomicAdd(&counts[turn], count);
+      __syncthreads();
+      if (counts[turn] >= static_cast<uint32_t>(asked.k)) key |= bit;
+    }
+    low = key > key_of(-INFINITY) ? logit_of(key) : -INFINITY;  // (a key below that of -inf takes everything in)
+  } else {
+    for (uint32_t i = threadIdx.x; i < kSteps; i += kPartThreads) table[i] = exp2(44.0 + static_cast<double>(i) / kSteps);
+    __syncthreads();
+  }
+  if (way == Way::kWeight) {
+    uint64_t need = 0;
+    const Reached halving = reach(sums, to.halving, 64, to.parts, [&](uint64_t all) {
+      need = share(all, asked.parts);
+      if (need == 0) need = 1;
+      return need;
+    });
+    const Reached in = reach(sums, to.range + halving.index * 64, kAllRanges, to.parts, [&](uint64_t) { return need - halving.before; });
+    const int32_t found = static_cast<int32_t>(halving.index * 64 + in.index);
+    if (part == 0 && threadIdx.x == 0) {
+      to.sums[0] = halving.before + in.before;
+      to.sums[1] = halving.all;
+    }
+    if (threadIdx.x < 128) {
+      const uint32_t key = range_edge(weigh, top, threadIdx.x < 64 ? found : found - 1);
+      if (threadIdx.x % 64 == 0) bound[threadIdx.x / 64] = key;
+    }
+    __syncthreads();
+    low = logit_of(bound[0] + 1);
+    high = logit_of(bound[1]);
+    above = bound[1];
+  }
+  if (way != Way::kCount) {
+    uint64_t sum = 0;
+#pragma unroll
+    for (uint32_t e = 0; e < 8; ++e) {
+      const uint64_t w = weigh(l[e]);
+      sum += key_of(l[e]) > above && w >= asked.least ? w : 0;
+    }
+    sum = wave_sum(sum);
+    if (threadIdx.x % 64 == 0) to.run[part * kPartWaves + threadIdx.x / 64] = sum;
+  }
+  if (way == Way::kAll) return;
+#pragma unroll
+  for (uint32_t e = 0; e < 8; ++e) {
+    if (!(l[e] >= low && l[e] <= high) || i0 + e >= a.vocab) continue;
+    const uint32_t at = atomicAdd(&listed, 1u);
+    if (at < kPartList) to.list[part * kPartList + at] = static_cast<uint64_t>(~key_of(l[e])) << 32 | (i0 + e);
+  }
+  __syncthreads();
+  if (threadIdx.x == 0) to.listed[part] = listed;
+}
+
+// The end of a split row; false: it is left to the code for one workgroup.
+template <class S>
+__device__ __forceinline__ bool draw_split(Lds& s, const Draw& a, uint32_t b, uint64_t* work) {
+  const Split from(work, b, a.vocab);
+  const uint64_t best = from.largest();
+  const float max = logit_of(static_cast<uint32_t>(best >> 32));
+  const Asked asked(a, b);
+  const Way way = way_of(a, b, asked, max);
+  if (way == Way::kOther) return false;
+  if (way == Way::kLargest) {
+    draw_largest(a, b, max, 0xFFFFFFFFu - static_cast<uint32_t>(best));
+    return true;
+  }
+  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature_of(a, b)), (LdsTable)s.table};
+  Cut cut{0, a.vocab, 0};
+  const uint32_t lane = threadIdx.x % 64;
+  uint32_t n = 0;
+  if (way != Way::kAll) {
+    const uint32_t mine = lane < from.parts ? static_cast<uint32_t>(from.listed[lane]) : 0;
+    const uint32_t upto = static_cast<uint32_t>(wave_upto(mine));
+    n = __builtin_amdgcn_readlane(upto, 63);
+    if (__any(mine > kPartList) || n > kList) return false;
+    for (uint32_t part = threadIdx.x / 64; part < from.parts; part += kWaves) {
+      const uint32_t count = __shfl(mine, static_cast<int>(part), 64), to = __shfl(upto, static_cast<int>(part), 64) - count;
+      for (uint32_t i = lane; i < count; i += 64) s.list[to + i] = from.list[part * kPartList + i];
+    }
+    __syncthreads();
+    if (way == Way::kCount) {
+      draw_listed(s, a, b, n, weigh, asked);
+      return true;
+    }
+    sort_list(s, n);
+    const uint32_t kept = cut_list(s, n, weigh, n, from.sums[0], from.sums[1], true, asked.parts, 0);
+    n = kept;
+    const uint64_t last = s.list[kept - 1];
+    cut.key = ~static_cast<uint32_t>(last >> 32);
+    cut.last = static_cast<uint32_t>(last);
+  }
+  const uint32_t runs = (a.vocab + kRun - 1) / kRun;
+  if (threadIdx.x < runs) s.run_weight[threadIdx.x] = from.run[threadIdx.x];
+  __syncthreads();
+  for (uint32_t i = threadIdx.x; i < n; i += kThreads) {
+    const uint64_t w = s.list_weight[i];
+    if (w >= asked.least)
+      atomicAdd(reinterpret_cast<unsigned long long*>(&s.run_weight[static_cast<uint32_t>(s.list[i]) / kRun]), static_cast<unsigned long long>(w));
+  }
+  __syncthreads();
+  draw_from_runs<S>(s, a, b, row_of<S>(a, b), weigh, asked, cut);
+  return true;
+}
+
+template <class S, bool kSplit>
+__global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a, uint64_t* work) {
   typedef typename S::storage T;
   __shared__ Lds s;
   const uint32_t b = blockIdx.x, vocab = a.vocab;
-  const T* row = reinterpret_cast<const T*>(a.logits) + static_cast<int64_t>(b) * a.row_stride;
+  const T* row = row_of<S>(a, b);
   for (uint32_t i = threadIdx.x; i < kSteps; i += kThreads) s.table[i] = exp2(44.0 + static_cast<double>(i) / kSteps);
+  if constexpr (kSplit) {
+    __syncthreads();
+    if (draw_split<S>(s, a, b, work)) return;  // all of the workgroup
+  }
 
   // the largest logit and its lowest index
   float mine = -INFINITY;
@@ -650,21 +1035,17 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
   for (uint32_t i = 0; i < kWaves; ++i) best = s.part_weight[i] > best ? s.part_weight[i] : best;
   __syncthreads();
   const uint32_t top = static_cast<uint32_t>(best >> 32), first = 0xFFFFFFFFu - static_cast<uint32_t>(best);
-  const float max = logit_of(top), temperature = a.temperature ? a.temperature[b] : 1.0f;
+  const float max = logit_of(top), temperature = temperature_of(a, b);
   if (max == -INFINITY || !(temperature > 0.0f)) {
-    if (threadIdx.x == 0) {
-      a.tokens[b] = max == -INFINITY ? -1 : static_cast<int32_t>(first);
-      if (a.logprobs) a.logprobs[b] = max == -INFINITY ? -INFINITY : 0.0f;
-    }
+    draw_largest(a, b, max, first);
     return;
   }
-  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature), s.table};
-  const int32_t k = a.top_k ? a.top_k[b] : 0;
-  const float p = a.top_p ? a.top_p[b] : 1.0f, mp = a.min_p ? a.min_p[b] : 0.0f, u = a.u[b];
-  const bool by_count = k > 0 && static_cast<uint32_t>(k) < vocab, by_weight = p < 1.0f;
-  const uint32_t parts = p > 0.0f ? static_cast<uint32_t>(rint(static_cast<double>(fminf(p, 1.0f)) * 16777216.0)) : 0u;
-  const uint64_t least = mp > 0.0f ? static_cast<uint64_t>(rint(static_cast<double>(mp < 1.0f ? mp : 1.0f) * kOne)) : 1ull;
-  const uint32_t draw = !(u > 0.0f) ? 0u : u >= 1.0f ? 0xFFFFFFu : static_cast<uint32_t>(u * 16777216.0f);
+  const Weigh weigh{static_cast<double>(max), 1.0 / static_cast<double>(temperature), (LdsTable)s.table};
+  const Asked asked(a, b);
+  const int32_t k = asked.k;
+  const bool by_count = asked.by_count, by_weight = asked.by_weight;
+  const uint32_t parts = asked.parts;
+  const uint64_t least = asked.least;
 
   if (by_count && k <= kMostK) {
     // the upper half of the key of the k-th largest of the threads' maxima: one wave counts, 16 in each lane
@@ -690,24 +1071,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     __syncthreads();
     // (a key below that of -inf takes everything in)
     if (fill_list<S>(s, row, vocab, s.bound[0] > key_of(-INFINITY) ? logit_of(s.bound[0]) : -INFINITY, INFINITY)) {
-      const uint32_t n = s.listed;
-      sort_list(s, n);
-      const uint32_t kept = cut_list(s, n, weigh, static_cast<uint32_t>(k), 0, 0, by_weight, parts, least);
-      // what is kept in the order of indices, each with its place in the list
-      uint64_t entry = 0;
-      const uint32_t i = threadIdx.x;
-      if (i < kept) entry = s.list[i] << 32 | i;
-      __syncthreads();
-      if (i < kept) s.list[i] = entry;
-      sort_list(s, kept);
-      const uint64_t w = i < kept ? s.list_weight[s.list[i] & 0xFFFFFFFFu] : 0;
-      uint64_t before, all, x, y;
-      block_before(s, w, 0, before, x, all, y);
-      const uint64_t target = share(all, draw);
-      if (before <= target && target < before + w) {
-        a.tokens[b] = static_cast<int32_t>(s.list[i] >> 32);
-        if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w) / static_cast<double>(all)));
-      }
+      draw_listed(s, a, b, s.listed, weigh, asked);
       return;
     }
   }
@@ -722,14 +1086,14 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     bins = static_cast<uint32_t>(code_top - code_low) + 1;
     __syncthreads();  // the list is read
     if (bins <= kBins && top < 0xFF7F0000u) {  // (the largest bf16 may stand for +inf)
-      binned = cut_by_value(s, row, vocab, weigh, code_top, bins, by_count ? static_cast<uint32_t>(k) : 0u, by_weight, parts, cut);
+      binned = cut_by_value<kSplit>(s, row, vocab, weigh, code_top, bins, by_count ? static_cast<uint32_t>(k) : 0u, by_weight, parts, cut);
       if (!binned) cut = Cut{0, vocab, 0};
     }
   }
-  const bool counted = !binned && by_count && find_cut<S>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
+  const bool counted = !binned && by_count && find_cut<S, kSplit>(s, row, vocab, weigh, top, false, static_cast<uint64_t>(k), cut);
   if (by_weight && counted) {
     const uint64_t need = share(cut.weight, parts);
-    find_cut<S>(s, row, vocab, weigh, top, true, need == 0 ? 1 : need, cut);
+    find_cut<S, kSplit>(s, row, vocab, weigh, top, true, need == 0 ? 1 : need, cut);
   } else if (!binned && by_weight) {  // of all tokens that weigh anything: there are no more than k
     __syncthreads();
     for (uint32_t i = threadIdx.x; i < kRanges; i += kThreads) s.range[i] = 0;
@@ -767,13 +1131,7 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     const uint64_t above = s.before_weight;
     // the keys of that range lie between the last ones that this range and the one above it do not reach
     if (threadIdx.x < 128) {
-      const int32_t edge = threadIdx.x < 64 ? found : found - 1;
-      const uint32_t key = last_untaken([&](uint32_t key) {
-        if (key <= key_of(-INFINITY)) return false;
-        if (key >= top) return edge >= 0 || key > top;
-        int n;
-        return weigh(logit_of(key), n) > 0 && -n / 16 <= edge;
-      });
+      const uint32_t key = range_edge(weigh, top, threadIdx.x < 64 ? found : found - 1);
       if (threadIdx.x % 64 == 0) s.bound[threadIdx.x / 64] = key;
     }
     __syncthreads();
@@ -785,13 +1143,12 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
       cut.key = ~static_cast<uint32_t>(last >> 32);
       cut.last = static_cast<uint32_t>(last);
     } else {
-      find_cut<S>(s, row, vocab, weigh, top, true, need, cut);
+      find_cut<S, kSplit>(s, row, vocab, weigh, top, true, need, cut);
     }
   }
 
   __syncthreads();  // the list is read
   // the kept weight of each run of 512 tokens
-  const uint32_t runs = (vocab + kRun - 1) / kRun;
   if (binned) {
     // (without a cut all bins are kept, whatever the index)
     const uint32_t cut_bin = cut.key == 0 ? bins - 1 : static_cast<uint32_t>(code_top - code_of(logit_of(cut.key)));
@@ -849,55 +1206,50 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a) {
     if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
   });
   __syncthreads();
-  const uint64_t in_run = threadIdx.x < runs ? s.run_weight[threadIdx.x] : 0;
-  uint64_t w_before, w_all, x, y;
-  block_before(s, in_run, 0, w_before, x, w_all, y);
-  const uint64_t target = share(w_all, draw);
-  if (w_before <= target && target < w_before + in_run) {  // one run of all
-    s.found = threadIdx.x;
-    s.before_weight = w_before;
-  }
-  __syncthreads();
-  if (threadIdx.x >= 64) return;
-
-  // the token inside the run
-  const uint32_t i0 = s.found * kRun + threadIdx.x * 8;
-  float l[8];
-  load8<S>(row, i0, vocab, l);
-  uint64_t w[8], sum = 0;
-#pragma unroll
-  for (uint32_t e = 0; e < 8; ++e) {
-    w[e] = cut.keeps(key_of(l[e]), i0 + e) ? (weigh(l[e])) : 0;
-    if (w[e] < least) w[e] = 0;
-    sum += w[e];
-  }
-  uint64_t upto = s.before_weight + wave_upto(sum) - sum;
-#pragma unroll
-  for (uint32_t e = 0; e < 8; ++e) {
-    if (upto <= target && target < upto + w[e]) {
-      a.tokens[b] = static_cast<int32_t>(i0 + e);
-      if (a.logprobs) a.logprobs[b] = static_cast<float>(log(static_cast<double>(w[e]) / static_cast<double>(w_all)));
-    }
-    upto += w[e];
-  }
+  draw_from_runs<S>(s, a, b, row, weigh, asked, cut);
 }
 
 }  // namespace
 }  // namespace zo
 
-extern "C" int zo_draw(const zo_draw_args* p, void* stream) {
+namespace {
+
+int draw_rows(const zo_draw_args* p, uint64_t* work, void* stream) {
   using namespace zo;
-  if (p == nullptr) return ZO_ERR_NULL;
-  const int rc = check_draw(*p);
-  if (rc != ZO_OK) return rc;
-  if (p->rows == 0) return ZO_OK;
   const Draw a{static_cast<const char*>(p->logits), p->row_stride, p->u, p->temperature, p->top_k, p->top_p, p->min_p, p->tokens,
                p->logprobs, p->vocab};
   (void)hipGetLastError();
   hipStream_t st = static_cast<hipStream_t>(stream);
+  const auto launch = [&](auto type) {
+    typedef decltype(type) S;
+    if (work == nullptr) {
+      draw_kernel<S, false><<<dim3(p->rows), dim3(kThreads), 0, st>>>(a, nullptr);
+      return;
+    }
+    const dim3 grid((p->vocab + kDrawPart - 1) / kDrawPart, p->rows);
+    split_max_kernel<S><<<grid, dim3(kPartThreads), 0, st>>>(a, work);
+    if (p->top_p != nullptr) split_ranges_kernel<S><<<grid, dim3(kPartThreads), 0, st>>>(a, work);
+    split_list_kernel<S><<<grid, dim3(kPartThreads), 0, st>>>(a, work);
+    draw_kernel<S, true><<<dim3(p->rows), dim3(kThreads), 0, st>>>(a, work);
+  };
   if (p->dtype == ZO_F32)
-    draw_kernel<F32><<<dim3(p->rows), dim3(kThreads), 0, st>>>(a);
+    launch(F32{});
   else
-    draw_kernel<BF16><<<dim3(p->rows), dim3(kThreads), 0, st>>>(a);
+    launch(BF16{});
   return launched();
+}
+
+}  // namespace
+
+extern "C" int zo_draw(const zo_draw_args* p, void* stream) {
+  if (p == nullptr) return ZO_ERR_NULL;
+  const int rc = zo::check_draw(*p);
+  return rc != ZO_OK || p->rows == 0 ? rc : draw_rows(p, nullptr, stream);
+}
+
+extern "C" int zo_draw_split(const zo_draw_args* p, void* work, uint64_t work_bytes, void* stream) {
+  if (p == nullptr) return ZO_ERR_NULL;
+  const int rc = zo::check_draw_split(*p, work, work_bytes);
+  if (rc != ZO_OK || p->rows == 0) return rc;
+  return draw_rows(p, zo_draw_work(p->rows, p->vocab, p->top_k != nullptr) != 0 ? static_cast<uint64_t*>(work) : nullptr, stream);
 }

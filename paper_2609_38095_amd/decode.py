@@ -35,11 +35,11 @@ ZO_ROTARY_LINEAR, ZO_ROTARY_BASE, ZO_ROTARY_BANDS = 0, 1, 2
 
 EXPORTS = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back",
            "zo_norm_rotate_back_work", "zo_cache_attend", "zo_cache_attend_work", "zo_cache_copy", "zo_draw",
-           "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork", "zo_pages_extend", "zo_pages_drop",
+           "zo_draw_split", "zo_draw_work", "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork", "zo_pages_extend", "zo_pages_drop",
            "zo_pages_left", "zo_pages_length", "zo_pages_table", "zo_pages_compact")
 # entry points that _tensors.so calls, in the order that it takes their addresses in
 _CALLED = ("zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_norm_rotate_back_work", "zo_cache_attend",
-           "zo_cache_attend_work", "zo_cache_copy", "zo_draw")
+           "zo_cache_attend_work", "zo_cache_copy", "zo_draw_split", "zo_draw_work")
 
 _READY = None
 _TENSORS = None
@@ -62,6 +62,7 @@ def _lib():
                 ("zo_norm_rotate_back", [args, vp], i32), ("zo_norm_rotate_back_work", [u32, u32, u32, u32], u64),
                 ("zo_cache_attend", [args, vp], i32), ("zo_cache_attend_work", [u32, u32, u32, u32], u64),
                 ("zo_cache_copy", [args, args, u32, vp, u32, i32, vp], i32), ("zo_draw", [args, vp], i32),
+                ("zo_draw_split", [args, vp, u64, vp], i32), ("zo_draw_work", [u32, u32, i32], u64),
                 ("zo_pages_open", [u32, u32], vp), ("zo_pages_close", [vp], None),
                 ("zo_pages_add", [vp, u32, pu], i32), ("zo_pages_fork", [vp, u32, pu], i32),
                 ("zo_pages_extend", [vp, u32, u32, move], i32), ("zo_pages_drop", [vp, u32], i32),
@@ -180,11 +181,13 @@ def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):
           _int32s(dst), _int32s(rows))
 
 
-def zo_draw(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=False, tokens=None, stream=None):
+def zo_draw(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, logprobs=False, tokens=None, work=None, stream=None):
     """int32 tokens [rows] drawn from logits [rows, vocab] with the random numbers u [rows] in [0, 1), each row with
     its temperature, top_k (int32), top_p and min_p (device tensors [rows] or None). logprobs: also returns
-    the drawn tokens' log probabilities among what was kept, float32."""
-    return _call((_TENSORS or _tensors()).draw, stream, logits, logits, u, temperature, top_k, top_p, min_p, logprobs, tokens)
+    the drawn tokens' log probabilities among what was kept, float32. work: a tensor of zo_draw_work() bytes
+    (allocated if None)."""
+    return _call((_TENSORS or _tensors()).draw, stream, logits, logits, u, temperature, top_k, top_p, min_p, logprobs, tokens,
+                 work)
 
 
 class ZoPages:

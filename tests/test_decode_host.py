@@ -223,3 +223,19 @@ def test_launches_of_2_to_the_32_threads_are_refused():
     for tokens, heads in ((1 << 15, 5), (1 << 20, 1), (1 << 12, 64)):  # pages of 64-dim heads above 2^23 elements
         cache = struct.pack("QQqqqIIII", 1 << 20, 1 << 40, tokens * heads * 64, tokens * 64, 64, 4, heads, tokens, 64)
         assert lib.zo_cache_copy(cache, one, 1, moves.ctypes.data, 1, 0, None) == zo.ZO_ERR_ARG
+
+
+def test_draw_split_workspace_is_checked():
+    lib = decode._lib()
+    draw = struct.Struct("QqQQQQQQQIIi4x")  # zo_draw_args
+    call = lambda work, size, rows=4, vocab=50_272, top_p=0, stride=50_272: lib.zo_draw_split(  # noqa: E731
+        draw.pack(0x1000, stride, 0x2000, 0, 0, top_p, 0, 0x3000, 0, rows, vocab, 0), work, size, None)
+    need = lib.zo_draw_work(4, 50_272, 0)
+    assert need > 0 and need % 8 == 0
+    assert call(None, need) == zo.ZO_ERR_NULL
+    assert call(0x10000, need - 1) == call(0x10008, need) == call(0x10000, 0) == call(0x10000, need, stride=-1) == zo.ZO_ERR_ARG
+    assert call(0x10000, need, top_p=0x2002) == call(0x10000, need, vocab=0) == zo.ZO_ERR_ARG
+    assert lib.zo_draw_split(None, 0x10000, need, None) == zo.ZO_ERR_NULL
+    assert call(None, 0, rows=0) == zo.ZO_OK
+    for rows, vocab, top_k in ((0, 50_272, 0), (33, 151_936, 0), (4, 16_383, 0), (4, (1 << 18) + 1, 0), (17, 151_936, 1), (4, 50_272, 1)):
+        assert lib.zo_draw_work(rows, vocab, top_k) == 0

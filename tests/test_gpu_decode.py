@@ -652,3 +652,39 @@ def test_work_and_outputs_given():
     assert zo.zo_draw(logits, u, tokens=tokens) is not None and torch.equal(tokens, zo.zo_draw(logits, u))
     assert zo.zo_draw(logits[:0], u[:0]).shape == (0,)
     assert zo.zo_cache_attend(q[:0], kc, vc, table[:0], lengths[:0]).shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kind,vocab", [("peaked", 16_384), ("masked", 16_385), ("ties", 20_000), ("flat", 33_000), ("steep", 40_001),
+                                        ("masked", 65_536), ("ties", 70_000), ("flat", 100_001), ("steep", 131_073),
+                                        ("sorted", 151_936), ("peaked", (1 << 18) - 1)])
+def test_draw_of_few_rows_is_that_of_many(kind, vocab, dtype):
+    """Rows split over workgroups (few long ones) give what one workgroup for a row gives (the same rows repeated), and the oracle's
+    tokens, where a part's list overflows too (ties, flat and sorted rows). The shorter rows are split without top-k only."""
+    from paper_2609_38095_amd import decode
+    settings = [  # temperature, top_k, top_p, min_p, u
+        (1.0, 0, 1.0, 0.0, 0.5), (0.7, 0, 0.9, 0.0, 0.1), (1.3, 40, 1.0, 0.0, 0.99999994), (1.0, 512, 0.8, 0.0, 0.7),
+        (1.0, 513, 0.9, 0.0, 0.9), (0.8, 0, 0.95, 0.01, 0.3), (1.0, 0, 1.0, 0.05, 0.6), (0.0, 0, 0.5, 0.0, 0.8),
+        (1e30, 0, 0.5, 0.0, 0.5), (1e-30, 0, 0.5, 0.0, 0.5), (1.0, 1, 0.0, 0.0, 0.5), (1.0, 0, 0.0, 0.0, 0.99)]
+    rows = len(settings)
+    x = draw_rows("peaked" if kind == "sorted" else kind, rows, vocab, dtype, 3)
+    if kind == "sorted":
+        x = x.float().sort(dim=1, descending=True).values.to(x.dtype)
+    counted = vocab >= 65_536
+    need = decode._lib().zo_draw_work(rows, vocab, counted)
+    assert need > 0 and decode._lib().zo_draw_work(4 * rows, vocab, counted) == 0
+    t, k, p, m, u = (torch.tensor(c, dtype=torch.int32 if i == 1 else torch.float32, device="cuda") for i, c in enumerate(zip(*settings)))
+    k, k_many = (k, k.repeat(4)) if counted else (None, None)
+    work = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    token, logprob = zo.zo_draw(x, u, t, k, p, m, logprobs=True, work=work)
+    many = zo.zo_draw(x.repeat(4, 1), u.repeat(4), t.repeat(4), k_many, p.repeat(4), m.repeat(4), logprobs=True)
+    again = zo.zo_draw(x, u, t, k, p, m, logprobs=True)
+    for j in range(4):
+        assert torch.equal(many[0][j * rows:(j + 1) * rows], token) and torch.equal(many[1][j * rows:(j + 1) * rows], logprob)
+    assert torch.equal(again[0], token) and torch.equal(again[1], logprob)
+    host = x.float().cpu().numpy()
+    for b, (ti, ki, pi, mi, ui) in enumerate(settings):
+        want, _ = oracle.draw(host[b], ui, ti, ki if counted else 0, pi, mi)
+        assert int(token[b]) == want, (b, settings[b])
+    with pytest.raises(zo.ZoError):
+        zo.zo_draw(x, u, t, k, p, m, work=work[16:])
