@@ -688,3 +688,26 @@ def test_draw_of_few_rows_is_that_of_many(kind, vocab, dtype):
         assert int(token[b]) == want, (b, settings[b])
     with pytest.raises(zo.ZoError):
         zo.zo_draw(x, u, t, k, p, m, work=work[16:])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_split_draw_on_a_stream_and_in_a_graph(dtype):
+    """New logits and randoms in each replay, with eager draws between; no replay leans on what the workspace held."""
+    x, u = draw_rows("peaked", 6, 50_272, dtype, 7), torch.rand(6, device="cuda")
+    p = torch.tensor([0.9, 1.0, 0.3, 0.95, 0.0, 0.99], device="cuda")
+    side = torch.cuda.Stream()
+    want = zo.zo_draw(x, u, top_p=p, logprobs=True)
+    torch.cuda.synchronize()
+    got = zo.zo_draw(x, u, top_p=p, logprobs=True, stream=side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = zo.zo_draw(x, u, top_p=p, logprobs=True)
+    for turn in range(4):
+        x.copy_(draw_rows(("peaked", "steep", "ties", "masked")[turn], 6, 50_272, dtype, turn))
+        u.copy_(torch.rand(6, device="cuda"))
+        graph.replay()
+        torch.cuda.synchronize()
+        want = zo.zo_draw(x.repeat(6, 1), u.repeat(6), top_p=p.repeat(6), logprobs=True)  # a workgroup for each row
+        assert torch.equal(held[0], want[0][:6]) and torch.equal(held[1], want[1][:6])
