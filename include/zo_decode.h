@@ -169,7 +169,8 @@ int zo_norm_rotate_back(const zo_rotate_back* b, void* stream);
  * of a sequence that was split are joined by a second launch. work: device memory of
  * zo_cache_attend_work() bytes, aligned to 16, contents irrelevant, one for each call in flight.
  * Weights are exp2 in fp32; for bf16 each is split in two bf16 parts (16 bits of it) where it meets
- * the values, and sums are fp32.
+ * the values, and sums are fp32. A value that is infinite or NaN reaches the outputs of its own sequence and
+ * dim, and makes them what the formula says as long as its weight is above 2^-90 of the largest.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (dtype, alignment, dim = 0 or above ZO_DIM_MAX, heads, pages or
  * page_tokens 0, too little work, 2^24 rows or more); ZO_ERR_NONFINITE (scale); ZO_ERR_HIP.
  */

@@ -441,14 +441,15 @@ __global__ void __launch_bounds__(kThreads, kAny ? (kDim > 128 ? 1 : 2) : waves_
       }
 
       if constexpr (sizeof(T) == 2) {
-        // weights as a sum of two bf16: 16 bits of each, so that only the output is rounded to 8
+        // weights as a sum of two bf16, 16 bits of each, so that only the output is rounded to 8. Both are positive: the largest
+        // bf16 below the weight and what is left of it. A signed or empty rest would make a NaN of an infinite value.
         u32x4 hi, lo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p0 = p[2 * i], p1 = p[2 * i + 1];
-          hi[i] = pack_bf16x2(p0, p1);
-          const float h0 = __uint_as_float(hi[i] << 16), h1 = __uint_as_float(hi[i] & 0xFFFF0000u);
-          lo[i] = pack_bf16x2(p0 - h0, p1 - h1);
+          const uint32_t b0 = __builtin_elementwise_sub_sat(__float_as_uint(p0), 1u), b1 = __builtin_elementwise_sub_sat(__float_as_uint(p1), 1u);
+          hi[i] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
+          lo[i] = pack_bf16x2(p0 - __uint_as_float(b0 & 0xFFFF0000u), p1 - __uint_as_float(b1 & 0xFFFF0000u));
         }
 #pragma unroll
         for (uint32_t w = 0; w < kValWords; ++w) {

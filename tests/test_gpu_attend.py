@@ -1,0 +1,72 @@
+"""zo_cache_attend where its arithmetic can go wrong: infinite values."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_38095_amd as zo
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+FORMS = [(64, 16), (128, 16), (128, 48), (256, 32), (20, 5), (96, 16)]  # head size, page: matrix-core and element-wise forms
+
+
+def normal(seed, shape, dtype, scale=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.empty(shape, device="cuda").normal_(0, scale, generator=g).to(TYPES[dtype])
+
+
+def paged(lengths, page, heads, dim, dtype, seed):
+    """Caches and a table in which sequence s has pages of its own, in order."""
+    width = max(1, -(-max(lengths) // page))
+    table = torch.arange(len(lengths) * width, dtype=torch.int32, device="cuda").view(len(lengths), width)
+    k, v = (normal(seed + i, (len(lengths) * width, heads, page, dim), dtype) for i in range(2))
+    return k, v, table, torch.tensor(lengths, dtype=torch.int32, device="cuda")
+
+
+def place(cache, table, page, seq, token, dim, value):
+    cache[int(table[seq, token // page]), :, token % page, dim] = value
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", FORMS)
+@pytest.mark.parametrize("seed", range(3))
+def test_infinite_values_reach_every_head(dim, page, dtype, seed):
+    """An infinite value under any weight is that infinity in the output, for the only token of a sequence (weight 1) and the one
+    with the largest weight too; infinities of both signs, or a NaN, make a NaN. The other dims are as without them."""
+    inf, nan = float("inf"), float("nan")
+    lengths, hq, hk = [1, 2, 20, 33, 300], 24, 4
+    k, v, table, n = paged(lengths, page, hk, dim, dtype, 10 * seed)
+    q = normal(100 + seed, (len(lengths), hq, dim), dtype)
+    plain = zo.zo_cache_attend(q, k, v, table, n)
+    rng = np.random.default_rng(seed)
+    for s, length in enumerate(lengths):
+        best = int(torch.stack([k[int(table[s, t // page]), 0, t % page].float() @ q[s, 0].float() for t in range(length)]).argmax())
+        place(v, table, page, s, best, 3, inf)
+        place(v, table, page, s, best, 4, -inf)
+        place(v, table, page, s, int(rng.integers(length)), 5, inf)
+        place(v, table, page, s, int(rng.integers(length)), 6, -inf)
+        place(v, table, page, s, 0, 7, inf)
+        place(v, table, page, s, length - 1, 7, -inf if length > 1 else nan)
+        place(v, table, page, s, int(rng.integers(length)), 8, nan)
+    out = zo.zo_cache_attend(q, k, v, table, n)
+    for i, want in ((3, inf), (4, -inf), (5, inf), (6, -inf)):
+        assert bool((out[..., i] == want).all()), i
+    assert bool(out[..., 7:9].isnan().all())
+    rest = [i for i in range(dim) if not 3 <= i <= 8]
+    assert torch.equal(out[..., rest], plain[..., rest])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", FORMS)
+def test_an_infinite_value_under_a_small_weight(dim, page, dtype):
+    """Weights down to e^-55 of the largest."""
+    k, v, table, n = paged([40], page, 1, dim, dtype, 5)
+    k.zero_()
+    q = torch.zeros(1, 2, dim, dtype=TYPES[dtype], device="cuda")
+    q[..., 0] = 1.0
+    for t in range(1, 20):
+        place(k, table, page, 0, t, 0, -2.9 * t)
+        place(v, table, page, 0, t, t, float("inf"))
+    assert bool((zo.zo_cache_attend(q, k, v, table, n, 1.0)[..., 1:20] == float("inf")).all())
