@@ -1,9 +1,10 @@
 // Attention of one new token of each sequence over the paged cache, for gfx950.
 //
-// Mathematics. One pass over the cached tokens with a running maximum m and sum l:
-// x_j = scale log2(e) q . k_j, p_j = 2^(x_j - m), l = sum p_j, o = sum p_j v_j; a larger maximum scales l
-// and o by 2^(m - m'). The maximum is raised only when a score passes it by more than 2^8, which
-// fp32 has room for, so that the usual tile neither exchanges maxima between lanes nor rescales o.
+// Mathematics. One pass over the cached tokens with a running bound m of the scores and a sum l:
+// x_j = scale log2(e) q . k_j, p_j = 2^(x_j - m), l = sum p_j, o = sum p_j v_j; a larger bound scales l
+// and o by 2^(m - m'). Only a score above the bound raises it, to 8 above the largest score, so that the usual
+// tile neither exchanges maxima between lanes nor rescales o; weights are at most 1 all the same, as in a
+// softmax by the maximum itself, and values up to the type's largest do not overflow by them.
 // Parts of a sequence join by the same rule.
 //
 // Split. An item is one sequence, one key head and up to 16 of its query heads: they read the same
@@ -42,7 +43,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr uint32_t kThreads = 256;
 constexpr uint32_t kWave = 64, kWaves = kThreads / kWave;
-constexpr float kLazy = 8.0f;  // how far (in powers of two) scores may pass the maximum in use
+constexpr float kLazy = 8.0f;  // how far (in powers of two) the bound of the scores is set above their maximum
 
 // Where an item's parts are: those of workers first .. last, the first one's in `slot`, the others' in slot 0;
 // the waves of workgroups group0 .. group1 - 1 have theirs together, with the workgroup's first wave.
@@ -422,10 +423,10 @@ __global__ void __launch_bounds__(kThreads, kAny ? (kDim > 128 ? 1 : 2) : waves_
       float top = x[0];
 #pragma unroll
       for (uint32_t i = 1; i < kKeys; ++i) top = fmaxf(top, x[i]);
-      if (__any(top > m + kLazy)) {
-        top = fmaxf(top, m);
+      if (__any(top > m)) {
         top = fmaxf(top, __shfl_xor(top, 16, 64));
         top = fmaxf(top, __shfl_xor(top, 32, 64));
+        top = fmaxf(top + kLazy, m);
         const float scale = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);  // m = -inf: 0
         l *= scale;
 #pragma unroll

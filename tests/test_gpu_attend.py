@@ -1,4 +1,4 @@
-"""zo_cache_attend where its arithmetic can go wrong: infinite values."""
+"""zo_cache_attend where its arithmetic can go wrong: infinite and very large values."""
 
 import numpy as np
 import pytest
@@ -70,3 +70,23 @@ def test_an_infinite_value_under_a_small_weight(dim, page, dtype):
         place(k, table, page, 0, t, 0, -2.9 * t)
         place(v, table, page, 0, t, t, float("inf"))
     assert bool((zo.zo_cache_attend(q, k, v, table, n, 1.0)[..., 1:20] == float("inf")).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", FORMS)
+def test_the_largest_finite_values_stay_finite(dim, page, dtype):
+    """Weights are at most 1 while they are summed, however the scores rise along a sequence: a value near the type's largest does
+    not overflow. The last score is 5.375 above the first (2^7.75), the others are far below; so the sum of all weights is 1.0046 of
+    the last one. 512 sequences of 8 key heads (with the same pages): each wave has all tiles of a sequence."""
+    most = torch.finfo(TYPES[dtype]).max
+    for length in (2, 33, 70):
+        k, v, table, _ = paged([length], page, 8, dim, dtype, 5)
+        k.zero_(), v.zero_()
+        for t in range(length):
+            place(k, table, page, 0, t, 0, 5.375 if t == length - 1 else -40.0 if t else 0.0)
+        place(v, table, page, 0, length - 1, slice(None), most)
+        q = torch.zeros(512, 16, dim, dtype=TYPES[dtype], device="cuda")
+        q[..., 0] = 1.0
+        n = torch.full((512,), length, dtype=torch.int32, device="cuda")
+        out = zo.zo_cache_attend(q, k, v, table.repeat(512, 1), n, 1.0).float()
+        assert bool(((out > 0.99 * most) & (out < most)).all()), length
