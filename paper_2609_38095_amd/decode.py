@@ -27,7 +27,7 @@ import os
 import numpy as np
 import torch
 
-from . import PKG_DIR, ZoLibraryMissing, _check, _lib as _base_lib, _stream
+from . import PKG_DIR, ZO_ERR_ARG, ZoError, ZoLibraryMissing, _check, _lib as _base_lib, _stream
 
 ZO_ERR_MEMORY, ZO_ERR_FULL = -5, -6
 ZO_DIM_MAX = 256
@@ -248,7 +248,9 @@ class ZoPages:
 
     def compact(self, room=None):
         """Moves pages in use to the lowest ids; returns (src, dst, rows) to hand to zo_cache_copy."""
-        room = self.pages if room is None else room
+        room = self.pages if room is None else min(room, self.pages)
+        if room < 0:
+            raise ZoError(ZO_ERR_ARG, "zo_pages_compact")
         moves = np.zeros((max(room, 1), 3), np.int32)
         n = ctypes.c_uint32()
         _check(_lib().zo_pages_compact(self._book, moves.ctypes.data, room, ctypes.byref(n)), "zo_pages_compact")
