@@ -22,6 +22,7 @@ is the caller's.
 
 import contextlib
 import ctypes
+import operator
 import os
 
 import numpy as np
@@ -126,6 +127,26 @@ def _call(f, stream, like, *args):
     return got
 
 
+def _whole(x, dtype, call):
+    """x as an array of a whole type that holds every number of it."""
+    x = np.asarray(x)
+    try:
+        with np.errstate(invalid="ignore"):
+            whole = x.astype(dtype)
+    except OverflowError:
+        raise ZoError(ZO_ERR_ARG, call) from None
+    if not np.array_equal(whole, x):
+        raise ZoError(ZO_ERR_ARG, call)
+    return whole
+
+
+def _count(n, call):
+    """n where it fits the 32 bits that the library takes (ctypes would hand on the lowest ones)."""
+    if not 0 <= operator.index(n) < 1 << 32:
+        raise ZoError(ZO_ERR_ARG, call)
+    return n
+
+
 def _doubles(turns):
     """Frequencies as an array of float64; None for none."""
     return turns if turns is None or type(turns) is np.ndarray and turns.dtype == np.float64 else np.array(turns, np.float64)
@@ -133,7 +154,7 @@ def _doubles(turns):
 
 def zo_rotary_turns(rotary, base=10000.0, kind=ZO_ROTARY_LINEAR, factor=1.0, original=0.0, low=1.0, high=4.0):
     """Rotation frequencies in turns per position, float64 [rotary / 2]; factor > 1 scales them for long contexts."""
-    out = np.zeros(max(int(rotary) // 2, 1))
+    out = np.zeros(max(_count(rotary, "zo_rotary_turns") // 2, 1))
     _check(_lib().zo_rotary_turns(kind, rotary, base, factor, original, low, high, out.ctypes.data), "zo_rotary_turns")
     return out
 
@@ -170,7 +191,7 @@ def zo_cache_attend(q, k_cache, v_cache, table, lengths, scale=None, out=None, l
 
 
 def _int32s(x):
-    return x if x is None or type(x) is np.ndarray and x.dtype == np.int32 else np.array(x, np.int32)
+    return x if x is None or type(x) is np.ndarray and x.dtype == np.int32 else _whole(x, np.int32, "zo_cache_copy")
 
 
 def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):
@@ -195,7 +216,8 @@ class ZoPages:
 
     def __init__(self, pages, page_tokens):
         self._book = None
-        self._book = _lib().zo_pages_open(pages, page_tokens)
+        if 0 <= pages < 1 << 32 and 0 <= page_tokens < 1 << 32:
+            self._book = _lib().zo_pages_open(pages, page_tokens)
         if not self._book:
             raise ValueError(f"no page book of {pages} pages of {page_tokens} tokens")
         self._close = _lib().zo_pages_close
@@ -209,23 +231,24 @@ class ZoPages:
     def add(self, tokens=0):
         """A new sequence with room for `tokens` tokens; returns its number."""
         seq = ctypes.c_uint32()
-        _check(_lib().zo_pages_add(self._book, tokens, ctypes.byref(seq)), "zo_pages_add")
+        _check(_lib().zo_pages_add(self._book, _count(tokens, "zo_pages_add"), ctypes.byref(seq)), "zo_pages_add")
         return seq.value
 
     def fork(self, seq):
         """A new sequence with the tokens of seq, sharing its pages; returns its number."""
         forked = ctypes.c_uint32()
-        _check(_lib().zo_pages_fork(self._book, seq, ctypes.byref(forked)), "zo_pages_fork")
+        _check(_lib().zo_pages_fork(self._book, _count(seq, "zo_pages_fork"), ctypes.byref(forked)), "zo_pages_fork")
         return forked.value
 
     def extend(self, seq, tokens=1):
         """Room for more tokens; returns the copy that this needs first, (src, dst, rows), or None."""
         move = ZoPageMove()
-        _check(_lib().zo_pages_extend(self._book, seq, tokens, ctypes.byref(move)), "zo_pages_extend")
+        _check(_lib().zo_pages_extend(self._book, _count(seq, "zo_pages_extend"), _count(tokens, "zo_pages_extend"),
+                                      ctypes.byref(move)), "zo_pages_extend")
         return (move.src, move.dst, move.rows) if move.rows else None
 
     def drop(self, seq):
-        _check(_lib().zo_pages_drop(self._book, seq), "zo_pages_drop")
+        _check(_lib().zo_pages_drop(self._book, _count(seq, "zo_pages_drop")), "zo_pages_drop")
 
     def left(self):
         """How many pages are free."""
@@ -233,11 +256,11 @@ class ZoPages:
 
     def length(self, seq):
         """The tokens of a sequence, -1 if there is none of that number."""
-        return _lib().zo_pages_length(self._book, seq)
+        return _lib().zo_pages_length(self._book, seq) if 0 <= seq < 1 << 32 else -1
 
     def table(self, seqs, width=None):
         """(page ids int32 [sequences, width], lengths int32 [sequences]) as numpy arrays."""
-        seqs = np.ascontiguousarray(np.asarray(seqs, dtype=np.uint32).reshape(-1))
+        seqs = np.ascontiguousarray(_whole(seqs, np.uint32, "zo_pages_table").reshape(-1))
         lengths = np.zeros(len(seqs), np.int32)
         if width is None:
             width = max([1] + [-(-self.length(s) // self.page_tokens) for s in seqs.tolist()])

@@ -26,3 +26,37 @@ def test_compact_takes_the_room_that_it_is_given():
         book, high = holed_book()
         src, dst, rows = book.compact(room)
         assert len(src) == len(dst) == len(rows) == moved and rows.tolist() == [4] * moved
+
+
+def refused(call, *args, **kw):
+    with pytest.raises(zo.ZoError) as e:
+        call(*args, **kw)
+    assert e.value.status == zo.ZO_ERR_ARG
+
+
+def test_page_ids_are_whole_numbers_of_32_bits():
+    """2^32 + 1 is not page 1, and neither is 1.5 (a call without caches copies nothing, and is checked all the same)."""
+    for bad in ([2 ** 32 + 1], np.array([2 ** 32 + 1]), np.array([-2 ** 32]), np.array([2 ** 31]), np.array([2 ** 64 - 1], np.uint64), [2 ** 70],
+                [1.5], np.array([1.5]), np.array([2.0 ** 32]), [float("nan")], [float("inf")]):
+        for args in ((bad, [2]), ([2], bad), ([2], [3], bad)):
+            refused(zo.zo_cache_copy, [], [], *args)
+    for good in ([1], (1,), np.array([1]), np.array([1], np.uint8), np.array([1, 7])[:1], np.array([1.0]), range(1, 2), []):
+        zo.zo_cache_copy([], [], good, good, good)
+    zo.zo_cache_copy([], [], [1], [2])
+
+
+def test_counts_and_sequences_fit_32_bits():
+    book = zo.ZoPages(8, 4)
+    a = book.add(6)
+    for wide in (2 ** 32, 2 ** 32 + 1, -2 ** 32, 2 ** 64 + 1, -1):
+        for call in (book.add, book.fork, book.drop, book.extend, lambda n: book.extend(a, n), lambda n: book.table([n]),
+                     lambda n: book.table(np.array([n])), lambda n: book.table([a, n], width=4)):
+            refused(call, wide)
+        assert book.length(wide) == -1 and book.length(a) == 6 and book.left() == 6
+        for args in ((wide, 4), (8, wide)):
+            with pytest.raises(ValueError):
+                zo.ZoPages(*args)
+        refused(zo.zo_rotary_turns, wide + 64)
+    refused(book.table, [0.5])
+    ids, lengths = book.table(np.array([a], np.int64))
+    assert lengths.tolist() == [6] and book.table([])[0].shape == (0, 1)
