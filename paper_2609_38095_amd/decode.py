@@ -149,7 +149,9 @@ def _count(n, call):
 
 def _doubles(turns):
     """Frequencies as an array of float64; None for none."""
-    return turns if turns is None or type(turns) is np.ndarray and turns.dtype == np.float64 else np.array(turns, np.float64)
+    if turns is None or type(turns) is np.ndarray and turns.dtype == np.float64 and turns.flags.c_contiguous:
+        return turns
+    return np.array(turns, np.float64, order="C")
 
 
 def zo_rotary_turns(rotary, base=10000.0, kind=ZO_ROTARY_LINEAR, factor=1.0, original=0.0, low=1.0, high=4.0):
@@ -191,7 +193,9 @@ def zo_cache_attend(q, k_cache, v_cache, table, lengths, scale=None, out=None, l
 
 
 def _int32s(x):
-    return x if x is None or type(x) is np.ndarray and x.dtype == np.int32 else _whole(x, np.int32, "zo_cache_copy")
+    if x is None or type(x) is np.ndarray and x.dtype == np.int32 and x.flags.c_contiguous:
+        return x
+    return np.ascontiguousarray(_whole(x, np.int32, "zo_cache_copy"))
 
 
 def zo_cache_copy(k_caches, v_caches, src, dst, rows=None, stream=None):

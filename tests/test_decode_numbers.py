@@ -60,3 +60,18 @@ def test_counts_and_sequences_fit_32_bits():
     refused(book.table, [0.5])
     ids, lengths = book.table(np.array([a], np.int64))
     assert lengths.tolist() == [6] and book.table([])[0].shape == (0, 1)
+
+
+def test_host_arrays_may_be_strided():
+    """Columns of an array of moves, every other frequency: taken as numbers, whatever lies between them."""
+    moves = np.array([[1, 2, 4], [3, 5, 4]], np.int32)
+    zo.zo_cache_copy([], [], *moves.T)
+    zo.zo_cache_copy([], [], moves[::-1, 0], moves[::-1, 1])
+    from paper_2609_38095_amd import decode
+    turns = np.arange(8.0)
+    for view in (turns[::2], turns[::-1]):
+        got = decode._doubles(view)
+        assert np.array_equal(got, view) and got.flags.c_contiguous
+        memoryview(got).cast("B")  # as the binding reads it
+    assert decode._doubles(turns) is turns
+    assert all(decode._int32s(c).flags.c_contiguous and np.array_equal(decode._int32s(c), c) for c in moves.T)
