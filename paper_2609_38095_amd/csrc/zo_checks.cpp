@@ -41,6 +41,56 @@ bool distinct(Axis* axes, int count, int64_t run) {
   return true;
 }
 
+// Places of runs: `count` axes, largest stride first, none with a stride of 0, over runs of reach[count] bytes; reach[k] bytes
+// lie from an index of the axes from k on to the end of its last run.
+struct Places {
+  Axis axes[3];
+  int64_t reach[4];
+  int count = 0;
+
+  void add(int64_t stride, uint64_t n) {
+    if (n > 1 && stride > 0) axes[count++] = Axis{stride, n};
+  }
+  // false: strides so small beside what lies below them that meets() would have to look at many indices.
+  bool close(int64_t run) {
+    std::sort(axes, axes + count, [](const Axis& a, const Axis& b) { return a.stride > b.stride; });
+    reach[count] = run;
+    bool few = true;
+    for (int k = count - 1; k >= 0; --k) {
+      few = few && reach[k + 1] <= 2 * axes[k].stride;
+      reach[k] = reach[k + 1] + axes[k].stride * static_cast<int64_t>(axes[k].n - 1);
+    }
+    return few;
+  }
+  // Whether the bytes [x, x + size) meet a run, x counted from the first run's.
+  bool meets(int64_t x, int64_t size, int k = 0) const {
+    if (x >= reach[k] || x + size <= 0) return false;
+    if (k == count || (x <= 0 && x + size >= reach[k])) return true;
+    const int64_t stride = axes[k].stride, n = static_cast<int64_t>(axes[k].n);
+    int64_t i = x < reach[k + 1] ? 0 : (x - reach[k + 1]) / stride + 1;  // the first that ends behind x
+    for (; i < n && i * stride < x + size; ++i)
+      if (meets(x - i * stride, size, k + 1)) return true;
+    return false;
+  }
+};
+
+// Two tensors of the same strides (bytes; of an axis that one has a single entry of, the other's), the second `gap` bytes behind the
+// first: whether two of their runs meet, exact where the strides are nested.
+struct Both {
+  int64_t stride;
+  uint64_t n, m;
+};
+bool same_strides_meet(const Both* axes, int count, int64_t gap, int64_t run) {
+  Places steps;  // differences of two indices, as steps from the lowest
+  int64_t lowest = gap;
+  for (int i = 0; i < count; ++i) {
+    if (axes[i].n == 0 || axes[i].m == 0) return false;
+    lowest -= axes[i].stride * static_cast<int64_t>(axes[i].n - 1);
+    steps.add(axes[i].stride, axes[i].n + axes[i].m - 1);
+  }
+  return !steps.close(1) || steps.meets(1 - run - lowest, 2 * run - 1);
+}
+
 int check_rows(const zo_heads& h, uint32_t tokens, uint32_t heads, uint32_t dim, size_t elem, bool written) {
   if (h.data == nullptr) return ZO_ERR_NULL;
   if (!aligned(h.data, elem) || !axis_ok(h.token_stride, tokens) || !axis_ok(h.head_stride, heads)) return ZO_ERR_ARG;
@@ -123,12 +173,16 @@ bool rows_overlap(const zo_heads& a, uint32_t a_heads, const zo_heads& b, uint32
     return lo(h) + h.token_stride * (static_cast<int64_t>(tokens) - 1) * size + span(h, heads);
   };
   if (end(a, a_heads) <= lo(b) || end(b, b_heads) <= lo(a)) return false;
-  const int64_t pitch = a.token_stride * size;
-  if (tokens > 1 && a.token_stride == b.token_stride && pitch > 0 && span(a, a_heads) <= pitch && span(b, b_heads) <= pitch) {
+  const int64_t pitch = tokens > 1 ? a.token_stride * size : 0;  // (the stride of a single token is anything)
+  if (a.token_stride == b.token_stride && pitch > 0 && span(a, a_heads) <= pitch && span(b, b_heads) <= pitch) {
     const int64_t gap = (((lo(b) - lo(a)) % pitch) + pitch) % pitch;  // b's token behind a's
     if (gap >= span(a, a_heads) && gap + span(b, b_heads) <= pitch) return false;
   }
-  return true;
+  const bool same = (tokens <= 1 || a.token_stride == b.token_stride) && (a_heads <= 1 || b_heads <= 1 || a.head_stride == b.head_stride);
+  if (!same) return true;
+  const int64_t head = a_heads > 1 ? a.head_stride : b_heads > 1 ? b.head_stride : 0;
+  const Both axes[2] = {{pitch, tokens, tokens}, {head * size, a_heads, b_heads}};
+  return same_strides_meet(axes, 2, lo(b) - lo(a), dim * size);
 }
 
 int check_rotate(const zo_rotate& a, bool k_out) {

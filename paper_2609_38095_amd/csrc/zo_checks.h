@@ -20,8 +20,8 @@ int check_draw(const zo_draw_args& a);
 int check_draw_split(const zo_draw_args& a, const void* work, uint64_t work_bytes);
 int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype);
 
-// Whether two sets of rows may share an element. Exact for rows of one interleaved buffer (equal
-// token strides, a token's heads inside one stride), otherwise by the ranges that they span.
+// Whether two sets of rows may share an element. Exact for rows of one interleaved buffer: equal strides, each as large as
+// what lies below it, or equal token strides and the heads of each side together. Otherwise by the ranges that they span.
 bool rows_overlap(const zo_heads& a, uint32_t a_heads, const zo_heads& b, uint32_t b_heads, uint32_t tokens, uint32_t dim,
                   size_t elem);
 

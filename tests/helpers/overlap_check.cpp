@@ -1,0 +1,131 @@
+// Overlap rules of the decode-step operators' argument checks against element-by-element counts, under
+// AddressSanitizer and UBSan.
+
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <random>
+#include <set>
+#include <vector>
+
+#include "zo_checks.h"
+#include "zo_decode.h"
+
+#define REQUIRE(x)                                            \
+  do {                                                        \
+    if (!(x)) {                                               \
+      std::printf("line %d: %s\n", __LINE__, #x);             \
+      std::exit(1);                                           \
+    }                                                         \
+  } while (0)
+
+namespace {
+
+void* at(int64_t v) { return reinterpret_cast<void*>(static_cast<uintptr_t>(v)); }
+
+std::set<int64_t> elements(const zo_heads& h, uint32_t tokens, uint32_t heads, uint32_t dim) {
+  std::set<int64_t> all;
+  for (uint32_t t = 0; t < tokens; ++t)
+    for (uint32_t g = 0; g < heads; ++g)
+      for (uint32_t i = 0; i < dim; ++i)
+        all.insert(static_cast<int64_t>(reinterpret_cast<uintptr_t>(h.data)) / 2 + t * h.token_stride + g * h.head_stride + i);
+  return all;
+}
+
+bool meet(const std::set<int64_t>& a, const std::set<int64_t>& b) {
+  for (int64_t e : a)
+    if (b.count(e)) return true;
+  return false;
+}
+
+// Random rows: an overlap is never missed, and none is claimed where two sets have nested strides in common.
+void rows() {
+  std::mt19937 rng(1);
+  const auto below = [&](uint32_t n) { return static_cast<int64_t>(rng() % n); };
+  uint32_t exact = 0, apart = 0;
+  for (int turn = 0; turn < 60000; ++turn) {
+    const uint32_t tokens = 1 + rng() % 4, dim = 1 + rng() % 5, ha = 1 + rng() % 4, hb = 1 + rng() % 4;
+    const bool nested = rng() % 2;
+    zo_heads a{at(2 * (1000 + below(200))), below(60), below(60)}, b{at(2 * (1000 + below(200))), below(60), below(60)};
+    if (nested) {  // heads inside tokens or tokens inside heads, with room between
+      const int64_t most = ha > hb ? ha : hb, inner = dim + below(3 * dim);
+      if (rng() % 2) {
+        a.head_stride = inner;
+        a.token_stride = inner * (most - 1) + dim + below(20);
+      } else {
+        a.token_stride = inner;
+        a.head_stride = inner * (tokens - 1) + dim + below(20);
+      }
+      b.token_stride = a.token_stride;
+      b.head_stride = a.head_stride;
+      if (tokens == 1 && rng() % 2) b.token_stride = below(60);  // a stride that counts for nothing
+      if (hb == 1 && rng() % 2) b.head_stride = below(60);
+    }
+    const bool truth = meet(elements(a, tokens, ha, dim), elements(b, tokens, hb, dim));
+    const bool got = zo::rows_overlap(a, ha, b, hb, tokens, dim, 2);
+    REQUIRE(got || !truth);
+    REQUIRE(got == zo::rows_overlap(b, hb, a, ha, tokens, dim, 2));
+    if (nested) {
+      REQUIRE(got == truth);
+      ++exact;
+      apart += !truth;
+    }
+  }
+  REQUIRE(apart > exact / 10 && apart < exact);
+}
+
+// Queries and keys that alternate head by head, rotated in place.
+void alternating_heads() {
+  const double turns[2] = {0.1, 0.01};
+  zo_rotate a;
+  std::memset(&a, 0, sizeof a);
+  a.q = a.q_out = zo_heads{at(0x10000), 4 * 3 * 64, 3 * 64};
+  a.k = a.k_out = zo_heads{at(0x10000 + 2 * 64), 4 * 3 * 64, 3 * 64};
+  a.positions = static_cast<const int32_t*>(at(0x100));
+  a.turns = turns;
+  a.tokens = 100;
+  a.q_heads = a.k_heads = 4;
+  a.dim = 64;
+  a.rotary = 4;
+  a.magnitude = 1.0f;
+  a.dtype = ZO_BF16;
+  REQUIRE(zo::check_rotate(a, true) == ZO_OK);
+  a.k.data = a.k_out.data = at(0x10000 + 2 * 63);  // an element too early
+  REQUIRE(zo::check_rotate(a, true) == ZO_ERR_ARG);
+  // head-major, keys behind the queries of each token
+  a.q = a.q_out = zo_heads{at(0x10000), 2 * 64, 100 * 2 * 64};
+  a.k = a.k_out = zo_heads{at(0x10000 + 2 * 64), 2 * 64, 100 * 2 * 64};
+  REQUIRE(zo::check_rotate(a, true) == ZO_OK);
+  // one token, whose stride is anything
+  a.tokens = 1;
+  a.q.token_stride = a.k.token_stride = a.q_out.token_stride = a.k_out.token_stride = int64_t{1} << 62;
+  REQUIRE(zo::check_rotate(a, true) == ZO_OK);
+  a.q_heads = a.k_heads = 1;
+  a.q.head_stride = a.k.head_stride = a.q_out.head_stride = a.k_out.head_stride = int64_t{1} << 62;
+  REQUIRE(zo::check_rotate(a, true) == ZO_OK);
+  // as an attention's output beside its queries
+  zo_attend t;
+  std::memset(&t, 0, sizeof t);
+  t.q = zo_heads{at(0x10000), 8 * 2 * 64, 2 * 64};
+  t.out = zo_heads{at(0x10000 + 2 * 64), 8 * 2 * 64, 2 * 64};
+  t.cache = zo_cache{at(0x1000000), at(0x9000000), 8 * 16 * 64, 16 * 64, 64, 100, 8, 16, 64};
+  t.table = zo_page_table{static_cast<const int32_t*>(at(0x400)), 7, 3, 7};
+  t.lengths = static_cast<const int32_t*>(at(0x800));
+  t.work = at(0x100000);
+  t.work_bytes = zo_cache_attend_work(3, 8, 8, 64);
+  t.q_heads = 8;
+  t.scale = 0.125f;
+  t.dtype = ZO_BF16;
+  REQUIRE(zo::check_attend(t) == ZO_OK);
+  t.out.data = at(0x10000 + 2 * 65 + 2 * 64);
+  REQUIRE(zo::check_attend(t) == ZO_ERR_ARG);
+}
+
+}  // namespace
+
+int main() {
+  rows();
+  alternating_heads();
+  std::printf("overlap_check ok\n");
+  return 0;
+}
