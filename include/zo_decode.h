@@ -122,8 +122,8 @@ int zo_norm_rotate(const zo_rotate* a, void* stream);
  * seqs[token] (seqs NULL: token t belongs to sequence t). a.k_out is not used. A token with a
  * negative position, a sequence or position outside the table, or an absent page is not put. Tokens
  * of one call have distinct places. v: a.k_heads heads of the same dim. q_heads = 0 puts alone.
- * Errors: as zo_norm_rotate; ZO_ERR_ARG also where the cache's heads or dim are not the keys', or
- * its pages or page_tokens are 0.
+ * Errors: as zo_norm_rotate; ZO_ERR_ARG also where the cache's heads or dim are not the keys', its pages or
+ * page_tokens are 0, its keys and values share an element, or q, k, v or q_out lie in the memory that either spans.
  */
 typedef struct {
   zo_rotate a;

@@ -120,6 +120,27 @@ int check_cache(const zo_cache& c, size_t elem, bool written) {
   return ZO_OK;
 }
 
+int64_t address(const void* p) { return static_cast<int64_t>(reinterpret_cast<uintptr_t>(p)); }
+
+// Whether the keys and the values of a cache that is written (its strides are nested) share an element.
+bool sides_overlap(const zo_cache& c, size_t elem) {
+  const int64_t size = static_cast<int64_t>(elem);
+  const auto axis = [&](int64_t stride, uint32_t n) { return Both{n > 1 ? stride * size : 0, n, n}; };
+  const Both axes[3] = {axis(c.page_stride, c.pages), axis(c.head_stride, c.heads), axis(c.token_stride, c.page_tokens)};
+  return same_strides_meet(axes, 3, address(c.v) - address(c.k), c.dim * size);
+}
+
+// Whether rows and a cache may share an element, by the ranges that they span.
+bool cache_overlaps(const zo_cache& c, const zo_heads& h, uint32_t tokens, uint32_t heads, size_t elem) {
+  if (tokens == 0 || heads == 0) return false;
+  const auto span = [&](int64_t stride, uint32_t n) { return n > 1 ? stride * (static_cast<int64_t>(n) - 1) : 0; };
+  const int64_t size = static_cast<int64_t>(elem), lo = address(h.data);
+  const int64_t hi = lo + (span(h.token_stride, tokens) + span(h.head_stride, heads) + c.dim) * size;
+  const int64_t extent = (span(c.page_stride, c.pages) + span(c.head_stride, c.heads) + span(c.token_stride, c.page_tokens) + c.dim) * size;
+  const auto meets = [&](const void* side) { return lo < address(side) + extent && address(side) < hi; };
+  return meets(c.k) || meets(c.v);
+}
+
 int check_table(const zo_page_table& t) {
   if (t.seqs == 0 || t.width == 0) return ZO_OK;
   if (t.ids == nullptr) return ZO_ERR_NULL;
@@ -213,6 +234,11 @@ int check_put(const zo_rotate_put& p) {
   ZO_TRY(check_cache(p.cache, elem, true));
   if (p.cache.heads != p.a.k_heads || p.cache.dim != p.a.dim) return ZO_ERR_ARG;
   ZO_TRY(check_table(p.table));
+  // where the rows go is known on the device alone: nothing else of the call may lie in the cache
+  if (sides_overlap(p.cache, elem) || cache_overlaps(p.cache, p.a.q, p.a.tokens, p.a.q_heads, elem) ||
+      cache_overlaps(p.cache, p.a.q_out, p.a.tokens, p.a.q_heads, elem) || cache_overlaps(p.cache, p.a.k, p.a.tokens, p.a.k_heads, elem) ||
+      cache_overlaps(p.cache, p.v, p.a.tokens, p.a.k_heads, elem))
+    return ZO_ERR_ARG;
   return check_apart(p.a.q_out, p.a.q_heads, p.v, p.a.k_heads, false, p.a.tokens, p.a.dim, elem);
 }
 

@@ -121,11 +121,57 @@ void alternating_heads() {
   REQUIRE(zo::check_attend(t) == ZO_ERR_ARG);
 }
 
+// A put writes wherever the table says: nothing that it reads or writes besides may lie in the cache.
+void put() {
+  zo_rotate_put p;
+  std::memset(&p, 0, sizeof p);
+  p.a.q = p.a.q_out = zo_heads{at(0x10000), 6 * 64, 64};
+  p.a.k = zo_heads{at(0x40000), 2 * 64, 64};
+  p.v = zo_heads{at(0x50000), 2 * 64, 64};
+  p.a.positions = static_cast<const int32_t*>(at(0x100));
+  p.a.tokens = 10;
+  p.a.q_heads = 6;
+  p.a.k_heads = 2;
+  p.a.dim = 64;
+  p.a.magnitude = 1.0f;
+  p.a.dtype = ZO_BF16;
+  const int64_t page = 2 * 16 * 64, bytes = 2 * page;
+  p.cache = zo_cache{at(0x1000000), at(0x9000000), page, 16 * 64, 64, 100, 2, 16, 64};
+  p.table = zo_page_table{static_cast<const int32_t*>(at(0x400)), 7, 10, 7};
+  REQUIRE(zo::check_put(p) == ZO_OK);
+  const auto with = [&](auto change) {
+    zo_rotate_put b = p;
+    change(b);
+    return zo::check_put(b);
+  };
+  // keys and values of a page, a layer or a head beside each other; the same or shifted by a row or a page
+  REQUIRE(with([&](zo_rotate_put& b) { b.cache.v = at(0x1000000 + bytes); b.cache.page_stride = 2 * page; }) == ZO_OK);
+  REQUIRE(with([&](zo_rotate_put& b) { b.cache.v = at(0x1000000 + 100 * bytes); }) == ZO_OK);
+  REQUIRE(with([&](zo_rotate_put& b) {
+            b.cache = zo_cache{at(0x1000000), at(0x1000000 + 2 * 64), 2 * page, 2 * 64, 2 * 2 * 64, 100, 2, 16, 64};
+          }) == ZO_OK);
+  for (int64_t shift : {int64_t{0}, int64_t{2 * 64}, int64_t{2}, bytes, 99 * bytes, -bytes})
+    REQUIRE(with([&](zo_rotate_put& b) { b.cache.v = at(0x1000000 + shift); }) == ZO_ERR_ARG);
+  // tokens of the call in the cache
+  for (int64_t in : {int64_t{0x1000000}, 0x1000000 + 99 * bytes, int64_t{0x9000000}, 0x9000000 + 50 * bytes + 2}) {
+    REQUIRE(with([&](zo_rotate_put& b) { b.v.data = at(in); }) == ZO_ERR_ARG);
+    REQUIRE(with([&](zo_rotate_put& b) { b.a.k.data = at(in); }) == ZO_ERR_ARG);
+    REQUIRE(with([&](zo_rotate_put& b) { b.a.q.data = at(in); }) == ZO_ERR_ARG);
+    REQUIRE(with([&](zo_rotate_put& b) { b.a.q_out.data = at(in); }) == ZO_ERR_ARG);
+    REQUIRE(with([&](zo_rotate_put& b) { b.a.q_out.data = b.a.q.data = at(in); b.a.q_heads = 0; }) == ZO_OK);  // not touched
+  }
+  const int64_t rows = 10 * 2 * 64 * 2;
+  REQUIRE(with([&](zo_rotate_put& b) { b.v.data = at(0x1000000 - rows); }) == ZO_OK);
+  REQUIRE(with([&](zo_rotate_put& b) { b.v.data = at(0x1000000 - rows + 2); }) == ZO_ERR_ARG);
+  REQUIRE(with([&](zo_rotate_put& b) { b.v.data = at(0x1000000 + 100 * bytes); }) == ZO_OK);
+}
+
 }  // namespace
 
 int main() {
   rows();
   alternating_heads();
+  put();
   std::printf("overlap_check ok\n");
   return 0;
 }
