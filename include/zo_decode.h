@@ -172,7 +172,8 @@ int zo_norm_rotate_back(const zo_rotate_back* b, void* stream);
  * the values, and sums are fp32. A value that is infinite or NaN reaches the outputs of its own sequence and
  * dim, and makes them what the formula says as long as its weight is above 2^-90 of the largest.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (dtype, alignment, dim = 0 or above ZO_DIM_MAX, heads, pages or
- * page_tokens 0, too little work, 2^24 rows or more); ZO_ERR_NONFINITE (scale); ZO_ERR_HIP.
+ * page_tokens 0, an out that shares an element with q or lies in the memory that the keys or the values span,
+ * too little work, 2^24 rows or more); ZO_ERR_NONFINITE (scale); ZO_ERR_HIP.
  */
 typedef struct {
   zo_heads q, out;

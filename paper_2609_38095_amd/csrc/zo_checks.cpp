@@ -299,8 +299,9 @@ int check_attend(const zo_attend& a) {
   ZO_TRY(check_table(a.table));
   ZO_TRY(check_rows(a.q, a.table.seqs, a.q_heads, a.cache.dim, elem, false));
   ZO_TRY(check_rows(a.out, a.table.seqs, a.q_heads, a.cache.dim, elem, true));
-  // a worker writes a head's output while others still read their queries
+  // a worker writes a head's output while others still read their queries and the cache
   ZO_TRY(check_apart(a.out, a.q_heads, a.q, a.q_heads, false, a.table.seqs, a.cache.dim, elem));
+  if (cache_overlaps(a.cache, a.out, a.table.seqs, a.q_heads, elem)) return ZO_ERR_ARG;
   // tiles of 16 tokens are numbered below 2^52 (a token that no memory of its own holds may count many times)
   if (static_cast<uint64_t>(a.table.width) * a.cache.page_tokens / 16 >= (1ull << 52) / (static_cast<uint64_t>(a.table.seqs) * a.q_heads))
     return ZO_ERR_ARG;

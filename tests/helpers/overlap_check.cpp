@@ -166,9 +166,40 @@ void put() {
   REQUIRE(with([&](zo_rotate_put& b) { b.v.data = at(0x1000000 + 100 * bytes); }) == ZO_OK);
 }
 
+// An attention's output is written while other waves read the cache. Its queries may lie in it, and its keys may be its values.
+void attend() {
+  zo_attend t;
+  std::memset(&t, 0, sizeof t);
+  t.q = zo_heads{at(0x10000), 8 * 64, 64};
+  t.out = zo_heads{at(0x20000), 8 * 64, 64};
+  t.cache = zo_cache{at(0x1000000), at(0x9000000), 8 * 16 * 64, 16 * 64, 64, 100, 8, 16, 64};
+  t.table = zo_page_table{static_cast<const int32_t*>(at(0x400)), 7, 3, 7};
+  t.lengths = static_cast<const int32_t*>(at(0x800));
+  t.work = at(0x100000);
+  t.work_bytes = zo_cache_attend_work(3, 8, 8, 64);
+  t.q_heads = 8;
+  t.scale = 0.125f;
+  t.dtype = ZO_BF16;
+  REQUIRE(zo::check_attend(t) == ZO_OK);
+  const int64_t extent = 100 * 8 * 16 * 64 * 2, rows = 3 * 8 * 64 * 2;
+  for (int64_t side : {int64_t{0x1000000}, int64_t{0x9000000}}) {
+    for (int64_t in : {side, side + extent - 2, side + 2 - rows}) {
+      t.out.data = at(in);
+      REQUIRE(zo::check_attend(t) == ZO_ERR_ARG);
+    }
+    for (int64_t beside : {side + extent, side - rows}) {
+      t.out.data = at(beside);
+      REQUIRE(zo::check_attend(t) == ZO_OK);
+    }
+  }
+  t.q.data = t.cache.v = t.cache.k;
+  REQUIRE(zo::check_attend(t) == ZO_OK);
+}
+
 }  // namespace
 
 int main() {
+  attend();
   rows();
   alternating_heads();
   put();
