@@ -198,7 +198,8 @@ int zo_cache_attend(const zo_attend* a, void* stream);
  * arrays. All moves read what the pages held before the call: no dst is repeated or is the src of a
  * move.
  * Errors: ZO_ERR_NULL, ZO_ERR_ARG (dtype, alignment, a page or rows out of range, rows = 0, a
- * repeated dst, a dst that is a src, pages that overlap, pages of more than 2^23 elements), ZO_ERR_MEMORY,
+ * repeated dst, a dst that is a src, pages that overlap, two different tensors that do, pages of more than 2^23
+ * elements), ZO_ERR_MEMORY,
  * ZO_ERR_HIP (earlier batches may already be enqueued).
  */
 typedef struct {

@@ -130,6 +130,31 @@ bool sides_overlap(const zo_cache& c, size_t elem) {
   return same_strides_meet(axes, 3, address(c.v) - address(c.k), c.dim * size);
 }
 
+// Whether two tensors of a list, all of the (nested) shape of `c`, share elements. The same tensor twice does not count: its moves
+// are the same. Sorted by address; layers one behind another, or side by side inside a page's stride, need no pairs.
+bool tensors_overlap(const zo_cache& c, void* const* tensors, uint32_t n, size_t elem) {
+  const int64_t size = static_cast<int64_t>(elem), run = c.dim * size;
+  Places all;
+  const auto stride = [&](int64_t s, uint32_t count) { return count > 1 ? s * size : 0; };
+  const Both axes[3] = {{stride(c.page_stride, c.pages), c.pages, c.pages},
+                        {stride(c.head_stride, c.heads), c.heads, c.heads},
+                        {stride(c.token_stride, c.page_tokens), c.page_tokens, c.page_tokens}};
+  for (const Both& a : axes) all.add(a.stride, a.n);
+  all.close(run);
+  std::vector<int64_t> at(n);
+  for (uint32_t i = 0; i < n; ++i) at[i] = address(tensors[i]);
+  std::sort(at.begin(), at.end());
+  at.erase(std::unique(at.begin(), at.end()), at.end());
+  int64_t least = all.reach[0];
+  for (size_t i = 1; i < at.size(); ++i) least = std::min(least, at[i] - at[i - 1]);
+  if (least >= all.reach[0]) return false;
+  if (all.count > 0 && least >= all.reach[1] && at.back() - at.front() + all.reach[1] <= all.axes[0].stride) return false;
+  for (size_t i = 0; i < at.size(); ++i)
+    for (size_t j = i + 1; j < at.size() && at[j] < at[i] + all.reach[0]; ++j)
+      if (same_strides_meet(axes, 3, at[j] - at[i], run)) return true;
+  return false;
+}
+
 // Whether rows and a cache may share an element, by the ranges that they span.
 bool cache_overlaps(const zo_cache& c, const zo_heads& h, uint32_t tokens, uint32_t heads, size_t elem) {
   if (tokens == 0 || heads == 0) return false;
@@ -345,6 +370,7 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
     if (!aligned(tensors[i], elem)) return ZO_ERR_ARG;
   }
   try {
+    if (tensors_overlap(first, tensors, n_tensors, elem)) return ZO_ERR_ARG;
     // bit 0: a destination, bit 1: a source
     std::vector<unsigned char> seen(first.pages, 0);
     for (uint32_t i = 0; i < n_moves; ++i) {

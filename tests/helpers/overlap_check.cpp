@@ -1,6 +1,7 @@
 // Overlap rules of the decode-step operators' argument checks against element-by-element counts, under
 // AddressSanitizer and UBSan.
 
+#include <algorithm>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -196,9 +197,74 @@ void attend() {
   REQUIRE(zo::check_attend(t) == ZO_OK);
 }
 
+std::set<int64_t> elements(const zo_cache& c, int64_t from) {
+  std::set<int64_t> all;
+  for (uint32_t p = 0; p < c.pages; ++p)
+    for (uint32_t h = 0; h < c.heads; ++h)
+      for (uint32_t t = 0; t < c.page_tokens; ++t)
+        for (uint32_t i = 0; i < c.dim; ++i) all.insert(from / 2 + p * c.page_stride + h * c.head_stride + t * c.token_stride + i);
+  return all;
+}
+
+// Caches of a copy share nothing, whatever their order; the same one may be given twice.
+void copy() {
+  const zo_page_move move{0, 1, 1};
+  const auto check = [&](const zo_cache& shape, std::vector<int64_t> from) {
+    std::vector<void*> tensors;
+    for (int64_t f : from) tensors.push_back(at(f));
+    return zo::check_copy(&shape, tensors.data(), static_cast<uint32_t>(tensors.size()), &move, 1, ZO_BF16);
+  };
+  const int64_t head = 16 * 64, page = 8 * head;
+  const zo_cache whole{nullptr, nullptr, page, head, 64, 10, 8, 16, 64};
+  std::vector<int64_t> layers, inside, pairs;
+  zo_cache side = whole, both = whole;
+  side.page_stride = 56 * page;
+  both.page_stride = 2 * page;
+  for (int i = 0; i < 56; ++i) {
+    layers.push_back(0x100000 + (55 - i) * 2 * 10 * page);            // [layers, 2, pages, ..], the last first
+    inside.push_back(0x100000 + i * 2 * page);                        // [pages, layers, 2, ..]
+    pairs.push_back(0x100000 + i / 2 * 2 * 20 * page + i % 2 * 2 * page);  // [layers, pages, 2, ..]
+  }
+  REQUIRE(check(whole, layers) == ZO_OK && check(side, inside) == ZO_OK && check(both, pairs) == ZO_OK);
+  for (auto* list : {&layers, &inside, &pairs}) {
+    list->push_back((*list)[3]);  // twice the same
+    const zo_cache& shape = list == &layers ? whole : list == &inside ? side : both;
+    REQUIRE(check(shape, *list) == ZO_OK);
+    list->back() += 2 * 64;       // a token further
+    REQUIRE(check(shape, *list) == ZO_ERR_ARG);
+  }
+  // random shapes and places
+  std::mt19937 rng(2);
+  const auto below = [&](uint32_t n) { return static_cast<int64_t>(rng() % n); };
+  uint32_t meets = 0, apart = 0;
+  for (int turn = 0; turn < 20000; ++turn) {
+    zo_cache c{nullptr, nullptr, 0, 0, 0, static_cast<uint32_t>(2 + below(3)), static_cast<uint32_t>(1 + below(3)),
+               static_cast<uint32_t>(1 + below(3)), static_cast<uint32_t>(1 + below(3))};
+    struct {
+      int64_t* stride;
+      uint32_t n;
+    } order[3] = {{&c.page_stride, c.pages}, {&c.head_stride, c.heads}, {&c.token_stride, c.page_tokens}};
+    std::shuffle(order, order + 3, rng);
+    int64_t extent = c.dim;
+    for (auto& o : order) {
+      *o.stride = extent * (1 + below(3)) + below(3);
+      extent += *o.stride * (static_cast<int64_t>(o.n) - 1);
+    }
+    std::vector<int64_t> from;
+    for (int i = 0, n = 1 + static_cast<int>(below(4)); i < n; ++i) from.push_back(2 * (1000 + below(static_cast<uint32_t>(2 * extent))));
+    bool truth = false;
+    for (size_t i = 0; i < from.size(); ++i)
+      for (size_t j = 0; j < i; ++j) truth = truth || (from[i] != from[j] && meet(elements(c, from[i]), elements(c, from[j])));
+    REQUIRE(check(c, from) == (truth ? ZO_ERR_ARG : ZO_OK));
+    ++(truth ? meets : apart);
+  }
+  REQUIRE(meets > 2000 && apart > 2000);
+}
+
 }  // namespace
 
 int main() {
+  copy();
   attend();
   rows();
   alternating_heads();
