@@ -155,6 +155,25 @@ bool tensors_overlap(const zo_cache& c, void* const* tensors, uint32_t n, size_t
   return false;
 }
 
+// Whether no dst of the moves is repeated or a src. A byte for each page, or, where a cache has very many for each move, the
+// sorted dsts: 32 moves in 2^20 pages 1 us (a byte for each page 22), 1,024 moves in 65,536 pages 52 us (a byte for each 4).
+bool moves_apart(const zo_page_move* moves, uint32_t n, uint32_t pages) {
+  if (pages / 2048 <= n) {
+    std::vector<unsigned char> seen(pages, 0);  // bit 0: a destination, bit 1: a source
+    for (uint32_t i = 0; i < n; ++i) {
+      if (seen[moves[i].dst] != 0 || (seen[moves[i].src] & 1) != 0 || moves[i].src == moves[i].dst) return false;
+      seen[moves[i].dst] |= 1;
+      seen[moves[i].src] |= 2;
+    }
+    return true;
+  }
+  std::vector<int32_t> to(n);
+  for (uint32_t i = 0; i < n; ++i) to[i] = moves[i].dst;
+  std::sort(to.begin(), to.end());
+  if (std::adjacent_find(to.begin(), to.end()) != to.end()) return false;
+  return std::none_of(moves, moves + n, [&](const zo_page_move& m) { return std::binary_search(to.begin(), to.end(), m.src); });
+}
+
 // Whether rows and a cache may share an element, by the ranges that they span.
 bool cache_overlaps(const zo_cache& c, const zo_heads& h, uint32_t tokens, uint32_t heads, size_t elem) {
   if (tokens == 0 || heads == 0) return false;
@@ -371,21 +390,16 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
   }
   try {
     if (tensors_overlap(first, tensors, n_tensors, elem)) return ZO_ERR_ARG;
-    // bit 0: a destination, bit 1: a source
-    std::vector<unsigned char> seen(first.pages, 0);
     for (uint32_t i = 0; i < n_moves; ++i) {
       const zo_page_move& m = moves[i];
       if (m.src < 0 || m.dst < 0 || static_cast<uint32_t>(m.src) >= first.pages || static_cast<uint32_t>(m.dst) >= first.pages)
         return ZO_ERR_ARG;
       if (m.rows <= 0 || static_cast<uint32_t>(m.rows) > first.page_tokens) return ZO_ERR_ARG;
-      if (seen[m.dst] != 0 || (seen[m.src] & 1) != 0 || m.src == m.dst) return ZO_ERR_ARG;
-      seen[m.dst] |= 1;
-      seen[m.src] |= 2;
     }
+    return moves_apart(moves, n_moves, first.pages) ? ZO_OK : ZO_ERR_ARG;
   } catch (const std::bad_alloc&) {
     return ZO_ERR_MEMORY;
   }
-  return ZO_OK;
 }
 
 }  // namespace zo

@@ -5,6 +5,7 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
+#include <new>
 #include <random>
 #include <set>
 #include <vector>
@@ -261,9 +262,43 @@ void copy() {
   REQUIRE(meets > 2000 && apart > 2000);
 }
 
+// The largest block asked for since it was set to 0.
+size_t largest_block = 0;
+
+// A copy's checks take memory by its moves, not by the pages of the cache, and find what is wrong with them all the same.
+void moves() {
+  std::mt19937 rng(3);
+  const auto check = [](uint32_t pages, const std::vector<zo_page_move>& list) {
+    const zo_cache shape{nullptr, nullptr, 64, 64, 8, pages, 1, 8, 8};
+    void* tensors[2] = {at(0x100000), at(int64_t{1} << 44)};
+    return zo::check_copy(&shape, tensors, 2, list.data(), static_cast<uint32_t>(list.size()), ZO_F32);
+  };
+  largest_block = 0;
+  REQUIRE(check(0x7FFFFFFF, {{0, 0x7FFFFFFE, 8}, {0, 5, 1}}) == ZO_OK && largest_block < 4096);
+  for (int turn = 0; turn < 3000; ++turn) {
+    const uint32_t pages = turn % 3 ? 20 + rng() % 20 : 50000, n = 1 + rng() % 8, ids = pages < 50000 ? pages : 20;
+    std::vector<zo_page_move> list;
+    for (uint32_t i = 0; i < n; ++i)
+      list.push_back({static_cast<int32_t>((pages - ids) + rng() % ids), static_cast<int32_t>((pages - ids) + rng() % ids), 1});
+    bool good = true;
+    for (const auto& a : list)
+      for (const auto& b : list) good = good && a.dst != b.src && (&a == &b || a.dst != b.dst);
+    REQUIRE(check(pages, list) == (good ? ZO_OK : ZO_ERR_ARG));
+  }
+}
+
 }  // namespace
 
+void* operator new(size_t size) {
+  largest_block = std::max(largest_block, size);
+  if (void* p = std::malloc(size)) return p;
+  throw std::bad_alloc();
+}
+void operator delete(void* p) noexcept { std::free(p); }
+void operator delete(void* p, size_t) noexcept { std::free(p); }
+
 int main() {
+  moves();
   copy();
   attend();
   rows();
