@@ -294,6 +294,8 @@ uint32_t back_blocks(uint32_t tokens, uint32_t heads) {
 int check_back(const zo_rotate_back& b) {
   const zo_rotate& a = b.a;
   ZO_TRY(check_common(a));
+  // gamma gradients of a side without rows are written too: zeros
+  if ((a.q_gamma && !aligned(b.dq_gamma, 4)) || (a.k_gamma && !aligned(b.dk_gamma, 4))) return ZO_ERR_ARG;
   if (a.tokens == 0) return ZO_OK;
   const size_t elem = elem_bytes(a.dtype);
   const auto side = [&](const zo_heads& x, const zo_heads& dy, const zo_heads& dx, uint32_t heads, const void* gamma,
@@ -305,8 +307,7 @@ int check_back(const zo_rotate_back& b) {
     if (gamma == nullptr) return ZO_OK;
     ZO_TRY(check_rows(x, a.tokens, heads, a.dim, elem, false));
     ZO_TRY(check_apart(dx, heads, x, heads, true, a.tokens, a.dim, elem));
-    if (dgamma == nullptr || b.work == nullptr) return ZO_ERR_NULL;
-    return aligned(dgamma, 4) ? ZO_OK : ZO_ERR_ARG;
+    return dgamma == nullptr || b.work == nullptr ? ZO_ERR_NULL : ZO_OK;
   };
   ZO_TRY(side(a.q, a.q_out, b.dq, a.q_heads, a.q_gamma, b.dq_gamma));
   ZO_TRY(side(a.k, a.k_out, b.dk, a.k_heads, a.k_gamma, b.dk_gamma));

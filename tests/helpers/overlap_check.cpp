@@ -1,5 +1,5 @@
-// Overlap rules of the decode-step operators' argument checks against element-by-element counts, under
-// AddressSanitizer and UBSan.
+// Argument checks of the decode-step operators, under AddressSanitizer and UBSan: overlap rules against element-by-element
+// counts, the memory that checks take, the addresses of outputs that have no rows.
 
 #include <algorithm>
 #include <cstdio>
@@ -262,6 +262,27 @@ void copy() {
   REQUIRE(meets > 2000 && apart > 2000);
 }
 
+// Gamma gradients are written for a side without rows as well, and their addresses are checked there too.
+void gradients_of_nothing() {
+  zo_rotate_back b;
+  std::memset(&b, 0, sizeof b);
+  b.a.q_gamma = b.a.k_gamma = at(0x100);
+  b.a.positions = static_cast<const int32_t*>(at(0x100));
+  b.a.dim = 64;
+  b.a.q_heads = 4;
+  b.a.dtype = ZO_BF16;
+  b.dq_gamma = static_cast<float*>(at(0x1000));
+  b.dk_gamma = static_cast<float*>(at(0x2000));
+  REQUIRE(zo::check_back(b) == ZO_OK);
+  b.dq_gamma = static_cast<float*>(at(0x1002));
+  REQUIRE(zo::check_back(b) == ZO_ERR_ARG);
+  b.dq_gamma = static_cast<float*>(at(0x1000));
+  b.dk_gamma = static_cast<float*>(at(0x2002));
+  REQUIRE(zo::check_back(b) == ZO_ERR_ARG);
+  b.a.k_gamma = nullptr;  // not written then
+  REQUIRE(zo::check_back(b) == ZO_OK);
+}
+
 // The largest block asked for since it was set to 0.
 size_t largest_block = 0;
 
@@ -298,6 +319,7 @@ void operator delete(void* p) noexcept { std::free(p); }
 void operator delete(void* p, size_t) noexcept { std::free(p); }
 
 int main() {
+  gradients_of_nothing();
   moves();
   copy();
   attend();
