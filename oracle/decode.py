@@ -90,18 +90,19 @@ def attend(q, k_cache, v_cache, table, lengths, scale):
     return out, lse, mag, big
 
 
-def draw(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
-    """(token, log probability) of one row of logits (float32 values), in whole numbers of any size."""
-    l = np.where(np.isnan(logits), -np.inf, logits.astype(np.float64))
+def draw(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, most=float(np.finfo(np.float32).max)):
+    """(token, log probability) of one row of logits (float32 values), in whole numbers of any size. most: the largest finite
+    number of the logits' type, which +inf counts as."""
+    l = np.minimum(np.where(np.isnan(logits), -np.inf, logits.astype(np.float64)), most)
     top = l.max()
     if top == -np.inf:
         return -1, -math.inf
     if not temperature > 0:
         return int(np.argmax(l)), 0.0
-    if top == np.inf:
-        w = [ONE if v == np.inf else 0 for v in l]
-    else:
-        w = np.rint(np.exp((l - top) * (1.0 / float(np.float32(temperature)))) * ONE).astype(np.int64).tolist()
+    live = l > -np.inf  # whatever the temperature
+    w = np.zeros(len(l), np.int64)
+    w[live] = np.rint(np.exp((l[live] - top) * (1.0 / float(np.float32(temperature)))) * ONE).astype(np.int64)
+    w = w.tolist()
     order = np.argsort(-l, kind="stable").tolist()
     if top_k > 0:
         order = order[:top_k]
