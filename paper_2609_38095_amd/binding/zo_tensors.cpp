@@ -124,12 +124,20 @@ uint32_t count_of(int64_t n, const char* name) {
   return static_cast<uint32_t>(n);
 }
 
+// The same sizes, and the same strides wherever there is more than one entry.
+bool same_layout(const at::Tensor& a, const at::Tensor& b) {
+  if (a.sizes() != b.sizes()) return false;
+  for (int64_t i = 0; i < a.dim(); ++i)
+    if (a.size(i) > 1 && a.stride(i) != b.stride(i)) return false;
+  return true;
+}
+
 zo_cache cache_of(const at::Tensor* k, const at::Tensor* v, at::ScalarType type) {
   if (k == nullptr || v == nullptr) refuse(PyExc_TypeError, "k_cache and v_cache are needed");
   check_type(*k, "k_cache", type);
   check_type(*v, "v_cache", type);
   if (k->dim() != 4) refuse(PyExc_ValueError, "k_cache must be [pages, heads, page_tokens, dim]");
-  if (v->sizes() != k->sizes() || v->strides() != k->strides())
+  if (!same_layout(*k, *v))
     refuse(PyExc_ValueError, "k_cache and v_cache must have the same shape and strides");
   if (k->stride(3) != 1 && k->size(3) > 1) refuse(PyExc_ValueError, "the last dimension of the cache must be contiguous");
   return zo_cache{k->data_ptr(), v->data_ptr(), k->stride(0), k->stride(1), k->stride(2), count_of(k->size(0), "k_cache"),
@@ -388,7 +396,7 @@ PyObject* cache_copy(PyObject* const* args, Py_ssize_t n) {
         dtype = type_of(*t, "each cache");
         shape = cache_of(t, t, t->scalar_type());
       }
-      if (t == nullptr || t->scalar_type() != first->scalar_type() || t->sizes() != first->sizes() || t->strides() != first->strides())
+      if (t == nullptr || t->scalar_type() != first->scalar_type() || !same_layout(*t, *first))
         refuse(PyExc_ValueError, "each cache must have the type, shape and strides of the first");
       tensors.push_back(t->data_ptr());
     }
