@@ -538,6 +538,8 @@ __device__ bool cut_by_value(Lds& s, const uint16_t* row, uint32_t vocab, const 
   if (threadIdx.x == 0) s.small_weight = 0;
   __syncthreads();
   if (cuts) {
+    // the bin of small values; where it would be `bins`, they weigh nothing, and `bins` is that of all that does not count
+    const uint32_t small_bin = static_cast<uint32_t>(code_top) < bins ? static_cast<uint32_t>(code_top) : ~0u;
     walk<BF16, 4>(row, vocab, [&](uint32_t, const Eight<BF16>& x) {
       uint32_t small = 0;
 #pragma unroll
@@ -545,7 +547,7 @@ __device__ bool cut_by_value(Lds& s, const uint16_t* row, uint32_t vocab, const 
         const u16x2 bin = bins_of(x.v[0][c], code_top, bins);
         atomicAdd(&s.bin_count[bin.x], 1u);  // (`bins` is a bin of what does not count)
         atomicAdd(&s.bin_count[bin.y], 1u);
-        small |= (bin.x == code_top ? 1u << 2 * c : 0u) | (bin.y == code_top ? 2u << 2 * c : 0u);
+        small |= (bin.x == small_bin ? 1u << 2 * c : 0u) | (bin.y == small_bin ? 2u << 2 * c : 0u);
       }
       if (small) {
         float l[8];

@@ -43,3 +43,20 @@ def test_the_largest_numbers(vocab, ends, dtype):
             want, lp = oracle.draw(x[b].float().numpy(), ui, ti, ki if with_k else 0, pi, mi, most=most)
             assert int(one[0][b]) == want, (b, SETTINGS[b], with_k)
             assert float(one[1][b]) == lp or abs(float(one[1][b]) - lp) <= 4 * E * max(1.0, abs(lp)), (b, SETTINGS[b], with_k)
+
+
+@pytest.mark.parametrize("top_p", [0.5, 0.95])
+def test_weights_that_end_near_zero(top_p):
+    """bf16 rows whose weights end at logits around 0: among those below 2^-10, in front of them and behind them."""
+    low = [0.0, 5e-4, 2.0 ** -10, 0.00098, 2.0 ** -10 * (1 + 2.0 ** -7), 0.002, -0.00098, -0.002]
+    t = torch.tensor([(16 - v) / 32 for v in low], device="cuda")  # 32 temperatures below the largest
+    x = torch.randn(len(low), 9000, generator=torch.Generator().manual_seed(1)).mul_(4).clamp_(max=15.5)
+    x[:, ::5] *= 2.0 ** -12
+    x[:, ::7] = 0.0
+    x[:, 77] = 16.0
+    x = x.bfloat16()
+    u = torch.linspace(0.05, 0.999, len(low), device="cuda")
+    token, lp = zo.zo_draw(x.cuda(), u, t, top_p=torch.full((len(low),), top_p, device="cuda"), logprobs=True)
+    for b in range(len(low)):
+        want, exact = oracle.draw(x[b].float().numpy(), float(u[b]), float(t[b]), 0, top_p, most=torch.finfo(torch.bfloat16).max)
+        assert int(token[b]) == want and abs(float(lp[b]) - exact) <= 4 * E * max(1.0, abs(exact)), (b, low[b])
