@@ -25,9 +25,9 @@
 //     the lane); output row r of product e is then dim r D/16 + e.
 // Nothing passes through LDS. fp32 takes the fp32 matrix instructions: its products are exact to fp32.
 //
-// Bound by HBM: the keys and values of the live tokens, once. Measured, join included: 1.69 GB in 266 us
-// (6.3 TB/s; a plain read of 4 GiB reaches 7.0), 0.56 GB of 48 ragged sequences in 102 us, of which about 6
-// pass before the first tile and 4 to 5 in the join. One short sequence: 11 us.
+// Bound by HBM: the keys and values of the live tokens, once. Measured by the device's clock: 1.89 GB of 4 long
+// sequences in 286 us and 5 for the join (6.5 TB/s; a plain read of 4 GiB reaches 7.0), 0.53 GB of 48 ragged ones in
+// 96 us and 5. One short sequence: 11 us a call.
 
 #include <algorithm>
 #include <cmath>

@@ -420,11 +420,12 @@ uint64_t zo_cache_attend_work(uint32_t seqs, uint32_t q_heads, uint32_t heads, u
   return zo::attend_items_bytes(seqs, q_heads, heads) + 2ull * zo::attend_workers(dim) * group * row * sizeof(float);
 }
 
-// Rows are split where that is sooner. us for fp32 (bf16) rows, one workgroup each | split: with top-p alone 16,384
+// Rows are split from about where that is sooner. us for fp32 (bf16) rows, one workgroup each | split: with top-p alone 16,384
 // logits 27 (25) | 27, 32,000 38 (33) | 28, 151,936 108 (75) | 33 for 4 rows, 43 for 16 and 57 for 32; without settings
 // 14 (17) | 12 and 56 (48) | 13 for 4 rows, 21 for 32. A top-k that counts ends early in one workgroup: 16,384 logits
-// 17 | 24, 151,936 25 | 23 for 4 rows, 28 for 16 and 36 for 32. Rows whose top_k is 0 are as above and may lie in the
-// same batch, so one with a top_k is split from where its other rows lose no more than a few us.
+// 17 | 24, 151,936 25 | 23 for 4 rows, 28 for 16 and 36 for 32. What each row's top_k is lies on the device: rows whose
+// top_k is 0 are as without one (108 us in one workgroup), so a call with a top_k is split as long as the rows that it
+// counts for lose no more than 3 us by it (16 of them 25 | 28).
 uint64_t zo_draw_work(uint32_t rows, uint32_t vocab, int top_k) {
   const uint32_t most_rows = top_k ? 16 : 32, least_vocab = top_k ? 1u << 16 : 4 * zo::kDrawPart;
   if (rows > most_rows || vocab < least_vocab || vocab > (1u << 18)) return 0;

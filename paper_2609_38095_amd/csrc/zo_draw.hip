@@ -18,11 +18,12 @@
 // The drawn token is then found in index order: weights of runs of 512 tokens, their running sums, and
 // the tokens of the run that holds the drawn share.
 //
-// The row is read from HBM once; later passes find it in the L2 (608 KB at 152 k fp32 logits). Bound by
-// the fp64 exponentials of one CU where every token's weight is needed, else by its reads. Measured, of
-// 151,936 logits: 256 bf16 rows with top-p 0.95 and min-p in 95 us (read 12, counts 25, runs 23, the rest
-// cuts and the slowest row), one fp32 row in 25 us with top-k 50 and in 108 with top-p 0.95 alone. Few
-// long rows are therefore split over workgroups where the caller gives a workspace: 33 us.
+// The row is read from HBM once; later passes read it from the Infinity Cache (of 256 bf16 rows of 304 KB a die has
+// 32 at once, and 4 MB of L2: 3.7 times the rows' bytes behind the L2s). A row is one workgroup's chain of passes with
+// barriers between; at 256 rows no unit is full (VALU 0.45 busy, LDS 0.17, CUs 0.72: the slowest row ends last).
+// Measured, of 151,936 logits: 256 bf16 rows with top-p 0.95 and min-p in 95 to 107 us by the rows, one fp32
+// row in 25 us with top-k 50 and in 108 with top-p 0.95 alone. Few long rows are therefore split over workgroups
+// where the caller gives a workspace: 33 us.
 
 #include <cmath>
 #include <type_traits>
@@ -44,7 +45,6 @@ constexpr uint32_t kSteps = 1024;               // of the exponential's table, f
 constexpr uint32_t kBins = 8192;                // values of a bf16 row that are weighed once each, at most
 constexpr uint32_t kSmall = 0x3A7F;             // bf16 below 2^-10 (of which there are very many values) share a bin
 constexpr uint32_t kRanges = 2888;              // of 16 steps, down to the smallest weight (45 halvings)
-
 
 // A logit as it counts: NaN as -inf, +inf as the largest finite number of its type. The median of three of which one is a NaN is
 // the smallest; the instruction itself, since the compiler takes the median with -inf for a minimum, NaN or not.
@@ -409,8 +409,8 @@ __device__ __forceinline__ uint32_t cut_list(Lds& s, uint32_t n, const Weigh& we
 // The cut at which the count reaches `most`, or (by_weight) the weight reaches `need`, whichever is
 // asked for; false: the row's weights end before. Tokens of no weight do not count.
 // kSplit: the kernel that calls it. A function of its own for each lets the compiler see where its arguments come
-// from; shared by two kernels, `weigh` and `cut` are kept in memory and read from there for each token (fp32 rows without
-// settings: 77 -> 141 us).
+// from; shared by two kernels, `weigh` and `cut` are kept in memory and read from there for each token, and passes over
+// all tokens took almost twice as long.
 template <class S, bool kSplit>
 __device__ __attribute__((noinline)) bool find_cut(Lds& s, const typename S::storage* row, uint32_t vocab, const Weigh& weigh, uint32_t top,
                                                    bool by_weight, uint64_t need, Cut& cut) {
@@ -1182,31 +1182,32 @@ __global__ void __launch_bounds__(kThreads) draw_kernel(const Draw a, uint64_t* 
       const uint64_t all = wave_sum(sum);
       if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
     });
-  } else
-  walk<S, 2>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
-    uint32_t in = 0;
+  } else {
+    walk<S, 2>(row, vocab, [&](uint32_t i0, const float(&l)[8]) {
+      uint32_t in = 0;
 #pragma unroll
-    for (uint32_t e = 0; e < 8; ++e) in |= cut.keeps(key_of(l[e]), i0 + e) ? 1u << e : 0u;
-    uint64_t sum = 0;
-    if (__any(__popc(in) > 4)) {
+      for (uint32_t e = 0; e < 8; ++e) in |= cut.keeps(key_of(l[e]), i0 + e) ? 1u << e : 0u;
+      uint64_t sum = 0;
+      if (__any(__popc(in) > 4)) {
 #pragma unroll
-      for (uint32_t e = 0; e < 8; ++e) {
-        const uint64_t w = weigh(l[e]);
-        sum += (in >> e & 1) && w >= least ? w : 0;
+        for (uint32_t e = 0; e < 8; ++e) {
+          const uint64_t w = weigh(l[e]);
+          sum += (in >> e & 1) && w >= least ? w : 0;
+        }
+      } else {  // few of the eight in any lane: those in a row of their own first
+        uint32_t kept = 0;
+#pragma unroll
+        for (uint32_t e = 0; e < 8; ++e)
+          if (in >> e & 1) s.kept[kept++ * kThreads + threadIdx.x] = l[e];
+        for (uint32_t j = 0; __any(j < kept); ++j) {
+          const uint64_t w = weigh(j < kept ? s.kept[j * kThreads + threadIdx.x] : -INFINITY);
+          sum += w >= least ? w : 0;
+        }
       }
-    } else {  // few of the eight in any lane: those in a row of their own first
-      uint32_t kept = 0;
-#pragma unroll
-      for (uint32_t e = 0; e < 8; ++e)
-        if (in >> e & 1) s.kept[kept++ * kThreads + threadIdx.x] = l[e];
-      for (uint32_t j = 0; __any(j < kept); ++j) {
-        const uint64_t w = weigh(j < kept ? s.kept[j * kThreads + threadIdx.x] : -INFINITY);
-        sum += w >= least ? w : 0;
-      }
-    }
-    const uint64_t all = wave_sum(sum);
-    if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
-  });
+      const uint64_t all = wave_sum(sum);
+      if (threadIdx.x % 64 == 0) s.run_weight[i0 / kRun] = all;
+    });
+  }
   __syncthreads();
   draw_from_runs<S>(s, a, b, row, weigh, asked, cut);
 }

@@ -13,9 +13,9 @@
 // is then a sum over L lanes by data-parallel moves, and nothing of a row passes through LDS.
 // Sizes that vectors do not divide take the same code with one element for a vector.
 //
-// Bound by HBM: one read and one write of each row. 16,387 fp32 tokens of 64 heads of 64 take 95 us
-// (5.6 TB/s), the gradient of 8,192 bf16 tokens of 32 + 8 heads of 128 53 us and 4.6 for the gammas' sum,
-// eight tokens 5 us.
+// Bound by HBM: one read and one write of each row. 16,387 fp32 tokens of 64 heads of 64 take 94 us
+// (5.7 TB/s), eight tokens 5 us. The gradient of 8,192 bf16 tokens of 32 + 8 heads of 128 takes 52 us (4.8 TB/s)
+// and 4.5 for the gammas' sum: both sides have 512 workgroups, so the keys' end after a quarter of the queries' walk.
 
 #include <algorithm>
 #include <cstring>

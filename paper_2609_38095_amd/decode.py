@@ -17,7 +17,8 @@ Rows of heads are tensors [tokens, heads, dim], caches [pages, heads, page_token
 the last dimension contiguous: permute a cache that is laid out otherwise). Results are allocated by
 torch where no output is given. All tensors of a call live on the current device; a call with a
 stream of its own allocates on that stream, and waiting for tensors that other streams still write
-is the caller's.
+is the caller's. torch's autograd sees none of these calls: results carry no gradient, whatever their
+inputs require, and zo_norm_rotate_back is called by the program.
 """
 
 import contextlib
@@ -36,8 +37,8 @@ ZO_ROTARY_LINEAR, ZO_ROTARY_BASE, ZO_ROTARY_BANDS = 0, 1, 2
 
 EXPORTS = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back",
            "zo_norm_rotate_back_work", "zo_cache_attend", "zo_cache_attend_work", "zo_cache_copy", "zo_draw",
-           "zo_draw_split", "zo_draw_work", "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork", "zo_pages_extend", "zo_pages_drop",
-           "zo_pages_left", "zo_pages_length", "zo_pages_table", "zo_pages_compact")
+           "zo_draw_split", "zo_draw_work", "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork",
+           "zo_pages_extend", "zo_pages_drop", "zo_pages_left", "zo_pages_length", "zo_pages_table", "zo_pages_compact")
 # entry points that _tensors.so calls, in the order that it takes their addresses in
 _CALLED = ("zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_norm_rotate_back_work", "zo_cache_attend",
            "zo_cache_attend_work", "zo_cache_copy", "zo_draw_split", "zo_draw_work")
