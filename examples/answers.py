@@ -8,10 +8,11 @@ step is the usual one: coefficients from the losses, one fused update.
 
     python examples/answers.py [--steps N] [--probes K] [--answers A] [--tokens T]
 
-The answers take every operator of a decode step: the prompt's keys and values are put in the paged
+The answers take the operators of a decode step: the prompt's keys and values are put in the paged
 cache once and its pages shared by all answers to it (a page is copied when the first answer writes
 into it), each new token's queries and keys are normed, rotated and put in one pass, attend to the
-cache, and the next token is drawn from the logits.
+cache, and the next token is drawn from the logits. A prompt's tokens attend one by one, as sequences
+that share their pages: right for prompts of this size, but each token reads what is before it again.
 """
 
 import argparse
