@@ -20,7 +20,8 @@ the C names of include/zo.h:
 
 The operators of a decode step (include/zo_decode.h) are bound in decode.py and reached here under their C
 names as well: zo_norm_rotate, zo_norm_rotate_back, zo_norm_rotate_put, zo_rotary_turns, zo_cache_attend,
-zo_cache_copy, zo_draw, ZoPages. They need torch, so they are loaded at their first use.
+zo_cache_copy, zo_draw, ZoPages. So are those for several new tokens of a sequence (include/zo_tree.h, tree.py):
+zo_tree_lay, zo_tree_attend, zo_tree_accept, zo_tree_keep. They need torch, so they are loaded at their first use.
 
 If libzo.so has not been built the import succeeds but every call raises ZoLibraryMissing:
 there is no fallback implementation.
@@ -284,12 +285,14 @@ def zo_version():
 _DECODE = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_cache_attend",
            "zo_cache_copy", "zo_draw", "ZoPages", "ZO_ERR_MEMORY", "ZO_ERR_FULL", "ZO_DIM_MAX", "ZO_ROTARY_LINEAR",
            "ZO_ROTARY_BASE", "ZO_ROTARY_BANDS")
+_TREE = ("zo_tree_lay", "zo_tree_attend", "zo_tree_accept", "zo_tree_keep", "ZO_TREE_WORDS")
 
 
 def __getattr__(name):
-    if name in _DECODE:
-        from . import decode
-        for n in _DECODE:  # later uses find them here
-            globals()[n] = getattr(decode, n)
+    if name in _DECODE or name in _TREE:
+        from . import decode, tree
+        for names, module in ((_DECODE, decode), (_TREE, tree)):  # later uses find them here
+            for n in names:
+                globals()[n] = getattr(module, n)
         return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")

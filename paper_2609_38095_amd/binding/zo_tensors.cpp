@@ -19,12 +19,13 @@
 #include <vector>
 
 #include "zo_decode.h"
+#include "zo_tree.h"
 
 namespace {
 
 struct Entry {
   decltype(&zo_norm_rotate) norm_rotate;
-  decltype(&zo_norm_rotate_put) norm_rotate_put;
+  decltype(&zo_norm_rotate_put_at) norm_rotate_put;
   decltype(&zo_norm_rotate_back) norm_rotate_back;
   decltype(&zo_norm_rotate_back_work) norm_rotate_back_work;
   decltype(&zo_cache_attend) cache_attend;
@@ -32,6 +33,11 @@ struct Entry {
   decltype(&zo_cache_copy) cache_copy;
   decltype(&zo_draw_split) draw_split;
   decltype(&zo_draw_work) draw_work;
+  decltype(&zo_tree_lay) tree_lay;
+  decltype(&zo_tree_attend) tree_attend;
+  decltype(&zo_tree_attend_work) tree_attend_work;
+  decltype(&zo_tree_accept) tree_accept;
+  decltype(&zo_tree_keep) tree_keep;
 } entry = {};
 
 struct Refusal {  // a Python exception to raise
@@ -264,12 +270,12 @@ PyObject* norm_rotate(PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* norm_rotate_put(PyObject* const* args, Py_ssize_t n) {
-  Args a(args, n, 17);
+  Args a(args, n, 18);
   const at::Tensor *q = a.tensor("q"), *k = a.tensor("k"), *v = a.tensor("v");
   const at::Tensor *k_cache = a.tensor("k_cache"), *v_cache = a.tensor("v_cache"), *table = a.tensor("table");
   const Sides s(q, k);
   const Rule rule(a);
-  const at::Tensor *seqs = a.tensor("seqs"), *q_given = a.tensor("q_out");
+  const at::Tensor *seqs = a.tensor("seqs"), *q_given = a.tensor("q_out"), *places = a.tensor("places");
   zo_rotate_put p = {};
   rule.fill(p.a, s);
   at::Tensor q_out;
@@ -283,7 +289,7 @@ PyObject* norm_rotate_put(PyObject* const* args, Py_ssize_t n) {
   p.cache = cache_of(k_cache, v_cache, s.type);
   p.table = table_of(table);
   p.seqs = vector_of<const int32_t>(seqs, "seqs", at::kInt, s.tokens);
-  const int rc = entry.norm_rotate_put(&p, a.stream);
+  const int rc = entry.norm_rotate_put(&p, vector_of<const int32_t>(places, "places", at::kInt, s.tokens), a.stream);
   return rc == ZO_OK ? wrap_or_none(q_out) : status(rc);
 }
 
@@ -369,44 +375,53 @@ PyObject* cache_attend(PyObject* const* args, Py_ssize_t n) {
   return lse ? tuple_of({out, sums}) : THPVariable_Wrap(out);
 }
 
+// Caches of a model's layers: the tensors' addresses, and their shape and type.
+struct Layers {
+  std::vector<void*> tensors;
+  zo_cache shape = {};
+  int32_t dtype = 0;
+  const at::Tensor* first = nullptr;  // nullptr: no layers
+
+  Layers(Args& a, PyObject* k_caches, PyObject* v_caches) {
+    PyObject* lists[2] = {k_caches, v_caches};
+    if (!PyList_Check(lists[0]) || !PyList_Check(lists[1]) || PyList_GET_SIZE(lists[0]) != PyList_GET_SIZE(lists[1]))
+      refuse(PyExc_ValueError, "one v_cache for each k_cache");
+    const Py_ssize_t layers = PyList_GET_SIZE(lists[0]);
+    tensors.reserve(2 * layers);
+    for (PyObject* list : lists) {
+      for (Py_ssize_t i = 0; i < layers; ++i) {
+        PyObject* o = PyList_GET_ITEM(list, i);
+        Args one = a;
+        one.at = &o;
+        const at::Tensor* t = one.tensor("each cache");
+        if (first == nullptr) {
+          if (t == nullptr) refuse(PyExc_TypeError, "each cache must be a CUDA (HIP) torch tensor");
+          first = t;
+          dtype = type_of(*t, "each cache");
+          shape = cache_of(t, t, t->scalar_type());
+        }
+        if (t == nullptr || t->scalar_type() != first->scalar_type() || !same_layout(*t, *first))
+          refuse(PyExc_ValueError, "each cache must have the type, shape and strides of the first");
+        tensors.push_back(t->data_ptr());
+      }
+    }
+  }
+};
+
 PyObject* cache_copy(PyObject* const* args, Py_ssize_t n) {
   Args a(args, n, 7);
   PyObject* lists[2] = {a.next(), a.next()};
   const Host src(a.next(), "src", "i"), dst(a.next(), "dst", "i"), rows_in(a.next(), "rows", "i");
-  if (!PyList_Check(lists[0]) || !PyList_Check(lists[1]) || PyList_GET_SIZE(lists[0]) != PyList_GET_SIZE(lists[1]))
-    refuse(PyExc_ValueError, "one v_cache for each k_cache");
-  const Py_ssize_t layers = PyList_GET_SIZE(lists[0]);
-  if (layers == 0) Py_RETURN_NONE;
+  Layers layers(a, lists[0], lists[1]);
+  if (layers.first == nullptr) Py_RETURN_NONE;
   if (src.count() != dst.count() || (rows_in.held && rows_in.count() != src.count()))
     refuse(PyExc_ValueError, "one dst, and one count of rows, for each src");
-  std::vector<void*> tensors;
-  tensors.reserve(2 * layers);
-  const at::Tensor* first = nullptr;
-  zo_cache shape = {};
-  int32_t dtype = 0;
-  for (PyObject* list : lists) {
-    for (Py_ssize_t i = 0; i < layers; ++i) {
-      PyObject* o = PyList_GET_ITEM(list, i);
-      Args one = a;
-      one.at = &o;
-      const at::Tensor* t = one.tensor("each cache");
-      if (first == nullptr) {
-        if (t == nullptr) refuse(PyExc_TypeError, "each cache must be a CUDA (HIP) torch tensor");
-        first = t;
-        dtype = type_of(*t, "each cache");
-        shape = cache_of(t, t, t->scalar_type());
-      }
-      if (t == nullptr || t->scalar_type() != first->scalar_type() || !same_layout(*t, *first))
-        refuse(PyExc_ValueError, "each cache must have the type, shape and strides of the first");
-      tensors.push_back(t->data_ptr());
-    }
-  }
   std::vector<zo_page_move> moves(src.count());
   for (size_t i = 0; i < moves.size(); ++i)
     moves[i] = zo_page_move{static_cast<const int32_t*>(src.data())[i], static_cast<const int32_t*>(dst.data())[i],
-                            rows_in.held ? static_cast<const int32_t*>(rows_in.data())[i] : static_cast<int32_t>(shape.page_tokens)};
-  const int rc = entry.cache_copy(&shape, tensors.data(), static_cast<uint32_t>(tensors.size()), moves.data(),
-                                  static_cast<uint32_t>(moves.size()), static_cast<zo_dtype>(dtype), a.stream);
+                            rows_in.held ? static_cast<const int32_t*>(rows_in.data())[i] : static_cast<int32_t>(layers.shape.page_tokens)};
+  const int rc = entry.cache_copy(&layers.shape, layers.tensors.data(), static_cast<uint32_t>(layers.tensors.size()), moves.data(),
+                                  static_cast<uint32_t>(moves.size()), static_cast<zo_dtype>(layers.dtype), a.stream);
   if (rc != ZO_OK) return status(rc);
   Py_RETURN_NONE;
 }
@@ -449,6 +464,145 @@ PyObject* draw(PyObject* const* args, Py_ssize_t n) {
   return logprobs ? tuple_of({tokens, probs}) : THPVariable_Wrap(tokens);
 }
 
+// starts int32 [sequences + 1]; returns the sequences.
+uint32_t starts_of(const at::Tensor* starts, const int32_t*& at) {
+  if (starts == nullptr) refuse(PyExc_TypeError, "starts is needed");
+  if (starts->dim() != 1 || starts->size(0) < 1) refuse(PyExc_ValueError, "starts must hold an entry more than there are sequences");
+  at = vector_of<const int32_t>(starts, "starts", at::kInt, starts->size(0));
+  return count_of(starts->size(0) - 1, "starts");
+}
+
+PyObject* tree_lay(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 7);
+  const at::Tensor *starts = a.tensor("starts"), *lengths = a.tensor("lengths");
+  const long long tokens = a.integer();
+  const at::Tensor* parents = a.tensor("parents");
+  const long long words = a.integer();
+  if (lengths == nullptr) refuse(PyExc_TypeError, "lengths is needed");
+  if (tokens < 0 || tokens > 0xFFFFFFFFll || words < 0 || words > 0xFFFFFFFFll) return status(ZO_ERR_ARG);
+  zo_tree t = {};
+  t.seqs = starts_of(starts, t.starts);
+  t.lengths = vector_of<const int32_t>(lengths, "lengths", at::kInt, t.seqs);
+  t.parents = vector_of<const int32_t>(parents, "parents", at::kInt, tokens);
+  t.tokens = static_cast<uint32_t>(tokens);
+  t.words = static_cast<uint32_t>(words);
+  if (t.words > ZO_TREE_WORDS || t.tokens >= (1u << 24)) return status(ZO_ERR_ARG);  // before anything of that size is allocated
+  if (parents != nullptr && tokens == 0) t.parents = nullptr;
+  at::Tensor out[3], seen;
+  for (at::Tensor& o : out) o = fresh(*starts, {tokens}, at::kInt);
+  t.seq_of = static_cast<int32_t*>(out[0].data_ptr());
+  t.positions = static_cast<int32_t*>(out[1].data_ptr());
+  t.places = static_cast<int32_t*>(out[2].data_ptr());
+  if (words > 0) {
+    seen = fresh(*starts, {tokens, words}, at::kLong);
+    t.seen = static_cast<uint64_t*>(seen.data_ptr());
+  }
+  const int rc = entry.tree_lay(&t, a.stream);
+  return rc == ZO_OK ? tuple_of({out[0], out[1], out[2], seen}) : status(rc);
+}
+
+PyObject* tree_attend(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 13);
+  const at::Tensor *q = a.tensor("q"), *k_cache = a.tensor("k_cache"), *v_cache = a.tensor("v_cache"), *table = a.tensor("table");
+  const at::Tensor *lengths = a.tensor("lengths"), *starts = a.tensor("starts"), *seen = a.tensor("seen");
+  PyObject* scale = a.next();
+  const at::Tensor* out_given = a.tensor("out");
+  const bool lse = a.flag();
+  const at::Tensor* work = a.tensor("work");
+  if (q == nullptr) refuse(PyExc_TypeError, "q must be a CUDA (HIP) torch tensor");
+  zo_tree_attention p = {};
+  p.dtype = type_of(*q, "q");
+  if (q->dim() != 3) refuse(PyExc_ValueError, "q must be [tokens, heads, dim]");
+  const int64_t tokens = q->size(0), heads = q->size(1), dim = q->size(2);
+  p.q = rows(q, "q", q->scalar_type(), tokens, heads, dim);
+  p.cache = cache_of(k_cache, v_cache, q->scalar_type());
+  if (p.cache.dim != dim)
+    refuse(PyExc_ValueError, "the cache's heads hold %u dims, the queries' %lld", p.cache.dim, static_cast<long long>(dim));
+  p.table = table_of(table);
+  if (starts_of(starts, p.starts) != p.table.seqs) refuse(PyExc_ValueError, "the table has one row for each sequence");
+  if (lengths == nullptr) refuse(PyExc_TypeError, "lengths is needed");
+  p.lengths = vector_of<const int32_t>(lengths, "lengths", at::kInt, p.table.seqs);
+  p.tokens = count_of(tokens, "q");
+  p.q_heads = count_of(heads, "q");
+  if (seen != nullptr) {
+    check_type(*seen, "seen", at::kLong);
+    if (seen->dim() != 2 || seen->size(0) != tokens || (seen->size(1) > 1 && seen->stride(1) != 1))
+      refuse(PyExc_ValueError, "seen must be [%lld, words], its rows contiguous", static_cast<long long>(tokens));
+    static const uint64_t nothing = 0;  // masks without words are no chain; with 0 words nothing is read
+    p.seen = seen->numel() > 0 ? static_cast<const uint64_t*>(seen->data_ptr()) : &nothing;
+    p.seen_stride = seen->stride(0);
+    p.words = count_of(seen->size(1), "seen");
+  }
+  if (scale == Py_None) {
+    p.scale = static_cast<float>(1.0 / std::sqrt(static_cast<double>(dim)));
+  } else {
+    const double v = PyFloat_AsDouble(scale);
+    if (v == -1.0 && PyErr_Occurred()) throw python_error();
+    p.scale = static_cast<float>(v);
+  }
+  at::Tensor sums, hold;
+  const at::Tensor out = out_given ? *out_given : fresh(*q, {tokens, heads, dim}, q->scalar_type());
+  p.out = rows(&out, "out", q->scalar_type(), tokens, heads, dim);
+  if (lse) {
+    sums = fresh(*q, {tokens, heads}, at::kFloat);
+    p.lse = static_cast<float*>(sums.data_ptr());
+  }
+  work_of(work, *q, entry.tree_attend_work(p.tokens, p.table.seqs, p.q_heads, p.cache.heads, p.cache.dim, p.dtype), hold, p.work, p.work_bytes);
+  const int rc = entry.tree_attend(&p, a.stream);
+  if (rc != ZO_OK) return status(rc);
+  return lse ? tuple_of({out, sums}) : THPVariable_Wrap(out);
+}
+
+PyObject* tree_accept(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 7);
+  const at::Tensor *drafted = a.tensor("drafted"), *drawn = a.tensor("drawn"), *starts = a.tensor("starts");
+  const long long most = a.integer();
+  const at::Tensor* parents = a.tensor("parents");
+  if (drafted == nullptr || drawn == nullptr) refuse(PyExc_TypeError, "drafted and drawn must be CUDA (HIP) torch tensors");
+  if (drafted->dim() != 1) refuse(PyExc_ValueError, "drafted must be [tokens]");
+  const int64_t tokens = drafted->size(0);
+  zo_tree_walk w = {};
+  w.seqs = starts_of(starts, w.starts);
+  w.drafted = vector_of<const int32_t>(drafted, "drafted", at::kInt, tokens);
+  w.drawn = vector_of<const int32_t>(drawn, "drawn", at::kInt, tokens);
+  w.parents = vector_of<const int32_t>(parents, "parents", at::kInt, tokens);
+  w.tokens = count_of(tokens, "drafted");
+  if (most < 1 || most >= (1 << 24) || static_cast<uint64_t>(most) * w.seqs >= (1u << 24)) return status(ZO_ERR_ARG);
+  w.most = static_cast<uint32_t>(most);
+  const at::Tensor path = fresh(*drafted, {w.seqs, most}, at::kInt), won = fresh(*drafted, {w.seqs, most}, at::kInt);
+  const at::Tensor counts = fresh(*drafted, {w.seqs}, at::kInt);
+  w.path = static_cast<int32_t*>(path.data_ptr());
+  w.tokens_out = static_cast<int32_t*>(won.data_ptr());
+  w.counts = static_cast<int32_t*>(counts.data_ptr());
+  const int rc = entry.tree_accept(&w, a.stream);
+  return rc == ZO_OK ? tuple_of({path, won, counts}) : status(rc);
+}
+
+PyObject* tree_keep(PyObject* const* args, Py_ssize_t n) {
+  Args a(args, n, 7);
+  PyObject* lists[2] = {a.next(), a.next()};
+  const at::Tensor *table = a.tensor("table"), *lengths = a.tensor("lengths"), *path = a.tensor("path");
+  Layers layers(a, lists[0], lists[1]);
+  if (layers.first == nullptr) Py_RETURN_NONE;
+  zo_tree_moves m = {};
+  m.shape = layers.shape;
+  m.dtype = layers.dtype;
+  m.tensors = layers.tensors.data();
+  m.n_tensors = static_cast<uint32_t>(layers.tensors.size());
+  m.table = table_of(table);
+  if (lengths == nullptr || path == nullptr) refuse(PyExc_TypeError, "lengths and path are needed");
+  m.lengths = vector_of<const int32_t>(lengths, "lengths", at::kInt, m.table.seqs);
+  check_type(*path, "path", at::kInt);
+  if (path->dim() != 2 || path->size(0) != m.table.seqs || (path->size(1) > 1 && path->stride(1) != 1))
+    refuse(PyExc_ValueError, "path must be [sequences, tokens], its rows contiguous");
+  m.path = static_cast<const int32_t*>(path->data_ptr());
+  m.path_stride = path->stride(0);
+  m.most = count_of(path->size(1), "path");
+  const int rc = entry.tree_keep(&m, a.stream);
+  if (rc != ZO_OK) return status(rc);
+  Py_RETURN_NONE;
+}
+
 // bind(addresses of the library's entry points, in Entry's order)
 PyObject* bind(PyObject* const* args, Py_ssize_t n) {
   if (n != static_cast<Py_ssize_t>(sizeof(Entry) / sizeof(void*))) refuse(PyExc_TypeError, "an address for each entry point");
@@ -481,7 +635,8 @@ PyMethodDef method(const char* name) {
 
 PyMethodDef methods[] = {method<bind>("bind"), method<norm_rotate>("norm_rotate"), method<norm_rotate_put>("norm_rotate_put"),
                          method<norm_rotate_back>("norm_rotate_back"), method<cache_attend>("cache_attend"),
-                         method<cache_copy>("cache_copy"), method<draw>("draw"), {nullptr, nullptr, 0, nullptr}};
+                         method<cache_copy>("cache_copy"), method<draw>("draw"), method<tree_lay>("tree_lay"),
+                         method<tree_attend>("tree_attend"), method<tree_accept>("tree_accept"), method<tree_keep>("tree_keep"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -403,9 +403,102 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
   }
 }
 
+int check_tree(const zo_tree& t) {
+  if (t.tokens >= (1u << 24) || t.seqs >= (1u << 24) || t.words > ZO_TREE_WORDS) return ZO_ERR_ARG;
+  if (t.parents != nullptr && t.words == 0) return ZO_ERR_ARG;
+  if (t.tokens == 0) return ZO_OK;
+  if (t.seq_of == nullptr || t.positions == nullptr || t.places == nullptr || (t.words > 0 && t.seen == nullptr)) return ZO_ERR_NULL;
+  if (t.seqs > 0 && (t.starts == nullptr || t.lengths == nullptr)) return ZO_ERR_NULL;
+  return aligned(t.starts, 4) && aligned(t.lengths, 4) && aligned(t.parents, 4) && aligned(t.seq_of, 4) && aligned(t.positions, 4) &&
+                 aligned(t.places, 4) && aligned(t.seen, 8)
+             ? ZO_OK
+             : ZO_ERR_ARG;
+}
+
+int check_walk(const zo_tree_walk& w) {
+  if (w.tokens >= (1u << 24) || w.seqs >= (1u << 24) || w.most == 0) return ZO_ERR_ARG;
+  if (static_cast<uint64_t>(w.seqs) * w.most >= (1u << 24)) return ZO_ERR_ARG;
+  if (w.seqs == 0) return ZO_OK;
+  if (w.starts == nullptr || w.path == nullptr || w.tokens_out == nullptr || w.counts == nullptr) return ZO_ERR_NULL;
+  if (w.tokens > 0 && (w.drafted == nullptr || w.drawn == nullptr)) return ZO_ERR_NULL;
+  return aligned(w.drafted, 4) && aligned(w.drawn, 4) && aligned(w.starts, 4) && aligned(w.parents, 4) && aligned(w.path, 4) &&
+                 aligned(w.tokens_out, 4) && aligned(w.counts, 4)
+             ? ZO_OK
+             : ZO_ERR_ARG;
+}
+
+int check_moves(const zo_tree_moves& m) {
+  if (!dtype_ok(m.dtype) || m.table.seqs >= (1u << 17) || m.most > 0x7FFFFFFFu) return ZO_ERR_ARG;  // 2^32 threads at most in a launch
+  if (m.n_tensors == 0 || m.table.seqs == 0 || m.most == 0) return ZO_OK;
+  if (m.tensors == nullptr || m.lengths == nullptr || m.path == nullptr) return ZO_ERR_NULL;
+  if (!aligned(m.lengths, 4) || !aligned(m.path, 4) || !axis_ok(m.path_stride, m.table.seqs)) return ZO_ERR_ARG;
+  zo_cache first = m.shape;
+  first.k = first.v = m.tensors[0];
+  const size_t elem = elem_bytes(m.dtype);
+  ZO_TRY(check_cache(first, elem, true));
+  if (first.heads > 0xFFFFu) return ZO_ERR_ARG;
+  ZO_TRY(check_table(m.table));
+  for (uint32_t i = 0; i < m.n_tensors; ++i) {
+    if (m.tensors[i] == nullptr) return ZO_ERR_NULL;
+    if (!aligned(m.tensors[i], elem)) return ZO_ERR_ARG;
+  }
+  try {
+    return tensors_overlap(first, m.tensors, m.n_tensors, elem) ? ZO_ERR_ARG : ZO_OK;
+  } catch (const std::bad_alloc&) {
+    return ZO_ERR_MEMORY;
+  }
+}
+
+TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim, int32_t dtype) {
+  TreeShape s = {};
+  if (heads == 0 || q_heads % heads != 0 || q_heads == 0 || seqs == 0 || tokens == 0) return s;
+  const uint64_t group = q_heads / heads, rows = (tokens * group + seqs - 1) / seqs;  // of a sequence, on average
+  // keys and values of four waves' own tiles have to fit the LDS
+  const bool own_tiles = dim * elem_bytes(dtype) <= 512;
+  s.row_waves = rows <= 32 && own_tiles ? 1 : 4;
+  s.rows = 32 * s.row_waves;
+  s.workers = dim * elem_bytes(dtype) <= 256 ? 512 : 256;
+  s.items = (tokens * group / s.rows + seqs) * heads;
+  return s;
+}
+
+int check_tree_attend(const zo_tree_attention& a) {
+  if (!dtype_ok(a.dtype)) return ZO_ERR_ARG;
+  const size_t elem = elem_bytes(a.dtype);
+  if (a.cache.heads == 0 || a.cache.heads > 0xFFFFu || a.q_heads > 0xFFFFu || a.q_heads % a.cache.heads != 0) return ZO_ERR_ARG;
+  // a workgroup for each item, 2^32 threads at most in a launch
+  if (static_cast<uint64_t>(a.tokens) * std::max(a.q_heads, 1u) >= (1u << 24)) return ZO_ERR_ARG;
+  if (static_cast<uint64_t>(a.table.seqs) * a.cache.heads >= (1u << 23)) return ZO_ERR_ARG;
+  if (!std::isfinite(a.scale)) return ZO_ERR_NONFINITE;
+  if (a.table.seqs == 0 || a.tokens == 0 || a.q_heads == 0) return ZO_OK;
+  ZO_TRY(check_cache(a.cache, elem, false));
+  ZO_TRY(check_table(a.table));
+  ZO_TRY(check_rows(a.q, a.tokens, a.q_heads, a.cache.dim, elem, false));
+  ZO_TRY(check_rows(a.out, a.tokens, a.q_heads, a.cache.dim, elem, true));
+  // a workgroup writes its rows while others still read their queries and the cache
+  ZO_TRY(check_apart(a.out, a.q_heads, a.q, a.q_heads, false, a.tokens, a.cache.dim, elem));
+  if (cache_overlaps(a.cache, a.out, a.tokens, a.q_heads, elem)) return ZO_ERR_ARG;
+  // keys of a sequence are numbered in 32 bits
+  if (static_cast<uint64_t>(a.table.width) * a.cache.page_tokens >= (1ull << 31)) return ZO_ERR_ARG;
+  if (a.lengths == nullptr || a.starts == nullptr || a.work == nullptr) return ZO_ERR_NULL;
+  if (a.seen != nullptr && (a.words > (1u << 20) || !aligned(a.seen, 8) || !axis_ok(a.seen_stride, a.tokens))) return ZO_ERR_ARG;
+  if (!aligned(a.lengths, 4) || !aligned(a.starts, 4) || !aligned(a.lse, 4) || !aligned(a.work, 16)) return ZO_ERR_ARG;
+  if (a.work_bytes < zo_tree_attend_work(a.tokens, a.table.seqs, a.q_heads, a.cache.heads, a.cache.dim, a.dtype)) return ZO_ERR_ARG;
+  return ZO_OK;
+}
+
 }  // namespace zo
 
 extern "C" {
+
+// A word for the count of items, the items' whereabouts, and two parts for each worker (of the items that its run begins and ends
+// in): for every row a maximum, a sum and a row of fp32.
+uint64_t zo_tree_attend_work(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim, int32_t dtype) {
+  if (dim == 0 || dim > ZO_DIM_MAX || (dtype != ZO_F32 && dtype != ZO_BF16)) return 0;
+  const zo::TreeShape s = zo::tree_shape(tokens, seqs, q_heads, heads, dim, dtype);
+  const uint64_t row = (dim + 3) / 4 * 4 + 4;
+  return 16 + s.items * zo::kTreeItemWords * 4 + 2ull * s.workers * s.rows * row * sizeof(float);
+}
 
 uint64_t zo_norm_rotate_back_work(uint32_t tokens, uint32_t q_heads, uint32_t k_heads, uint32_t dim) {
   return (static_cast<uint64_t>(zo::back_blocks(tokens, q_heads)) + zo::back_blocks(tokens, k_heads)) * dim * sizeof(float);

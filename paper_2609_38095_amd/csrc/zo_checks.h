@@ -7,6 +7,7 @@
 #include <cstdint>
 
 #include "zo_decode.h"
+#include "zo_tree.h"
 
 namespace zo {
 
@@ -19,6 +20,10 @@ int check_attend(const zo_attend& a);
 int check_draw(const zo_draw_args& a);
 int check_draw_split(const zo_draw_args& a, const void* work, uint64_t work_bytes);
 int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, const zo_page_move* moves, uint32_t n_moves, int32_t dtype);
+int check_tree(const zo_tree& t);
+int check_walk(const zo_tree_walk& w);
+int check_moves(const zo_tree_moves& m);
+int check_tree_attend(const zo_tree_attention& a);
 
 // Whether two sets of rows may share an element. Exact for rows of one interleaved buffer: equal strides, each as large as
 // what lies below it, or equal token strides and the heads of each side together. Otherwise by the ranges that they span.
@@ -31,6 +36,15 @@ constexpr uint32_t kBackBlocks = 512;
 uint32_t back_blocks(uint32_t tokens, uint32_t heads);
 uint64_t attend_items_bytes(uint32_t seqs, uint32_t q_heads, uint32_t heads);  // the parts' whereabouts
 uint32_t attend_workers(uint32_t dim);  // at most
+
+// zo_tree_attend: rows (a new token, a query head of a key head's group) of an item, waves that hold them, workgroups among which the
+// tiles are split (at most), and the most items of a call.
+struct TreeShape {
+  uint32_t row_waves, rows, workers;
+  uint64_t items;
+};
+TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim, int32_t dtype);
+constexpr uint32_t kTreeItemWords = 8;  // of 4 bytes: where an item's parts are
 
 // zo_draw_split: tokens of a workgroup's part, and words of 8 bytes that a part and a row keep.
 constexpr uint32_t kDrawPart = 4096, kDrawPartWords = 4074, kDrawRowWords = 2;

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "zo_decode.h"
+#include "zo_tree.h"
 
 struct zo_pages {
   struct Seq {
@@ -140,6 +141,19 @@ int zo_pages_extend(zo_pages* book, uint32_t seq, uint32_t tokens, zo_page_move*
     q.tokens += tokens;
     return ZO_OK;
   });
+}
+
+int zo_pages_cut(zo_pages* book, uint32_t seq, uint32_t tokens) {
+  if (book == nullptr) return ZO_ERR_NULL;
+  if (!book->has(seq) || tokens > book->seqs[seq].tokens) return ZO_ERR_ARG;
+  zo_pages::Seq& q = book->seqs[seq];
+  const uint64_t keep = book->pages_of(tokens);
+  while (q.pages.size() > keep) {
+    book->leave(q.pages.back());
+    q.pages.pop_back();
+  }
+  q.tokens = tokens;
+  return ZO_OK;
 }
 
 int zo_pages_drop(zo_pages* book, uint32_t seq) {

@@ -47,6 +47,7 @@ struct Rotation {
   Side side[3];
   const int32_t* positions;
   const int32_t* seqs;
+  const int32_t* places;  // of the tokens in their sequences, NULL: the positions
   const int32_t* ids;  // page table
   int64_t table_stride, page_stride, cache_token;
   uint32_t table_seqs, table_width, pages, page_tokens;
@@ -173,6 +174,7 @@ __device__ __forceinline__ void turn_share(const Sh& sh, int n, float (&a)[kVec]
 __device__ __forceinline__ int64_t place_of(const Rotation& r, const Side& sd, uint32_t token, int32_t pos) {
   if (!sd.put) return static_cast<int64_t>(token) * sd.y_token;
   const uint32_t seq = r.seqs ? static_cast<uint32_t>(r.seqs[token]) : token;
+  if (r.places) pos = r.places[token];
   if (pos < 0 || seq >= r.table_seqs) return -1;
   const uint32_t slot = static_cast<uint32_t>(pos) / r.page_tokens;
   if (slot >= r.table_width) return -1;
@@ -613,16 +615,18 @@ int zo_norm_rotate(const zo_rotate* a, void* stream) {
   return forward(r, *a, stream);
 }
 
-int zo_norm_rotate_put(const zo_rotate_put* p, void* stream) {
+int zo_norm_rotate_put_at(const zo_rotate_put* p, const int32_t* places, void* stream) {
   using namespace zo;
   if (p == nullptr) return ZO_ERR_NULL;
   const int rc = check_put(*p);
   if (rc != ZO_OK) return rc;
+  if (reinterpret_cast<uintptr_t>(places) % 4 != 0) return ZO_ERR_ARG;
   const zo_rotate& a = p->a;
   if (a.tokens == 0 || a.q_heads + a.k_heads == 0) return ZO_OK;
   Rotation r = rotation_of(a);
   const zo_cache& c = p->cache;
   r.seqs = p->seqs;
+  r.places = places;
   r.ids = p->table.ids;
   r.table_stride = p->table.stride;
   r.table_seqs = p->table.seqs;
@@ -637,6 +641,8 @@ int zo_norm_rotate_put(const zo_rotate_put* p, void* stream) {
   r.side[1].put = r.side[2].put = 1;
   return forward(r, a, stream);
 }
+
+int zo_norm_rotate_put(const zo_rotate_put* p, void* stream) { return zo_norm_rotate_put_at(p, nullptr, stream); }
 
 int zo_norm_rotate_back(const zo_rotate_back* b, void* stream) {
   using namespace zo;

@@ -11,7 +11,7 @@ the C names:
   zo_cache_attend(q, k_cache, v_cache, table, lengths)  one new token of each sequence over the cache
   zo_cache_copy(k_caches, v_caches, src, dst, rows)     copies of pages, every layer
   zo_draw(logits, u, temperature, top_k, top_p, min_p)  tokens from given random numbers
-  ZoPages(pages, page_tokens)                           the page book: add, fork, extend, drop, compact
+  ZoPages(pages, page_tokens)                           the page book: add, fork, extend, cut, drop, compact
 
 Rows of heads are tensors [tokens, heads, dim], caches [pages, heads, page_tokens, dim] (any strides,
 the last dimension contiguous: permute a cache that is laid out otherwise). Results are allocated by
@@ -40,8 +40,9 @@ EXPORTS = ("zo_rotary_turns", "zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_r
            "zo_draw_split", "zo_draw_work", "zo_pages_open", "zo_pages_close", "zo_pages_add", "zo_pages_fork",
            "zo_pages_extend", "zo_pages_drop", "zo_pages_left", "zo_pages_length", "zo_pages_table", "zo_pages_compact")
 # entry points that _tensors.so calls, in the order that it takes their addresses in
-_CALLED = ("zo_norm_rotate", "zo_norm_rotate_put", "zo_norm_rotate_back", "zo_norm_rotate_back_work", "zo_cache_attend",
-           "zo_cache_attend_work", "zo_cache_copy", "zo_draw_split", "zo_draw_work")
+_CALLED = ("zo_norm_rotate", "zo_norm_rotate_put_at", "zo_norm_rotate_back", "zo_norm_rotate_back_work", "zo_cache_attend",
+           "zo_cache_attend_work", "zo_cache_copy", "zo_draw_split", "zo_draw_work", "zo_tree_lay", "zo_tree_attend",
+           "zo_tree_attend_work", "zo_tree_accept", "zo_tree_keep")
 
 _READY = None
 _TENSORS = None
@@ -70,7 +71,10 @@ def _lib():
                 ("zo_pages_extend", [vp, u32, u32, move], i32), ("zo_pages_drop", [vp, u32], i32),
                 ("zo_pages_left", [vp], u32), ("zo_pages_length", [vp, u32], ctypes.c_int64),
                 ("zo_pages_table", [vp, vp, u32, vp, u64, u32, vp], i32),
-                ("zo_pages_compact", [vp, vp, u32, pu], i32)):
+                ("zo_pages_compact", [vp, vp, u32, pu], i32), ("zo_pages_cut", [vp, u32, u32], i32),
+                ("zo_norm_rotate_put_at", [args, vp, vp], i32), ("zo_tree_lay", [args, vp], i32),
+                ("zo_tree_attend", [args, vp], i32), ("zo_tree_attend_work", [u32, u32, u32, u32, u32, i32], u64),
+                ("zo_tree_accept", [args, vp], i32), ("zo_tree_keep", [args, vp], i32)):
             f = getattr(lib, name)
             f.argtypes, f.restype = argtypes, restype
         _READY = lib
@@ -171,11 +175,12 @@ def zo_norm_rotate(q, k, positions, turns=None, interleaved=False, magnitude=1.0
 
 
 def zo_norm_rotate_put(q, k, v, k_cache, v_cache, table, positions, turns=None, interleaved=False, magnitude=1.0,
-                       q_gamma=None, k_gamma=None, norm_eps=1e-6, seqs=None, q_out=None, stream=None):
+                       q_gamma=None, k_gamma=None, norm_eps=1e-6, seqs=None, q_out=None, stream=None, places=None):
     """zo_norm_rotate whose keys, with the values v, are put at token positions[t] of sequence seqs[t] (t itself
-    where seqs is None) of the paged cache. Returns q_out. q may be None."""
+    where seqs is None) of the paged cache, or at token places[t] where places are given (zo_norm_rotate_put_at: tokens of
+    different branches share positions). Returns q_out. q may be None."""
     return _call((_TENSORS or _tensors()).norm_rotate_put, stream, k, q, k, v, k_cache, v_cache, table, positions, _doubles(turns),
-                 interleaved, magnitude, q_gamma, k_gamma, norm_eps, seqs, q_out)
+                 interleaved, magnitude, q_gamma, k_gamma, norm_eps, seqs, q_out, places)
 
 
 def zo_norm_rotate_back(dq_out, dk_out, q, k, positions, turns=None, interleaved=False, magnitude=1.0, q_gamma=None,
@@ -251,6 +256,10 @@ class ZoPages:
         _check(_lib().zo_pages_extend(self._book, _count(seq, "zo_pages_extend"), _count(tokens, "zo_pages_extend"),
                                       ctypes.byref(move)), "zo_pages_extend")
         return (move.src, move.dst, move.rows) if move.rows else None
+
+    def cut(self, seq, tokens):
+        """The sequence keeps its first tokens; pages behind them are free again where no other holds them."""
+        _check(_lib().zo_pages_cut(self._book, _count(seq, "zo_pages_cut"), _count(tokens, "zo_pages_cut")), "zo_pages_cut")
 
     def drop(self, seq):
         _check(_lib().zo_pages_drop(self._book, _count(seq, "zo_pages_drop")), "zo_pages_drop")
