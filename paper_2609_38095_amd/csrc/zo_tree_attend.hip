@@ -232,11 +232,11 @@ __device__ __forceinline__ void write_row(const Attend& a, uint32_t token, uint3
     a.lse[static_cast<size_t>(token) * a.heads * a.group + q_head] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
 }
 
-// Sixteen bytes of a row from dim `at` on; behind the row's end zeros (kAny).
-template <class T, bool kAny>
-__device__ __forceinline__ u32x4 load_chunk(const char* row, uint32_t at, uint32_t dim) {
+// Sixteen bytes of a row from dim `at` on; behind the row's end zeros.
+template <class T>
+__device__ __forceinline__ u32x4 load_chunk_of(const char* row, uint32_t at, uint32_t dim) {
   constexpr uint32_t kElems = 16 / sizeof(T);
-  if (!kAny || at + kElems <= dim) return *reinterpret_cast<const u32x4_any*>(row + at * sizeof(T));
+  if (at + kElems <= dim) return *reinterpret_cast<const u32x4_any*>(row + at * sizeof(T));
   T got[kElems] = {};
 #pragma unroll
   for (uint32_t e = 0; e < kElems; ++e)
@@ -260,7 +260,16 @@ __device__ __forceinline__ bool odd_values(u32x4 v) {
   return odd;
 }
 
-template <class S, uint32_t kDim, uint32_t kRowWaves>
+// The kernel's arguments read anew: a copy of its own for each part of the kernel, so that those of one part do not hold (and spill) the
+// scalar registers of another.
+__device__ __forceinline__ Attend arguments() {
+  typedef const __attribute__((address_space(4))) Attend* Arguments;
+  Arguments from = (Arguments)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(from));
+  return *(const Attend*)from;
+}
+
+template <class S, uint32_t kDim, uint32_t kRowWaves, bool kAny>
 struct Form {
   typedef typename S::storage T;
   static constexpr uint32_t kRowBytes = kDim * sizeof(T), kChunks = kRowBytes / 16;
@@ -268,33 +277,56 @@ struct Form {
   static constexpr uint32_t kBlocks = kRowWaves == 4 && kRowBytes <= 256 ? 2 : 1;  // of 32 keys, of a wave in a tile
   static constexpr uint32_t kKeys = 32 * kBlocks, kTile = kKeys * kKeyWaves;
   static constexpr uint32_t kStageRows = kKeys / kRowWaves;          // rows that a wave brings
-  static constexpr uint32_t kLoads = kStageRows * kChunks / kWave;   // 16-byte loads of each lane for the keys; for the values as many
+  static constexpr uint32_t kLoadRows = kWave / kChunks;             // rows of a load of all lanes
+  static constexpr uint32_t kLoads = kStageRows / kLoadRows;         // of the keys, and as many of the values
   static constexpr uint32_t kBuffers = kRowWaves > 1 ? 2 : 1;
   static constexpr uint32_t kBufferBytes = 2 * kTile * kRowBytes;
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
   static constexpr uint32_t kPerCu = kRowBytes <= 256 ? 2 : 1;  // workgroups
   static_assert(kRowWaves != 1 || 2 * 32 * (kDim + 4) * 4 <= kBufferBytes, "the join at an item's end has room");
+  static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
 };
 
+typedef __attribute__((address_space(3))) char lds_char;
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>((lds_char*)p)); }
+
+// Sixteen bytes of each lane from base + offset straight into LDS, one lane behind another from `to` on. The compiler does not
+// count these loads: loads_left() waits for them.
+__device__ __forceinline__ void load_to_lds(uint32_t to, uint64_t base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(to), "v"(offset), "s"(base) : "memory", "m0");
+}
+template <int kLeft>
+__device__ __forceinline__ void loads_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
+}
+
+// kAny: any head size (kDim: the size that it is padded to with zeros), page size and alignment; keys and values pass through
+// registers. Else: heads of kDim, pages of whole sixteens of tokens, 16-byte aligned rows, straight into LDS.
 template <class S, uint32_t kDim, uint32_t kRowWaves, bool kAny>
-__global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) attend_kernel(const Attend a) {
-  typedef Form<S, kDim, kRowWaves> F;
+__global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves, kAny>::kPerCu)) attend_kernel(const Attend) {
+  typedef Form<S, kDim, kRowWaves, kAny> F;
   typedef typename S::storage T;
   constexpr bool kWide = sizeof(T) == 4;
   constexpr uint32_t kRowBytes = F::kRowBytes, kChunks = F::kChunks, kRows = F::kRows, kBlocks = F::kBlocks, kKeys = F::kKeys;
-  constexpr uint32_t kTile = F::kTile, kLoads = F::kLoads, kOuts = kDim / 32, kSteps = kChunks / 2;
+  constexpr uint32_t kTile = F::kTile, kLoads = F::kLoads, kLoadRows = F::kLoadRows, kOuts = kDim / 32, kSteps = kChunks / 2;
   constexpr uint32_t kKeyMask = kChunks < 16 ? kChunks - 1 : 15;                 // the keys' swizzle
   extern __shared__ __align__(16) char lds[];
   __shared__ uint64_t before[kThreads];
   __shared__ uint32_t items_before[kThreads];
-  __shared__ uint32_t odd_keys[3][F::kKeyWaves][2];  // of the tile in use, the next one, and emptied for the one behind it
+  __shared__ uint32_t odd_there[2];  // odd values in this item's tiles, and emptied for the next item's
   __shared__ float2 merge_sums[2][32];
 
   const uint32_t wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 32, g = lane / 32;
   const uint32_t rw = wave % kRowWaves, kw = wave / kRowWaves;  // which rows, which keys
-  const Deal d = deal<kRows, kTile>(a, before, items_before);
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.item_count = d.items;
-  const Runs runs(d.total, a.workers);
+  Deal d;
+  uint32_t workers;
+  {
+    const Attend a = arguments();
+    d = deal<kRows, kTile>(a, before, items_before);
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.item_count = d.items;
+    workers = a.workers;
+  }
+  const Runs runs(d.total, workers);
   // neighbouring runs on one XCD: workgroup b runs on XCD b % 8
   const uint32_t per_xcd = (runs.workers + kXcds - 1) / kXcds;
   const uint32_t slot_of = blockIdx.x / kXcds, worker = blockIdx.x % kXcds * per_xcd + slot_of;
@@ -308,6 +340,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   uint64_t item_first;
   Seq s;
   {
+    const Attend a = arguments();
     uint32_t chunk = 0;  // the last thread's sequences that begin at or before it
 #pragma unroll
     for (uint32_t step = kThreads / 2; step > 0; step /= 2)
@@ -350,7 +383,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   }
 
   // LDS places of the lane's shares: of the rows that it brings, of the key and of the values that it uses
-  const uint32_t stage_row = rw * F::kStageRows + lane / kChunks, stage_chunk = lane % kChunks;
+  const uint32_t stage_row = rw * F::kStageRows, load_row = lane / kChunks, load_chunk = lane % kChunks;
   char* own = lds + kw * 2 * kKeys * kRowBytes;  // the keys of the waves that share them, and their values behind these
   const uint32_t key_at = r * kRowBytes + ((g ^ (r & kKeyMask)) * 16);
   uint32_t value_at;
@@ -361,9 +394,12 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
     const uint32_t chunk = (lane / 16 % 2 * 2 + lane % 4 / 2) ^ (row * 2 & (kChunks - 1));
     value_at = row * kRowBytes + chunk * 16 + lane % 2 * 8;
   }
+  const auto key_swizzle = [](uint32_t row) { return row & kKeyMask; };
   const auto value_swizzle = [](uint32_t row) { return kWide ? 0u : row % 8 * 2 & (kChunks - 1); };
 
-  while (at < end) {
+  if (threadIdx.x == 0) odd_there[0] = 0;
+  for (uint32_t turn = 0; at < end; turn ^= 1) {
+    const Attend a = arguments();
     const uint32_t rows = s.count * a.group, row0 = block * kRows, in_block = min(kRows, rows - row0);
     const uint32_t sees = visible(a, s, row0 + kRows);
     const uint32_t tiles = max(1u, (sees + kTile - 1) / kTile);
@@ -381,9 +417,28 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
     const char* kp = a.k + head * a.head_bytes;
     const char* vp = a.v + head * a.head_bytes;
 
-    // The page id of the lane's key of a tile; then its row's place (bytes, -1: dead) and which of the wave's keys are live.
-    const auto key_of = [&](uint32_t t) { return t * kTile + kw * kKeys + lane % kKeys; };
     const auto page_of = [&](uint32_t j) { return a.page_shift >= 0 ? j >> a.page_shift : j / a.page_tokens; };
+    constexpr uint64_t kAll = kKeys == 64 ? ~0ull : (1ull << (kKeys % 64)) - 1;
+    // Whether values of the tile may have to be emptied: not all rows see all of its keys.
+    const auto some_see = [&](uint32_t t) { return t * kTile + kTile > all_see; };
+    // The lane's 16 bytes of row `row` (of the wave's keys) of the values, as they go to LDS: zeros where the row is dead, and, in a tile
+    // that only some rows see, where it has an infinity or a NaN. Both are known to all lanes of a row.
+    const auto kept = [&](uint32_t t, uint32_t row, uint64_t live, u32x4 v) {
+      bool keep = live >> row & 1;
+      if (some_see(t)) {
+        const uint64_t odd = __ballot(keep && odd_values<T>(v));
+        if (odd != 0) {
+          if (lane == 0) odd_there[turn] = 1;
+          const uint64_t row_lanes = (kChunks == 64 ? ~0ull : (1ull << (kChunks % 64)) - 1) << (lane / kChunks * kChunks);
+          keep = keep && (odd & row_lanes) == 0;
+        }
+      }
+      return keep;
+    };
+    const u32x4 zero = {0, 0, 0, 0};
+
+    // kAny: the page id of the lane's key of a tile; then its row's place (bytes, -1: dead).
+    const auto key_of = [&](uint32_t t) { return t * kTile + kw * kKeys + lane % kKeys; };
     const auto id_of = [&](uint32_t t) {
       const uint32_t j = key_of(t);
       return t < t_end && j < sees ? ids[page_of(j)] : -1;
@@ -393,39 +448,92 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
       if (static_cast<uint32_t>(id) >= a.pages) return -1;
       return id * a.page_bytes + static_cast<int64_t>(j - page_of(j) * a.page_tokens) * a.token_bytes;
     };
-    u32x4 kr[kLoads], vr[kLoads];
-    const auto stage = [&](int64_t place) {
+    u32x4 kr[kAny ? kLoads : 1], vr[kAny ? kLoads : 1];
+    const auto fetch = [&](int64_t place) {
 #pragma unroll
-      for (uint32_t i = 0; i < kLoads; ++i) {
-        const uint32_t from = stage_row + i * (kWave / kChunks);
+      for (uint32_t i = 0; i < (kAny ? kLoads : 0); ++i) {
+        const uint32_t from = stage_row + load_row + i * kLoadRows;
         const int32_t lo = __shfl(static_cast<int32_t>(place), from, 64), hi = __shfl(static_cast<int32_t>(place >> 32), from, 64);
         const int64_t off = hi < 0 ? 0 : static_cast<int64_t>(hi) << 32 | static_cast<uint32_t>(lo);
-        kr[i] = load_chunk<T, kAny>(kp + off, stage_chunk * (16 / sizeof(T)), a.dim);
-        vr[i] = load_chunk<T, kAny>(vp + off, stage_chunk * (16 / sizeof(T)), a.dim);
+        kr[i] = load_chunk_of<T>(kp + off, load_chunk * (16 / sizeof(T)), a.dim);
+        vr[i] = load_chunk_of<T>(vp + off, load_chunk * (16 / sizeof(T)), a.dim);
       }
     };
-    // Into LDS, dead rows as zeros. A tile that not all rows see: rows of values with an infinity or a NaN as zeros too, and listed.
-    const auto put = [&](uint32_t t, uint32_t buffer, uint32_t list, uint64_t live) {
+    const auto put = [&](uint32_t t, uint32_t buffer, uint64_t live) {
       char* keys = own + buffer * F::kBufferBytes;
       char* values = keys + kKeys * kRowBytes;
-      const bool some = t * kTile + kTile > all_see;
+#pragma unroll
+      for (uint32_t i = 0; i < (kAny ? kLoads : 0); ++i) {
+        const uint32_t to = stage_row + load_row + i * kLoadRows;
+        *reinterpret_cast<u32x4*>(keys + to * kRowBytes + ((load_chunk ^ key_swizzle(to)) * 16)) = kr[i];
+        *reinterpret_cast<u32x4*>(values + to * kRowBytes + ((load_chunk ^ value_swizzle(to)) * 16)) = kept(t, to, live, vr[i]) ? vr[i] : zero;
+      }
+    };
+
+    // Else: the page ids of 64 sixteens of tokens at a time, one in each lane. Rows of an absent page are read from page 0,
+    // those behind the last token are inside their page.
+    int32_t lane_id = -1;
+    uint32_t lane_ids = ~0u;  // which 64 these are
+    const auto sixteen_of = [&](uint32_t t) { return t * (kTile / 16) + kw * (kKeys / 16); };
+    const auto page_at = [&](uint32_t sixteen) { return __builtin_amdgcn_readlane(lane_id, sixteen % 64); };
+    // Which keys of the tile are live; brings the ids along.
+    const auto live_of = [&](uint32_t t) -> uint64_t {
+      const uint32_t first = sixteen_of(t);
+      if (first / 64 != lane_ids) {
+        lane_ids = first / 64;
+        const uint32_t j = (lane_ids * 64 + lane) * 16;
+        lane_id = j < sees ? ids[page_of(j)] : -1;
+        asm volatile("s_waitcnt vmcnt(0)" : "+v"(lane_id));  // once in 64, not at every use
+      }
+      uint64_t live = 0;
+#pragma unroll
+      for (uint32_t k = 0; k < kKeys / 16; ++k) {
+        const uint32_t j = (first + k) * 16;
+        const bool there = static_cast<uint32_t>(page_at(first + k)) < a.pages && j < sees;
+        const uint32_t mask = !there ? 0u : sees - j >= 16 ? 0xFFFFu : (1u << (sees - j)) - 1;
+        live |= static_cast<uint64_t>(mask) << (16 * k);
+      }
+      return live;
+    };
+    // Bytes from the first row of a tensor to the wave's sixteen k of a tile.
+    const auto sixteen_at = [&](uint32_t t, uint32_t k) {
+      const uint32_t sixteen = sixteen_of(t) + k, j = sixteen * 16;
+      const uint32_t id = static_cast<uint32_t>(page_at(sixteen));
+      const bool there = id < a.pages;
+      const uint32_t page_row = a.page_shift >= 0 ? j & (a.page_tokens - 1) : j % a.page_tokens;
+      return static_cast<uint64_t>(there ? id : 0u) * static_cast<uint64_t>(a.page_bytes) + (there ? page_row : 0u) * static_cast<uint64_t>(a.token_bytes);
+    };
+    constexpr uint32_t kSixteens = (F::kStageRows + 15) / 16;  // that the wave's rows lie in
+    struct Places {
+      uint64_t at[kSixteens];
+    };
+    const auto places_of = [&](uint32_t t) {
+      Places p;
+#pragma unroll
+      for (uint32_t k = 0; k < kSixteens; ++k) p.at[k] = sixteen_at(t, stage_row / 16 + k);
+      return p;
+    };
+    const auto bring = [&](const char* from, const Places& p, char* to, auto swizzle) {
 #pragma unroll
       for (uint32_t i = 0; i < kLoads; ++i) {
-        const uint32_t to = stage_row + i * (kWave / kChunks);
-        bool keep = live >> to & 1;
-        const u32x4 zero = {0, 0, 0, 0};
-        *reinterpret_cast<u32x4*>(keys + to * kRowBytes + ((stage_chunk ^ (to & kKeyMask)) * 16)) = keep ? kr[i] : zero;
-        if (some) {
-          const uint64_t odd = __ballot(keep && odd_values<T>(vr[i]));
-          if (odd != 0) {
-            const uint64_t row_lanes = (kChunks == 64 ? ~0ull : (1ull << kChunks) - 1) << (lane / kChunks * kChunks);
-            if (odd & row_lanes) {
-              keep = false;
-              if (lane % kChunks == 0) atomicOr(&odd_keys[list][kw][to / 32], 1u << (to % 32));
-            }
-          }
-        }
-        *reinterpret_cast<u32x4*>(values + to * kRowBytes + ((stage_chunk ^ value_swizzle(to)) * 16)) = keep ? vr[i] : zero;
+        const uint32_t row = stage_row + i * kLoadRows;
+        const uint64_t base = reinterpret_cast<uint64_t>(from) + p.at[i * kLoadRows / 16] + (row % 16) * static_cast<uint64_t>(a.token_bytes);
+        const uint32_t offset = load_row * static_cast<uint32_t>(a.token_bytes) + ((load_chunk ^ swizzle(row + load_row)) * 16);
+        load_to_lds(lds_address(to) + row * kRowBytes, base, offset);
+      }
+    };
+    const auto bring_keys = [&](const Places& p, uint32_t buffer) { bring(kp, p, own + buffer * F::kBufferBytes, key_swizzle); };
+    const auto bring_values = [&](const Places& p, uint32_t buffer) {
+      bring(vp, p, own + buffer * F::kBufferBytes + kKeys * kRowBytes, value_swizzle);
+    };
+    // Empties rows of values that are in LDS.
+    const auto mend = [&](uint32_t t, uint32_t buffer, uint64_t live) {
+      if (live == kAll && !some_see(t)) return;
+      char* values = own + buffer * F::kBufferBytes + kKeys * kRowBytes;
+      for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t row = stage_row + load_row + i * kLoadRows;
+        u32x4* at_lds = reinterpret_cast<u32x4*>(values + row * kRowBytes + load_chunk * 16);
+        if (!kept(t, row, live, *at_lds)) *at_lds = zero;
       }
     };
     const auto ready = [&] {  // what is put is there for all that read it
@@ -445,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
 #pragma unroll
       for (uint32_t c = 0; c < kSteps; ++c) {
         q[c] = u32x4{0, 0, 0, 0};
-        if (mine) q[c] = load_chunk<T, kAny>(qp, (2 * c + g) * (16 / sizeof(T)), a.dim);
+        if (mine) q[c] = kAny ? load_chunk_of<T>(qp, (2 * c + g) * (16 / sizeof(T)), a.dim) : *reinterpret_cast<const u32x4_any*>(qp + (2 * c + g) * 16);
         if (a.scale < 0.0f) q[c] ^= kWide ? 0x80000000u : 0x80008000u;
       }
     }
@@ -457,47 +565,98 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
 #pragma unroll
     for (uint32_t e = 0; e < kOuts; ++e) o[e] = f32x16{};
 
-    if (lane == 0 && rw == 0)
-      for (uint32_t b = 0; b < 3; ++b) odd_keys[b][kw][0] = odd_keys[b][kw][1] = 0;
-    int64_t place = row_of(t_begin, id_of(t_begin));
-    uint64_t live = __ballot(place >= 0), live_next = 0;
-    stage(place);
-    int32_t id = id_of(t_begin + 1);
-    __syncthreads();  // the item before is done with the LDS, and the lists are empty
-    put(t_begin, 0, 0, live);
-    place = row_of(t_begin + 1, id);
-    live_next = __ballot(place >= 0);
+    int64_t place = -1;
+    int32_t id = -1;
+    uint64_t live, live_next = 0;
+    Places next;
+    if constexpr (kAny) {
+      place = row_of(t_begin, id_of(t_begin));
+      live = __ballot(place >= 0) & kAll;
+      fetch(place);
+      id = id_of(t_begin + 1);
+    } else {
+      live = live_of(t_begin);
+    }
+    __syncthreads();  // the item before is done with the LDS
+    if (threadIdx.x == 0) odd_there[turn ^ 1] = 0;
+    if constexpr (kAny) {
+      put(t_begin, 0, live);
+      place = row_of(t_begin + 1, id);
+      live_next = __ballot(place >= 0) & kAll;
+    } else {
+      next = places_of(t_begin);
+      bring_keys(next, 0);
+      bring_values(next, 0);
+      if constexpr (kRowWaves > 1) {
+        loads_left<0>();
+        mend(t_begin, 0, live);
+      }
+    }
     ready();
 
-    uint32_t buffer = 0, list = 0;
+    uint32_t buffer = 0;
     for (uint32_t t = t_begin; t < t_end; ++t) {
       const bool more = t + 1 < t_end;
-      const uint32_t next_list = list == 2 ? 0 : list + 1, empty_list = list == 0 ? 2 : list - 1;
-      if (lane == 0 && rw == 0) odd_keys[empty_list][kw][0] = odd_keys[empty_list][kw][1] = 0;
-      if (more) stage(place);
-      id = id_of(t + 2);
+      const uint32_t other = (buffer + 1) % F::kBuffers;
+      if constexpr (kAny) {
+        if (more) fetch(place);
+        id = id_of(t + 2);
+      } else {
+        if constexpr (kRowWaves > 1) {
+          if (more) {
+            live_next = live_of(t + 1);
+            next = places_of(t + 1);
+            bring_keys(next, other);
+            bring_values(next, other);
+          }
+        } else {
+          loads_left<kLoads>();  // the keys are there
+          ready();
+        }
+      }
       const uint32_t key0 = t * kTile + kw * kKeys;
-      if (key0 < wave_end) {
-        const char* keys = own + buffer * F::kBufferBytes;
-        const char* values = keys + kKeys * kRowBytes;
-        f32x16 x[kBlocks];
+      const bool use = key0 < wave_end;
+      const char* keys = own + buffer * F::kBufferBytes;
+      const char* values = keys + kKeys * kRowBytes;
+      f32x16 x[kBlocks];
+      if (use) {
+        u32x4 kf[kBlocks][kSteps];
+#pragma unroll
+        for (uint32_t b = 0; b < kBlocks; ++b)
+#pragma unroll
+          for (uint32_t c = 0; c < kSteps; ++c) kf[b][c] = *reinterpret_cast<const u32x4*>(keys + b * 32 * kRowBytes + (key_at ^ (c * 32)));
+        __builtin_amdgcn_sched_barrier(0);  // all reads on their way before the first product waits for one
 #pragma unroll
         for (uint32_t b = 0; b < kBlocks; ++b) {
           x[b] = f32x16{};
 #pragma unroll
           for (uint32_t c = 0; c < kSteps; ++c) {
-            const u32x4 kf = *reinterpret_cast<const u32x4*>(keys + b * 32 * kRowBytes + (key_at ^ (c * 32)));
             if constexpr (kWide) {
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[e]), __uint_as_float(q[c][e]), x[b], 0, 0, 0);
+                x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kf[b][c][e]), __uint_as_float(q[c][e]), x[b], 0, 0, 0);
             } else {
-              x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, q[c]), x[b], 0, 0, 0);
+              x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[b][c]), __builtin_bit_cast(bf16x8, q[c]), x[b], 0, 0, 0);
             }
           }
         }
-        const uint64_t wanted = kKeys == 64 ? ~0ull : (1ull << (kKeys % 64)) - 1;
-        const bool some = key0 + kKeys > wave_sees || (live & wanted) != wanted;
+      }
+      if constexpr (!kAny && kRowWaves == 1) {
+        asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the keys are read
+        ready();
+        if (more) {
+          live_next = live_of(t + 1);
+          next = places_of(t + 1);
+          bring_keys(next, 0);
+          loads_left<kLoads>();  // the values are there
+        } else {
+          loads_left<0>();
+        }
+        mend(t, 0, live);
+        ready();
+      }
+      if (use) {
+        const bool some = key0 + kKeys > wave_sees || live != kAll;
         uint32_t see[kBlocks];
         if (some) {
 #pragma unroll
@@ -526,6 +685,24 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
             for (int i = 0; i < 16; ++i) x[b][i] = shown >> (8 * (i / 4) + i % 4) & 1 ? x[b][i] : -INFINITY;
           }
         }
+        // the values' operands, on their way while the weights are computed
+        u32x4 vf[kWide ? 1 : kOuts][2];
+        const auto read_values = [&](uint32_t b) {
+          if constexpr (!kWide) {
+            typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+#pragma unroll
+            for (uint32_t e = 0; e < kOuts; ++e)
+#pragma unroll
+              for (uint32_t c = 0; c < 2; ++c) {
+                const char* from = values + (32 * b + 16 * c) * kRowBytes + (value_at ^ (e * 64));
+                const u32x2 v0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from));
+                const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 8 * kRowBytes)));
+                vf[e][c] = u32x4{v0.x, v0.y, v1.x, v1.y};
+              }
+          }
+        };
+        read_values(0);
+        __builtin_amdgcn_sched_barrier(0);
         float top = x[0][0];
 #pragma unroll
         for (uint32_t b = 0; b < kBlocks; ++b)
@@ -568,50 +745,77 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
               hi[i / 4][i % 4] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
               lo[i / 4][i % 4] = pack_bf16x2(p0 - __uint_as_float(b0 & 0xFFFF0000u), p1 - __uint_as_float(b1 & 0xFFFF0000u));
             }
+            if (b == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (uint32_t e = 0; e < kOuts; ++e)
 #pragma unroll
               for (uint32_t c = 0; c < 2; ++c) {
-                typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-                const char* from = vb + (value_at ^ (e * 64)) + 16 * c * kRowBytes;
-                const u32x2 v0 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)from));
-                const u32x2 v1 = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(from + 8 * kRowBytes)));
-                const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{v0.x, v0.y, v1.x, v1.y});
-                o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, hi[c]), o[e], 0, 0, 0);
-                o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, lo[c]), o[e], 0, 0, 0);
+                const bf16x8 v = __builtin_bit_cast(bf16x8, vf[e][c]);
+                o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, hi[c]), o[e], 0, 0, 0);
+                o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v, __builtin_bit_cast(bf16x8, lo[c]), o[e], 0, 0, 0);
               }
-          }
-          // values with an infinity or a NaN, one key at a time, for the rows that see it
-          if (t * kTile + kTile > all_see) {
-            for (uint32_t odd = uniform(odd_keys[list][kw][b]); odd != 0; odd &= odd - 1) {
-              const uint32_t key = static_cast<uint32_t>(__builtin_ctz(odd)), j = key0 + 32 * b + key;
-              float weight = 0.0f;
-#pragma unroll
-              for (uint32_t i = 0; i < 16; ++i)
-                if (i == key / 8 * 4 + key % 4) weight = p[i];
-              weight = __shfl(weight, r + 32 * (key / 4 % 2), 64);
-              const int32_t page = ids[page_of(j)];
-              if (static_cast<uint32_t>(page) >= a.pages || (some && !(see[b] >> key & 1))) continue;
-              const T* vrow = reinterpret_cast<const T*>(vp + page * a.page_bytes + static_cast<int64_t>(j - page_of(j) * a.page_tokens) * a.token_bytes);
-#pragma unroll
-              for (uint32_t e = 0; e < kOuts; ++e)
-#pragma unroll
-                for (uint32_t i = 0; i < 16; ++i) {
-                  const uint32_t dim = 32 * e + 8 * (i / 4) + 4 * g + i % 4;
-                  if (!kAny || dim < a.dim) o[e][i] += weight * S::load1(vrow + dim);
-                }
-            }
+            if (b + 1 < kBlocks) read_values(b + 1);
           }
         }
       }
-      if constexpr (F::kBuffers == 1) ready();  // with the tile
-      buffer = (buffer + 1) % F::kBuffers;
-      if (more) put(t + 1, buffer, next_list, live_next);
-      list = next_list;
-      live = live_next;
-      place = row_of(t + 2, id);
-      live_next = __ballot(place >= 0);
+      if constexpr (kAny) {
+        if constexpr (F::kBuffers == 1) ready();  // with the tile
+        if (more) put(t + 1, other, live_next);
+        place = row_of(t + 2, id);
+        live = live_next;
+        live_next = __ballot(place >= 0) & kAll;
+      } else {
+        if constexpr (kRowWaves > 1) {
+          loads_left<0>();
+          if (more) mend(t + 1, other, live_next);
+        } else {
+          asm volatile("s_waitcnt lgkmcnt(0)" : : : "memory");  // the values are read
+          ready();
+          if (more) bring_values(next, 0);
+        }
+        live = live_next;
+      }
+      buffer = other;
       ready();
+    }
+    if constexpr (kRowWaves == 1) __syncthreads();
+    // Values with an infinity or a NaN in tiles that only some rows see: one key at a time, for the rows that see it. Its score is
+    // in m and l already.
+    if (odd_there[turn] != 0) {
+      for (uint32_t t = t_begin; t < t_end; ++t) {
+        if (!some_see(t)) continue;
+        for (uint32_t j = t * kTile + kw * kKeys; j < min(t * kTile + (kw + 1) * kKeys, wave_end); ++j) {
+          const int32_t page = ids[page_of(j)];
+          if (static_cast<uint32_t>(page) >= a.pages) continue;
+          const int64_t at_row = page * a.page_bytes + static_cast<int64_t>(j - page_of(j) * a.page_tokens) * a.token_bytes;
+          const T* key = reinterpret_cast<const T*>(kp + at_row);
+          const T* value = reinterpret_cast<const T*>(vp + at_row);
+          bool odd = false;
+          for (uint32_t dim = lane; dim < a.dim; dim += kWave) {
+            const float v = S::load1(value + dim);
+            odd = odd || !(fabsf(v) <= 3.402823466e38f);
+          }
+          if (__ballot(odd) == 0) continue;
+          const int32_t e = static_cast<int32_t>(j) - static_cast<int32_t>(s.cached);
+          bool sees_it = mine && e < 0;
+          if (mine && e >= 0)
+            sees_it = a.seen == nullptr ? static_cast<uint32_t>(e) <= node
+                                        : static_cast<uint32_t>(e) / 64 < a.words &&
+                                              (a.seen[static_cast<int64_t>(s.token + node) * a.seen_stride + e / 64] >> (e % 64) & 1);
+          if (!sees_it) continue;
+          const T* query = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(s.token + node) * a.q_token + static_cast<int64_t>(q_head) * a.q_head;
+          float score = 0.0f;
+          for (uint32_t dim = 0; dim < a.dim; ++dim) score = __builtin_fmaf(S::load1(query + dim), S::load1(key + dim), score);
+          const float weight = __builtin_amdgcn_exp2f(__builtin_fmaf(a.scale < 0.0f ? -score : score, scale, -m));
+#pragma unroll
+          for (uint32_t c = 0; c < kOuts; ++c)
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) {
+              const uint32_t dim = 32 * c + 8 * (i / 4) + 4 * g + i % 4;
+              if (!kAny || dim < a.dim) o[c][i] += weight * S::load1(value + dim);
+            }
+        }
+      }
     }
     l += __shfl_xor(l, 32, 64);
 
@@ -719,7 +923,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
 
 template <class S, uint32_t kDim, uint32_t kRowWaves, bool kAny>
 int launch(Attend& a, hipStream_t st) {
-  typedef Form<S, kDim, kRowWaves> F;
+  typedef Form<S, kDim, kRowWaves, kAny> F;
   if (F::kLds > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_kernel<S, kDim, kRowWaves, kAny>), hipFuncAttributeMaxDynamicSharedMemorySize,
                           F::kLds) != hipSuccess)
@@ -742,15 +946,15 @@ int rows(Attend& a, uint32_t row_waves, hipStream_t st) {
 
 template <class S>
 int attend(Attend& a, uint32_t row_waves, hipStream_t st) {
-  switch (a.dim) {
-    case 64: return rows<S, 64, false>(a, row_waves, st);
-    case 128: return rows<S, 128, false>(a, row_waves, st);
-    case 256: return rows<S, 256, false>(a, row_waves, st);
-    default:
-      if (a.dim < 64) return rows<S, 64, true>(a, row_waves, st);
-      if (a.dim < 128) return rows<S, 128, true>(a, row_waves, st);
-      return rows<S, 256, true>(a, row_waves, st);
-  }
+  // pages of whole sixteens, in which 32-bit offsets reach every row, at vectors' addresses
+  const uint64_t places = reinterpret_cast<uint64_t>(a.k) | reinterpret_cast<uint64_t>(a.v) | a.page_bytes | a.head_bytes | a.token_bytes;
+  const bool fast = a.page_tokens % 16 == 0 && places % 16 == 0 && a.token_bytes < (int64_t{1} << 28);
+  if (fast && a.dim == 64) return rows<S, 64, false>(a, row_waves, st);
+  if (fast && a.dim == 128) return rows<S, 128, false>(a, row_waves, st);
+  if (fast && a.dim == 256) return rows<S, 256, false>(a, row_waves, st);
+  if (a.dim <= 64) return rows<S, 64, true>(a, row_waves, st);
+  if (a.dim <= 128) return rows<S, 128, true>(a, row_waves, st);
+  return rows<S, 256, true>(a, row_waves, st);
 }
 
 }  // namespace
