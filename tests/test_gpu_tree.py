@@ -3,8 +3,11 @@
 Tolerances follow from the arithmetic, with e = 2^-24 (half an fp32 ulp, relative). A score is a sum of dim products and one scaling, off
 by at most (dim + 8) e of its products' magnitudes, which moves each weight by that share, twice (weight and sum). The
 weighted sum adds a rounding for each 16 keys and each of a bf16 weight's two parts, a rescaling and a join now and
-then: below keys / 8 + 64. bf16 weights are two parts of 8 bits each (2^-16 of the weight, 2^8 e), a bf16 output adds half a
-bf16 ulp. Whole numbers and moved rows are equal.
+then: below keys / 8 + 64. bf16 weights are two parts of 8 bits each (2^-16 of the weight, 2^8 e); with more than 32 rows (a new
+token and a query head of a key head's) a sequence, and heads of 64 or 128, they are rounded once and divided by the sum of the rounded
+ones: with w' = w (1 + d), |d| <= 2^-8, sum w' v / sum w' - sum w v / sum w = sum w d (v - out) / sum w', below 2^-8 (1 + 2^-7) times
+(sum w |v| / sum w + |out|), so below 2.1 times 2^-8 of the weighted magnitudes, 2.1 2^16 e (and log sum' - log sum below 2.1 2^-8). A
+bf16 output adds half a bf16 ulp. Whole numbers and moved rows are equal.
 """
 
 import numpy as np
@@ -47,9 +50,10 @@ def near(got, want, magnitude, steps, dtype):
     assert worst <= 1.0, f"off by {worst:.2f} of what rounding allows"
 
 
-def bound(dim, keys, big, dtype):
-    """Steps of rounding behind an output, relative to the weighted magnitudes of the values."""
-    return 2 * (dim + 8) * big + keys / 8 + 64 + (2.0 ** 8 if dtype == "bf16" else 0)
+def bound(dim, keys, big, dtype, rows):
+    """Steps of rounding behind an output, relative to the weighted magnitudes of the values. rows: of a sequence, on average."""
+    once = rows > 32 and dim in (64, 128)
+    return 2 * (dim + 8) * big + keys / 8 + 64 + (0 if dtype == "f32" else 2.1 * 2.0 ** 16 if once else 2.0 ** 8)
 
 
 def trees(counts, seed, roots=0.05):
@@ -196,10 +200,10 @@ def attend_case(cached, counts, hq, hk, dim, page, layout, dtype, room=400):
     return q, kc, vc, table, used
 
 
-def check(got, sums, want, dim, keys, dtype):
+def check(got, sums, want, dim, keys, dtype, rows):
     out, lse, mag, big = want
     there = ~np.isnan(lse)
-    steps = bound(dim, keys, big, dtype)
+    steps = bound(dim, keys, big, dtype, rows)
     near(got[dev(there)], out[there].reshape(-1, dim), mag[there].reshape(-1, dim), steps[there].reshape(-1, 1), dtype)
     sums = wide(sums)
     assert np.array_equal(np.isneginf(sums[there]), np.isneginf(lse[there]))
@@ -227,7 +231,7 @@ def test_attend(case, kind, dtype):
     spoil(kc, vc, table, used, page)
     args = (q, kc, vc, dev(table), ints(cached), dev(starts), None if seen is None else dev(seen), scale)
     out, sums = zo.zo_tree_attend(*args, lse=True)
-    check(out, sums, want, dim, 3100, dtype)
+    check(out, sums, want, dim, 3100, dtype, n * hq / hk / len(counts))
     assert torch.equal(out, zo.zo_tree_attend(*args))
 
 
@@ -244,7 +248,7 @@ def test_attend_many_sequences(seqs, dtype):
     want = oracle.attend(wide(q), wide(kc), wide(vc), table, cached, starts, None, 0.125)
     spoil(kc, vc, table, used, 16)
     out, sums = zo.zo_tree_attend(q, kc, vc, dev(table), dev(cached.astype(np.int32)), dev(starts), lse=True)
-    check(out, sums, want, 64, 360, dtype)
+    check(out, sums, want, 64, 360, dtype, counts.sum() * 2 / seqs)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -261,7 +265,7 @@ def test_attend_absent_pages(page, dim, nodes, dtype):
     want = oracle.attend(wide(q), wide(kc), wide(vc), table, cached, starts, None, 0.2)
     spoil(kc, vc, table, [0 if s == 2 else c + n for s, (c, n) in enumerate(zip(cached, counts))], page)
     out, sums = zo.zo_tree_attend(q, kc, vc, dev(table), ints(cached), dev(starts), scale=0.2, lse=True)
-    check(out, sums, want, dim, 400, dtype)
+    check(out, sums, want, dim, 400, dtype, 2 * nodes)
     assert not out[2 * nodes:3 * nodes].any() and bool(torch.isneginf(sums[2 * nodes:3 * nodes]).all())
 
 
@@ -297,8 +301,9 @@ def test_values_reach_the_rows_that_see_them(dim, page, nodes, dtype):
                     assert bool((row[:, 5] == -inf).all())
                 rest = [d for d in range(dim) if not (d in (3, 4) and sees or d == 5 and s == 0)]
                 assert bool(torch.isfinite(row[:, rest]).all())
-                # where a value is added by itself the sum has another order: the rounding of a few terms
-                assert float((row[:, rest].float() - plain[t][:, rest].float()).abs().max()) <= (0.02 if dtype == "bf16" else 1e-4)
+                # where a value is added by itself the sum has another order, and its weight is not rounded to bf16: off by 2^-8 of values
+                # below 5 at the most, and by both results' rounding
+                assert float((row[:, rest].float() - plain[t][:, rest].float()).abs().max()) <= (0.04 if dtype == "bf16" else 1e-4)
         # a key that is not a number: its own rows alone
         k[at(0, cached[0] + bad[0])][..., 0] = nan
         out = zo.zo_tree_attend(q, k, vc, dt, dl, ds, masks)
@@ -340,7 +345,7 @@ def test_attend_leaves_other_rows():
         want = oracle.attend(wide(q), wide(kc), wide(vc), table.cpu().numpy(), [5, 17, 0, 33], starts, None, 128 ** -0.5)
         there = ~np.isnan(want[1][:, 0])
         assert torch.equal(out[dev(~there)], torch.full_like(out[dev(~there)], 7.0)) and bool((buffer[:, 0] == 7.0).all())
-        steps = bound(128, 50, want[3], "bf16")
+        steps = bound(128, 50, want[3], "bf16", 12 * 2 / 4)
         near(out[dev(there)], want[0][there], want[2][there], steps[there][..., None], "bf16")
 
 
@@ -371,8 +376,8 @@ def test_attend_long_prompt(dim):
             w = torch.softmax(x, 0)
             want, mag = w @ v[h // 2, :live], w @ v[h // 2, :live].abs()
             big = float((k[h // 2, :live].abs() @ q[i, h].double().abs()).max()) * dim ** -0.5
-            near(out[i, h], wide(want), wide(mag), bound(dim, live, big, "bf16"), "bf16")
-            assert abs(float(sums[i, h]) - float(torch.logsumexp(x, 0))) <= bound(dim, live, big, "bf16") * E + 1e-5
+            near(out[i, h], wide(want), wide(mag), bound(dim, live, big, "bf16", n), "bf16")
+            assert abs(float(sums[i, h]) - float(torch.logsumexp(x, 0))) <= bound(dim, live, big, "bf16", n) * E + 1e-5
 
 
 def test_attend_far_pages():
