@@ -458,7 +458,6 @@ TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t 
   s.row_waves = rows <= 32 && own_tiles ? 1 : 4;
   s.rows = 32 * s.row_waves;
   s.workers = dim * elem_bytes(dtype) <= 256 ? 512 : 256;
-  s.items = (tokens * group / s.rows + seqs) * heads;
   return s;
 }
 
@@ -491,13 +490,13 @@ int check_tree_attend(const zo_tree_attention& a) {
 
 extern "C" {
 
-// A word for the count of items, the items' whereabouts, and two parts for each worker (of the items that its run begins and ends
-// in): for every row a maximum, a sum and a row of fp32.
+// A word for the workers that have tiles; for each of them where a split item's parts are, and two parts (of the items that its run
+// begins and ends in): for every row a maximum, a sum and a row of fp32.
 uint64_t zo_tree_attend_work(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim, int32_t dtype) {
   if (dim == 0 || dim > ZO_DIM_MAX || (dtype != ZO_F32 && dtype != ZO_BF16)) return 0;
   const zo::TreeShape s = zo::tree_shape(tokens, seqs, q_heads, heads, dim, dtype);
   const uint64_t row = (dim + 3) / 4 * 4 + 4;
-  return 16 + s.items * zo::kTreeItemWords * 4 + 2ull * s.workers * s.rows * row * sizeof(float);
+  return 16 + s.workers * (zo::kTreeSplitWords * 4 + 2ull * s.rows * row * sizeof(float));
 }
 
 uint64_t zo_norm_rotate_back_work(uint32_t tokens, uint32_t q_heads, uint32_t k_heads, uint32_t dim) {

@@ -37,14 +37,13 @@ uint32_t back_blocks(uint32_t tokens, uint32_t heads);
 uint64_t attend_items_bytes(uint32_t seqs, uint32_t q_heads, uint32_t heads);  // the parts' whereabouts
 uint32_t attend_workers(uint32_t dim);  // at most
 
-// zo_tree_attend: rows (a new token, a query head of a key head's group) of an item, waves that hold them, workgroups among which the
-// tiles are split (at most), and the most items of a call.
+// zo_tree_attend: rows (a new token, a query head of a key head's group) of an item, waves that hold them, and workgroups among which the
+// tiles are split (at most).
 struct TreeShape {
   uint32_t row_waves, rows, workers;
-  uint64_t items;
 };
 TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t heads, uint32_t dim, int32_t dtype);
-constexpr uint32_t kTreeItemWords = 8;  // of 4 bytes: where an item's parts are
+constexpr uint32_t kTreeSplitWords = 8;  // of 4 bytes: where a split item's parts are
 
 // zo_draw_split: tokens of a workgroup's part, and words of 8 bytes that a part and a row keep.
 constexpr uint32_t kDrawPart = 4096, kDrawPartWords = 4074, kDrawRowWords = 2;

@@ -41,27 +41,28 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t kThreads = 256, kWave = 64, kWaves = kThreads / kWave, kXcds = 8;
 constexpr float kLazy = 8.0f;  // how far (in powers of two) the bound of the scores is set above their maximum
 
-// Where an item's parts are, written by the workgroup of its last tile: those of workgroups first .. last, the first one's in
-// slot first_slot % 2, the others' in slot 0; first = last: that workgroup wrote the output.
-struct Item {
-  uint32_t first_slot, last;
+// An item that was split: its parts are those of the workgroup that this is the entry of, in slot `slot`, and of the ones up to `last`, in
+// slot 0. At most one item that is split begins in a workgroup's run. last = 0: none does. Written by the workgroup of the item's last
+// tile, or by the entry's own workgroup where none is split.
+struct Split {
+  uint32_t last, slot;
   uint32_t token, row, rows, head;  // the sequence's first new token; the item's first row and their number; key head
   uint32_t unused[2];
 };
-static_assert(sizeof(Item) == kTreeItemWords * 4, "the workspace holds items of this size");
+static_assert(sizeof(Split) == kTreeSplitWords * 4, "the workspace holds entries of this size");
 
 struct Attend {
   const char *q, *k, *v;
   char* out;
   float* lse;
-  uint32_t* item_count;
-  Item* items;
+  uint32_t* active;  // workgroups that have tiles
+  Split* splits;
   float* parts;
   const int32_t *ids, *lengths, *starts;
   const uint64_t* seen;
   int64_t seen_stride, q_token, q_head, out_token, out_head, page_bytes, head_bytes, token_bytes, table_stride;
   double inv_group;
-  uint32_t most_items, tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row;
+  uint32_t tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row;
   int32_t page_shift;  // of a page's tokens where they are a power of two, else -1
   float scale;         // times log2(e)
 };
@@ -141,24 +142,23 @@ __device__ uint64_t head_tiles(const Attend& a, const Seq& s, uint32_t lane) {
   return uniform(__shfl(sums_upto(mine, lane), 63, 64));
 }
 
-// Tiles and items before each thread's sequences. Thread t counts sequences [t each, (t + 1) each).
+// Tiles before each thread's sequences. Thread t counts sequences [t each, (t + 1) each).
 struct Deal {
   uint64_t total;
-  uint32_t items, each;
+  uint32_t each;
 };
 
 template <uint32_t kRows, uint32_t kTile>
-__device__ Deal deal(const Attend& a, uint64_t* before, uint32_t* items_before) {
-  __shared__ uint64_t wave_tiles[kWaves], wave_items[kWaves];
+__device__ Deal deal(const Attend& a, uint64_t* before) {
+  __shared__ uint64_t wave_tiles[kWaves];
   const uint32_t lane = threadIdx.x % kWave;
   Deal d;
   d.each = (a.seqs + kThreads - 1) / kThreads;
-  uint64_t tiles = 0, items = 0;
+  uint64_t tiles = 0;
   for (uint32_t i = 0; i < d.each; ++i) {
     const uint32_t seq = threadIdx.x * d.each + i;
     Seq s = {};
     if (seq < a.seqs) s = seq_of<kRows>(a, seq);
-    items += s.blocks;
     constexpr uint32_t kFew = 8;  // blocks that a thread counts by itself; a longer sequence's by the whole wave
     if (a.seen) {
       if (s.blocks) tiles += static_cast<uint64_t>(s.blocks) * tiles_of<kRows, kTile>(a, s, 0);
@@ -178,26 +178,16 @@ __device__ Deal deal(const Attend& a, uint64_t* before, uint32_t* items_before) 
       }
     }
   }
-  const uint64_t tiles_upto = sums_upto(tiles, lane), items_upto = sums_upto(items, lane);
-  if (lane == 63) {
-    wave_tiles[threadIdx.x / kWave] = tiles_upto;
-    wave_items[threadIdx.x / kWave] = items_upto;
-  }
+  const uint64_t upto = sums_upto(tiles, lane);
+  if (lane == 63) wave_tiles[threadIdx.x / kWave] = upto;
   __syncthreads();
-  uint64_t tiles_at = 0, tiles_all = 0, items_at = 0, items_all = 0;
+  uint64_t at = 0, all = 0;
   for (uint32_t w = 0; w < kWaves; ++w) {
-    if (w < threadIdx.x / kWave) {
-      tiles_at += wave_tiles[w];
-      items_at += wave_items[w];
-    }
-    tiles_all += wave_tiles[w];
-    items_all += wave_items[w];
+    if (w < threadIdx.x / kWave) at += wave_tiles[w];
+    all += wave_tiles[w];
   }
-  before[threadIdx.x] = (tiles_at + tiles_upto - tiles) * a.heads;
-  const uint64_t item = (items_at + items_upto - items) * a.heads;
-  items_before[threadIdx.x] = static_cast<uint32_t>(item < a.most_items ? item : a.most_items);
-  d.total = uniform(tiles_all * a.heads);
-  d.items = uniform(static_cast<uint32_t>(items_all * a.heads < a.most_items ? items_all * a.heads : a.most_items));
+  before[threadIdx.x] = (at + upto - tiles) * a.heads;
+  d.total = uniform(all * a.heads);
   __syncthreads();
   return d;
 }
@@ -225,11 +215,14 @@ __device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint
   return a.parts + (static_cast<size_t>(worker) * 2 + slot) * kRows * a.part_row;
 }
 
+// Whether a row with the sum l of weights saw anything (a NaN among its scores counts).
+__device__ __forceinline__ bool any_seen(float l) { return l > 0.0f || l != l; }
+
 // Four dims of a row's output from its sums, and its log-sum once.
 template <class S>
 __device__ __forceinline__ void write_row(const Attend& a, uint32_t token, uint32_t q_head, uint32_t dim, float m, float l, f32x4 o) {
   typedef typename S::storage T;
-  const bool any = l > 0.0f || l != l;
+  const bool any = any_seen(l);
   T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(token) * a.out_token + static_cast<int64_t>(q_head) * a.out_head;
 #pragma unroll
   for (uint32_t i = 0; i < 4; ++i)
@@ -304,7 +297,6 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   constexpr uint32_t kTile = F::kTile, kLoads = F::kLoads, kLoadRows = F::kLoadRows, kOuts = kDim / 32, kSteps = kChunks / 2;
   extern __shared__ __align__(16) char lds[];
   __shared__ uint64_t before[kThreads];
-  __shared__ uint32_t items_before[kThreads];
   __shared__ uint32_t odd_there[2];  // odd values in this item's tiles, and emptied for the next item's
   __shared__ float2 merge_sums[2][32];
 
@@ -314,11 +306,11 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   uint32_t workers;
   {
     const Attend a = arguments();
-    d = deal<kRows, kTile>(a, before, items_before);
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.item_count = d.items;
+    d = deal<kRows, kTile>(a, before);
     workers = a.workers;
   }
   const Runs runs(d.total, workers);
+  if (blockIdx.x == 0 && threadIdx.x == 0) *arguments().active = d.total > 0 ? runs.workers : 0;
   // neighbouring runs on one XCD: workgroup b runs on XCD b % 8
   const uint32_t per_xcd = (runs.workers + kXcds - 1) / kXcds;
   const uint32_t slot_of = blockIdx.x / kXcds, worker = blockIdx.x % kXcds * per_xcd + slot_of;
@@ -328,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   if (at >= end) return;
 
   // the sequence, key head and block that tile `at` lies in
-  uint32_t seq, head, block, item;
+  uint32_t seq, head, block;
   uint64_t item_first;
   Seq s;
   {
@@ -339,14 +331,12 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
       if (before[chunk + step] <= at) chunk += step;
     chunk = uniform(chunk);
     seq = chunk * d.each;
-    item = uniform(items_before[chunk]);
     uint64_t first = uniform(before[chunk]), tiles;
     for (;; ++seq) {  // `at` < the total: a sequence holds it
       s = uniform(seq_of<kRows>(a, seq));
       tiles = s.blocks ? head_tiles<kRows, kTile>(a, s, lane) : 0;
       if (at < first + tiles * a.heads) break;
       first += tiles * a.heads;
-      item += s.blocks * a.heads;
     }
     head = uniform(static_cast<uint32_t>(quotient(at - first, tiles)));
     first += tiles * head;
@@ -371,7 +361,6 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
         rest -= all;
       }
     }
-    item = uniform(min(item + head * s.blocks + block, a.most_items));
     item_first = uniform(item_first);
     block = uniform(block);
   }
@@ -495,14 +484,16 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
         *at_lds = kept;
       }
     };
+    const auto ready_wave = [&] {  // what the wave put is there for its lanes: its LDS accesses are carried out in order
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    };
     const auto ready = [&] {  // what is put is there for all that read it
       if constexpr (kRowWaves > 1)
         __syncthreads();
-      else {  // the wave itself, whose LDS accesses are carried out in order
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-      }
+      else
+        ready_wave();
     };
 
     // queries: dims 16 s + 8 g .. + 7 (bf16), 8 s + 4 g .. + 3 (fp32) of the lane's row, negated for a negative scale
@@ -924,25 +915,66 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
     }
 
     const bool whole = t_begin == 0 && t_end == tiles;
-    if (t_end == tiles && threadIdx.x == 0 && item < a.most_items) {
-      const uint32_t first = t_begin == 0 ? worker : runs.worker_of(item_first);
-      const uint32_t slot = runs.first(first) == item_first ? 0 : 1;
-      a.items[item] = Item{2 * first + slot, worker, s.token, row0, in_block, head, {0, 0}};
+    if (threadIdx.x == 0) {
+      if (t_end == tiles && !whole) {  // so it began in another run
+        const uint32_t first = runs.worker_of(item_first);
+        a.splits[first] = Split{worker, runs.first(first) == item_first ? 0u : 1u, s.token, row0, in_block, head, {0, 0}};
+      }
+      // at the run's end: unless an item goes on that began in it
+      const uint64_t item_end = item_first + tiles;
+      if (item_end == end || (item_end > end && item_first < begin)) a.splits[worker].last = 0;
     }
-    if (kw == 0 && mine) {
-      float* part = part_at<kRows>(a, worker, at == begin ? 0 : 1) + static_cast<size_t>(rw * 32 + r) * a.part_row;
-      if (!whole && g == 0) *reinterpret_cast<float2*>(part) = make_float2(m, l);
+    if (a.lse && whole && kw == 0 && mine && g == 0)
+      a.lse[static_cast<size_t>(s.token + node) * a.heads * a.group + q_head] = any_seen(l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    if constexpr (kRowWaves > 1) __syncthreads();  // the last tile is read
+    // Results through LDS, for whole lines: rows of kPass dims, swizzled by 16 bytes; then each lane takes 16 bytes of a row of the output.
+    if (kw == 0 && wave_rows) {
+      constexpr uint32_t kRoom = F::kLds / (kRowWaves * 32 * 4), kPass = kDim < kRoom ? kDim : kRoom;
+      constexpr uint32_t kQuads = kPass / 4;
+      float* rest = reinterpret_cast<float*>(lds) + rw * 32 * kPass;
+      const float by = !whole ? 1.0f : any_seen(l) ? 1.0f / l : 0.0f;
+      const bool none = whole && !any_seen(l);
+      float* parts = part_at<kRows>(a, worker, at == begin ? 0 : 1) + static_cast<size_t>(rw * 32) * a.part_row;
+      if (!whole && g == 0) *reinterpret_cast<float2*>(parts + static_cast<size_t>(r) * a.part_row) = make_float2(m, l);
 #pragma unroll
-      for (uint32_t e = 0; e < kOuts; ++e)
+      for (uint32_t pass = 0; pass < kDim / kPass; ++pass) {
 #pragma unroll
-        for (uint32_t i = 0; i < 16; i += 4) {
-          const uint32_t dim = 32 * e + 2 * i + 4 * g;
-          const f32x4 four = {o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]};
-          if (whole)
-            write_row<S>(a, s.token + node, q_head, dim, m, l, four);
-          else
-            *reinterpret_cast<f32x4*>(part + 4 + dim) = four;
+        for (uint32_t e = 0; e < kPass / 32; ++e)
+#pragma unroll
+          for (uint32_t i = 0; i < 16; i += 4) {
+            const f32x16& from = o[pass * (kPass / 32) + e];
+            f32x4 four = {from[i], from[i + 1], from[i + 2], from[i + 3]};
+            four = none ? f32x4{0, 0, 0, 0} : four * by;
+            const uint32_t quad = 8 * e + i / 2 + g;
+            *reinterpret_cast<f32x4*>(rest + r * kPass + (quad ^ r % kQuads) * 4) = four;
+          }
+        ready_wave();
+        const uint32_t wave_count = min(32u, in_block - rw * 32);
+        constexpr uint32_t kTake = kWide ? 1 : 2;  // quads of a lane's 16 bytes
+        if (whole) {
+          constexpr uint32_t kLanes = kQuads / kTake;  // of a row
+          for (uint32_t i = lane / kLanes; i < wave_count; i += kWave / kLanes) {
+            const uint32_t quad = lane % kLanes * kTake, out_row = row0 + rw * 32 + i, out_node = node_of(a, out_row);
+            float v[4 * kTake];
+#pragma unroll
+            for (uint32_t n = 0; n < kTake; ++n) {
+              const f32x4 four = *reinterpret_cast<const f32x4*>(rest + i * kPass + ((quad + n) ^ i % kQuads) * 4);
+#pragma unroll
+              for (uint32_t d4 = 0; d4 < 4; ++d4) v[4 * n + d4] = four[d4];
+            }
+            T* to = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + out_node) * a.out_token +
+                    static_cast<int64_t>(head * a.group + out_row - out_node * a.group) * a.out_head + pass * kPass + quad * 4;
+            *reinterpret_cast<u32x4_any*>(to) = S::pack(v);
+          }
+        } else {
+          for (uint32_t i = lane / kQuads; i < wave_count; i += kWave / kQuads) {
+            const uint32_t quad = lane % kQuads;
+            *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + pass * kPass + quad * 4) =
+                *reinterpret_cast<const f32x4*>(rest + i * kPass + (quad ^ i % kQuads) * 4);
+          }
         }
+        ready_wave();
+      }
     }
     // Infinities and NaN in tiles that only some rows see, to the results of the rows that see them. (The waves have passed a barrier
     // since the last one was found.)
@@ -980,7 +1012,6 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
     at = item_first + t_end;
     if (t_end == tiles) {
       item_first += tiles;
-      if (item < a.most_items) ++item;
       if (++block == s.blocks) {
         block = 0;
         if (++head == a.heads) {
@@ -994,32 +1025,30 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   }
 }
 
-// Joins the parts of items that were split. A workgroup takes every gridDim.x-th item; a thread has four dims of a row.
+// Joins the parts of the items that were split: a workgroup has a share of one's rows, a thread four dims of a row at a time.
 template <class S, uint32_t kRows>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
-  const uint32_t items = *a.item_count, quads = (a.dim + 3) / 4;
-  for (uint32_t i = blockIdx.x; i < items; i += gridDim.x) {
-    const Item it = a.items[i];
-    const uint32_t first = it.first_slot / 2, slot = it.first_slot & 1;
-    if (it.last == first) continue;
-    for (uint32_t e = blockIdx.y * kThreads + threadIdx.x; e < it.rows * quads; e += gridDim.y * kThreads) {
-      const uint32_t row = e / quads, dim = (e - row * quads) * 4;
-      float m = -INFINITY, l = 0.0f;
-      f32x4 o = {0, 0, 0, 0};
+  if (blockIdx.x >= *a.active) return;
+  const Split it = a.splits[blockIdx.x];
+  if (it.last == 0) return;
+  const uint32_t quads = (a.dim + 3) / 4, first = blockIdx.x;
+  for (uint32_t e = blockIdx.y * kThreads + threadIdx.x; e < it.rows * quads; e += gridDim.y * kThreads) {
+    const uint32_t row = e / quads, dim = (e - row * quads) * 4;
+    float m = -INFINITY, l = 0.0f;
+    f32x4 o = {0, 0, 0, 0};
 #pragma unroll 4
-      for (uint32_t w = first; w <= it.last; ++w) {
-        const float* part = part_at<kRows>(a, w, w == first ? slot : 0) + static_cast<size_t>(row) * a.part_row;
-        const float2 ml = *reinterpret_cast<const float2*>(part);
-        const f32x4 po = *reinterpret_cast<const f32x4*>(part + 4 + dim);
-        const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.0f : top;
-        const float s0 = __builtin_amdgcn_exp2f(m - ref), s1 = __builtin_amdgcn_exp2f(ml.x - ref);
-        l = l * s0 + ml.y * s1;
-        o = o * s0 + po * s1;
-        m = top;
-      }
-      const uint32_t node = node_of(a, it.row + row);
-      write_row<S>(a, it.token + node, it.head * a.group + it.row + row - node * a.group, dim, m, l, o);
+    for (uint32_t w = first; w <= it.last; ++w) {
+      const float* part = part_at<kRows>(a, w, w == first ? it.slot : 0) + static_cast<size_t>(row) * a.part_row;
+      const float2 ml = *reinterpret_cast<const float2*>(part);
+      const f32x4 po = *reinterpret_cast<const f32x4*>(part + 4 + dim);
+      const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.0f : top;
+      const float s0 = __builtin_amdgcn_exp2f(m - ref), s1 = __builtin_amdgcn_exp2f(ml.x - ref);
+      l = l * s0 + ml.y * s1;
+      o = o * s0 + po * s1;
+      m = top;
     }
+    const uint32_t node = node_of(a, it.row + row);
+    write_row<S>(a, it.token + node, it.head * a.group + it.row + row - node * a.group, dim, m, l, o);
   }
 }
 
@@ -1130,8 +1159,7 @@ int launch(Attend& a, hipStream_t st) {
   attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(kThreads), F::kLds, st>>>(a);
   const int rc = launched();
   if (rc != ZO_OK) return rc;
-  const uint32_t parts = std::max(1u, std::min(16u, F::kRows * ((a.dim + 3) / 4) / kThreads));
-  join_kernel<S, F::kRows><<<dim3(std::min(a.most_items, 1024u), parts), dim3(kThreads), 0, st>>>(a);
+  join_kernel<S, F::kRows><<<dim3(a.workers, std::max(1u, F::kRows * kDim / 4096)), dim3(kThreads), 0, st>>>(a);
   return launched();
 }
 
@@ -1174,9 +1202,9 @@ extern "C" int zo_tree_attend(const zo_tree_attention* p, void* stream) {
   a.out = static_cast<char*>(p->out.data);
   a.lse = p->lse;
   char* work = static_cast<char*>(p->work);
-  a.item_count = reinterpret_cast<uint32_t*>(work);
-  a.items = reinterpret_cast<Item*>(work + 16);
-  a.parts = reinterpret_cast<float*>(work + 16 + shape.items * sizeof(Item));
+  a.active = reinterpret_cast<uint32_t*>(work);
+  a.splits = reinterpret_cast<Split*>(work + 16);
+  a.parts = reinterpret_cast<float*>(work + 16 + shape.workers * sizeof(Split));
   a.ids = p->table.ids;
   a.lengths = p->lengths;
   a.starts = p->starts;
@@ -1192,7 +1220,6 @@ extern "C" int zo_tree_attend(const zo_tree_attention* p, void* stream) {
   a.table_stride = p->table.stride;
   a.group = p->q_heads / p->cache.heads;
   a.inv_group = 1.0 / a.group;
-  a.most_items = static_cast<uint32_t>(shape.items);
   a.tokens = p->tokens;
   a.words = p->words;
   a.seqs = p->table.seqs;

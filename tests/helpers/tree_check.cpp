@@ -154,24 +154,18 @@ void other_refusals() {
   CHECK(moves([&](zo_tree_moves& x) { x.tensors = none; x.n_tensors = 2; }) == ZO_ERR_NULL);
 }
 
-// The most items that a call is given room for hold those of every split of its tokens over its sequences.
-void item_bounds() {
+// The workspace holds an entry and two parts of all rows for each workgroup.
+void workspace() {
   std::mt19937 rng(1);
   for (int round = 0; round < 20000; ++round) {
-    const uint32_t seqs = 1 + rng() % 9, heads = 1 + rng() % 4, group = 1 + rng() % 20;
+    const uint32_t seqs = 1 + rng() % 9, heads = 1 + rng() % 4, group = 1 + rng() % 20, tokens = 1 + rng() % (rng() % 3 ? 20 : 500);
     const uint32_t dim = 1 + rng() % ZO_DIM_MAX;
     const int32_t dtype = rng() % 2 ? ZO_BF16 : ZO_F32;
-    std::vector<uint32_t> counts(seqs);
-    uint32_t tokens = 0;
-    for (uint32_t& c : counts) tokens += c = rng() % (rng() % 3 ? 20 : 500);
-    if (tokens == 0) continue;
     const zo::TreeShape s = zo::tree_shape(tokens, seqs, heads * group, heads, dim, dtype);
-    uint64_t items = 0;
-    for (uint32_t c : counts) items += (uint64_t{c} * group + s.rows - 1) / s.rows * heads;
-    CHECK(items <= s.items && s.rows == 32 * s.row_waves);
+    CHECK(s.rows == 32 * s.row_waves && s.workers > 0 && s.workers % 8 == 0);
     const uint64_t row = (dim + 3) / 4 * 4 + 4;
     CHECK(zo_tree_attend_work(tokens, seqs, heads * group, heads, dim, dtype) ==
-          16 + s.items * zo::kTreeItemWords * 4 + 2 * uint64_t{s.workers} * s.rows * row * 4);
+          16 + s.workers * (zo::kTreeSplitWords * 4 + 2 * uint64_t{s.rows} * row * 4));
   }
   CHECK(zo_tree_attend_work(1, 1, 3, 2, 64, ZO_F32) == 16 && zo_tree_attend_work(1, 1, 2, 2, 257, ZO_F32) == 0);
 }
@@ -235,7 +229,7 @@ void cuts() {
 int main() {
   attention_refusals();
   other_refusals();
-  item_bounds();
+  workspace();
   cuts();
   std::printf("tree_check ok\n");
 }
