@@ -455,9 +455,9 @@ TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t 
   const uint64_t group = q_heads / heads, rows = (tokens * group + seqs - 1) / seqs;  // of a sequence, on average
   // keys and values of four waves' own tiles have to fit the LDS
   const bool own_tiles = dim * elem_bytes(dtype) <= 512;
-  s.row_waves = rows <= 32 && own_tiles ? 1 : 4;
+  s.row_waves = rows <= 32 && own_tiles ? 1 : rows > 128 && dtype == ZO_BF16 && dim <= 128 ? 8 : 4;
   s.rows = 32 * s.row_waves;
-  s.workers = dim * elem_bytes(dtype) <= 256 ? 512 : 256;
+  s.workers = dim * elem_bytes(dtype) <= 256 && s.row_waves < 8 ? 512 : 256;
   return s;
 }
 

@@ -148,8 +148,9 @@ struct Deal {
   uint32_t each;
 };
 
-template <uint32_t kRows, uint32_t kTile>
+template <uint32_t kRows, uint32_t kTile, uint32_t kThreads>
 __device__ Deal deal(const Attend& a, uint64_t* before) {
+  constexpr uint32_t kWaves = kThreads / kWave;
   __shared__ uint64_t wave_tiles[kWaves];
   const uint32_t lane = threadIdx.x % kWave;
   Deal d;
@@ -259,8 +260,9 @@ template <class S, uint32_t kDim, uint32_t kRowWaves>
 struct Form {
   typedef typename S::storage T;
   static constexpr uint32_t kRowBytes = kDim * sizeof(T), kChunks = kRowBytes / 16;
+  static constexpr uint32_t kWaves = kRowWaves > 4 ? kRowWaves : 4, kThreads = kWaves * kWave;
   static constexpr uint32_t kRows = 32 * kRowWaves, kKeyWaves = kWaves / kRowWaves;
-  static constexpr uint32_t kBlocks = kRowWaves == 4 && kRowBytes <= 256 ? 2 : 1;  // of 32 keys, of a wave in a tile
+  static constexpr uint32_t kBlocks = kRowWaves > 1 && kRowBytes <= 256 ? 2 : 1;  // of 32 keys, of a wave in a tile
   static constexpr uint32_t kKeys = 32 * kBlocks, kTile = kKeys * kKeyWaves;
   static constexpr uint32_t kStageRows = kKeys / kRowWaves;          // rows that a wave brings
   static constexpr uint32_t kLoadRows = kWave / kChunks;             // rows of a load of all lanes
@@ -268,8 +270,8 @@ struct Form {
   static constexpr uint32_t kBuffers = kRowWaves > 1 ? 2 : 1;
   static constexpr uint32_t kBufferBytes = 2 * kTile * kRowBytes;
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
-  static constexpr bool kPiped = kRowWaves == 4 && sizeof(T) == 2 && kBlocks == 2;
-  static constexpr uint32_t kPerCu = kRowBytes <= 256 ? 2 : 1;  // workgroups
+  static constexpr bool kPiped = kRowWaves > 1 && sizeof(T) == 2 && kBlocks == 2;
+  static constexpr uint32_t kSimdWaves = kRowBytes <= 256 ? 2 : 1;
   static_assert(kRowWaves != 1 || 2 * 32 * (kDim + 4) * 4 <= kBufferBytes, "the join at an item's end has room");
   static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
 };
@@ -289,14 +291,14 @@ __device__ __forceinline__ void loads_left() {
 
 // Heads of kDim, pages of whole sixteens of tokens, rows at 16-byte aligned places.
 template <class S, uint32_t kDim, uint32_t kRowWaves>
-__global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) attend_kernel(const Attend) {
+__global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S, kDim, kRowWaves>::kSimdWaves)) attend_kernel(const Attend) {
   typedef Form<S, kDim, kRowWaves> F;
   typedef typename S::storage T;
   constexpr bool kWide = sizeof(T) == 4;
   constexpr uint32_t kRowBytes = F::kRowBytes, kChunks = F::kChunks, kRows = F::kRows, kBlocks = F::kBlocks, kKeys = F::kKeys;
   constexpr uint32_t kTile = F::kTile, kLoads = F::kLoads, kLoadRows = F::kLoadRows, kOuts = kDim / 32, kSteps = kChunks / 2;
   extern __shared__ __align__(16) char lds[];
-  __shared__ uint64_t before[kThreads];
+  __shared__ uint64_t before[F::kThreads];
   __shared__ uint32_t odd_there[2];  // odd values in this item's tiles, and emptied for the next item's
   __shared__ float2 merge_sums[2][32];
 
@@ -306,7 +308,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   uint32_t workers;
   {
     const Attend a = arguments();
-    d = deal<kRows, kTile>(a, before);
+    d = deal<kRows, kTile, F::kThreads>(a, before);
     workers = a.workers;
   }
   const Runs runs(d.total, workers);
@@ -327,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
     const Attend a = arguments();
     uint32_t chunk = 0;  // the last thread's sequences that begin at or before it
 #pragma unroll
-    for (uint32_t step = kThreads / 2; step > 0; step /= 2)
+    for (uint32_t step = F::kThreads / 2; step > 0; step /= 2)
       if (before[chunk + step] <= at) chunk += step;
     chunk = uniform(chunk);
     seq = chunk * d.each;
@@ -1025,30 +1027,51 @@ __global__ void __launch_bounds__(kThreads, (Form<S, kDim, kRowWaves>::kPerCu)) 
   }
 }
 
-// Joins the parts of the items that were split: a workgroup has a share of one's rows, a thread four dims of a row at a time.
+// Joins the parts of the items that were split. A workgroup takes every gridDim.x-th entry, and of its item's rows, four dims a thread,
+// every gridDim.y-th share; kSlices groups of its threads take every kSlices-th part each and join theirs through LDS, so that an item of
+// many parts is not read one after another.
 template <class S, uint32_t kRows>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
-  if (blockIdx.x >= *a.active) return;
-  const Split it = a.splits[blockIdx.x];
-  if (it.last == 0) return;
-  const uint32_t quads = (a.dim + 3) / 4, first = blockIdx.x;
-  for (uint32_t e = blockIdx.y * kThreads + threadIdx.x; e < it.rows * quads; e += gridDim.y * kThreads) {
-    const uint32_t row = e / quads, dim = (e - row * quads) * 4;
-    float m = -INFINITY, l = 0.0f;
-    f32x4 o = {0, 0, 0, 0};
+  constexpr uint32_t kSlices = 4, kShare = kThreads / kSlices;
+  __shared__ float2 sums[kThreads];
+  __shared__ f32x4 rows[kThreads];
+  const uint32_t active = *a.active, quads = (a.dim + 3) / 4, lane = threadIdx.x % kWave;
+  const uint32_t slice = threadIdx.x / kShare;
+  for (uint32_t base = blockIdx.x; base < active; base += gridDim.x * kWave) {
+    const uint32_t mine = base + lane * gridDim.x;
+    for (uint64_t left = __ballot(mine < active && a.splits[min(mine, active - 1)].last != 0); left != 0; left &= left - 1) {
+      const uint32_t first = base + static_cast<uint32_t>(__builtin_ctzll(left)) * gridDim.x;
+      const Split it = a.splits[first];
+      for (uint32_t share = blockIdx.y; share * kShare < it.rows * quads; share += gridDim.y) {
+        const uint32_t e = share * kShare + threadIdx.x % kShare, row = e / quads, dim = (e - row * quads) * 4;
+        float m = -INFINITY, l = 0.0f;
+        f32x4 o = {0, 0, 0, 0};
+        const auto add = [&](float2 ml, f32x4 po) {
+          const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.0f : top;
+          const float s0 = __builtin_amdgcn_exp2f(m - ref), s1 = __builtin_amdgcn_exp2f(ml.x - ref);
+          l = l * s0 + ml.y * s1;
+          o = o * s0 + po * s1;
+          m = top;
+        };
+        if (row < it.rows) {
 #pragma unroll 4
-    for (uint32_t w = first; w <= it.last; ++w) {
-      const float* part = part_at<kRows>(a, w, w == first ? it.slot : 0) + static_cast<size_t>(row) * a.part_row;
-      const float2 ml = *reinterpret_cast<const float2*>(part);
-      const f32x4 po = *reinterpret_cast<const f32x4*>(part + 4 + dim);
-      const float top = fmaxf(m, ml.x), ref = top == -INFINITY ? 0.0f : top;
-      const float s0 = __builtin_amdgcn_exp2f(m - ref), s1 = __builtin_amdgcn_exp2f(ml.x - ref);
-      l = l * s0 + ml.y * s1;
-      o = o * s0 + po * s1;
-      m = top;
+          for (uint32_t w = first + slice; w <= it.last; w += kSlices) {
+            const float* part = part_at<kRows>(a, w, w == first ? it.slot : 0) + static_cast<size_t>(row) * a.part_row;
+            add(*reinterpret_cast<const float2*>(part), *reinterpret_cast<const f32x4*>(part + 4 + dim));
+          }
+        }
+        __syncthreads();  // the share before is joined
+        sums[threadIdx.x] = make_float2(m, l);
+        rows[threadIdx.x] = o;
+        __syncthreads();
+        if (slice == 0 && row < it.rows) {
+#pragma unroll
+          for (uint32_t n = 1; n < kSlices; ++n) add(sums[threadIdx.x + n * kShare], rows[threadIdx.x + n * kShare]);
+          const uint32_t node = node_of(a, it.row + row);
+          write_row<S>(a, it.token + node, it.head * a.group + it.row + row - node * a.group, dim, m, l, o);
+        }
+      }
     }
-    const uint32_t node = node_of(a, it.row + row);
-    write_row<S>(a, it.token + node, it.head * a.group + it.row + row - node * a.group, dim, m, l, o);
   }
 }
 
@@ -1156,10 +1179,13 @@ int launch(Attend& a, hipStream_t st) {
       hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_kernel<S, kDim, kRowWaves>), hipFuncAttributeMaxDynamicSharedMemorySize,
                           F::kLds) != hipSuccess)
     return ZO_ERR_HIP;
-  attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(kThreads), F::kLds, st>>>(a);
+  attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(F::kThreads), F::kLds, st>>>(a);
   const int rc = launched();
   if (rc != ZO_OK) return rc;
-  join_kernel<S, F::kRows><<<dim3(a.workers, std::max(1u, F::kRows * kDim / 4096)), dim3(kThreads), 0, st>>>(a);
+  // no more items are split than there are
+  const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;
+  const dim3 grid(static_cast<uint32_t>(std::min<uint64_t>(a.workers, items)), std::min(16u, F::kRows * kDim / 256));
+  join_kernel<S, F::kRows><<<grid, dim3(kThreads), 0, st>>>(a);
   return launched();
 }
 
@@ -1167,6 +1193,9 @@ template <class S, uint32_t kDim>
 int rows(Attend& a, uint32_t row_waves, hipStream_t st) {
   if constexpr (kDim * sizeof(typename S::storage) <= 512) {
     if (row_waves == 1) return launch<S, kDim, 1>(a, st);
+  }
+  if constexpr (Form<S, kDim, 8>::kPiped) {
+    if (row_waves == 8) return launch<S, kDim, 8>(a, st);
   }
   return launch<S, kDim, 4>(a, st);
 }
