@@ -61,9 +61,8 @@ struct Attend {
   const int32_t *ids, *lengths, *starts;
   const uint64_t* seen;
   int64_t seen_stride, q_token, q_head, out_token, out_head, page_bytes, head_bytes, token_bytes, table_stride;
-  double inv_group;
+  double inv_group, inv_page;  // of a group's query heads; of a page's sixteens
   uint32_t tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row;
-  int32_t page_shift;  // of a page's tokens where they are a power of two, else -1
   float scale;         // times log2(e)
 };
 
@@ -142,14 +141,14 @@ __device__ uint64_t head_tiles(const Attend& a, const Seq& s, uint32_t lane) {
   return uniform(__shfl(sums_upto(mine, lane), 63, 64));
 }
 
-// Tiles before each thread's sequences. Thread t counts sequences [t each, (t + 1) each).
+// Tiles before each thread's sequences, and the sequences where each thread has one. Thread t counts sequences [t each, (t + 1) each).
 struct Deal {
   uint64_t total;
   uint32_t each;
 };
 
 template <uint32_t kRows, uint32_t kTile, uint32_t kThreads>
-__device__ Deal deal(const Attend& a, uint64_t* before) {
+__device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
   constexpr uint32_t kWaves = kThreads / kWave;
   __shared__ uint64_t wave_tiles[kWaves];
   const uint32_t lane = threadIdx.x % kWave;
@@ -160,6 +159,7 @@ __device__ Deal deal(const Attend& a, uint64_t* before) {
     const uint32_t seq = threadIdx.x * d.each + i;
     Seq s = {};
     if (seq < a.seqs) s = seq_of<kRows>(a, seq);
+    if (d.each == 1) seqs[threadIdx.x] = s;
     constexpr uint32_t kFew = 8;  // blocks that a thread counts by itself; a longer sequence's by the whole wave
     if (a.seen) {
       if (s.blocks) tiles += static_cast<uint64_t>(s.blocks) * tiles_of<kRows, kTile>(a, s, 0);
@@ -299,6 +299,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   constexpr uint32_t kTile = F::kTile, kLoads = F::kLoads, kLoadRows = F::kLoadRows, kOuts = kDim / 32, kSteps = kChunks / 2;
   extern __shared__ __align__(16) char lds[];
   __shared__ uint64_t before[F::kThreads];
+  __shared__ Seq seqs[F::kThreads];
   __shared__ uint32_t odd_there[2];  // odd values in this item's tiles, and emptied for the next item's
   __shared__ float2 merge_sums[2][32];
 
@@ -308,7 +309,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   uint32_t workers;
   {
     const Attend a = arguments();
-    d = deal<kRows, kTile, F::kThreads>(a, before);
+    d = deal<kRows, kTile, F::kThreads>(a, before, seqs);
     workers = a.workers;
   }
   const Runs runs(d.total, workers);
@@ -335,7 +336,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     seq = chunk * d.each;
     uint64_t first = uniform(before[chunk]), tiles;
     for (;; ++seq) {  // `at` < the total: a sequence holds it
-      s = uniform(seq_of<kRows>(a, seq));
+      s = uniform(d.each == 1 ? seqs[seq] : seq_of<kRows>(a, seq));
       tiles = s.blocks ? head_tiles<kRows, kTile>(a, s, lane) : 0;
       if (at < first + tiles * a.heads) break;
       first += tiles * a.heads;
@@ -405,7 +406,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     const char* kp = a.k + head * a.head_bytes;
     const char* vp = a.v + head * a.head_bytes;
 
-    const auto page_of = [&](uint32_t j) { return a.page_shift >= 0 ? j >> a.page_shift : j / a.page_tokens; };
+    // The page of a token (tokens below 2^31, in sixteens: the product's error stays below the half's share).
+    const auto page_of = [&](uint32_t j) { return static_cast<uint32_t>((static_cast<double>(j / 16) + 0.5) * a.inv_page); };
     constexpr uint64_t kAll = kKeys == 64 ? ~0ull : (1ull << (kKeys % 64)) - 1;
     // Whether values of the tile may have to be emptied: not all rows see all of its keys.
     const auto some_see = [&](uint32_t t) { return t * kTile + kTile > all_see; };
@@ -471,6 +473,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     const auto mend = [&](uint32_t t, uint32_t buffer, uint64_t live) {
       if (live == kAll && !some_see(t)) return;
       char* values = own + buffer * F::kBufferBytes + kKeys * kRowBytes;
+#pragma unroll 1
       for (uint32_t i = 0; i < kLoads; ++i) {
         const uint32_t row = stage_row + load_row + i * kLoadRows;
         u32x4* at_lds = reinterpret_cast<u32x4*>(values + row * kRowBytes + load_chunk * 16);
@@ -952,27 +955,24 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
           }
         ready_wave();
         const uint32_t wave_count = min(32u, in_block - rw * 32);
-        constexpr uint32_t kTake = kWide ? 1 : 2;  // quads of a lane's 16 bytes
-        if (whole) {
-          constexpr uint32_t kLanes = kQuads / kTake;  // of a row
-          for (uint32_t i = lane / kLanes; i < wave_count; i += kWave / kLanes) {
-            const uint32_t quad = lane % kLanes * kTake, out_row = row0 + rw * 32 + i, out_node = node_of(a, out_row);
-            float v[4 * kTake];
-#pragma unroll
-            for (uint32_t n = 0; n < kTake; ++n) {
-              const f32x4 four = *reinterpret_cast<const f32x4*>(rest + i * kPass + ((quad + n) ^ i % kQuads) * 4);
-#pragma unroll
-              for (uint32_t d4 = 0; d4 < 4; ++d4) v[4 * n + d4] = four[d4];
-            }
+        constexpr uint32_t kEach = kWave / kQuads;  // rows at a time
+        const uint32_t quad = lane % kQuads;
+#pragma unroll 2
+        for (uint32_t i = lane / kQuads; i < wave_count; i += kEach) {
+          const f32x4 four = *reinterpret_cast<const f32x4*>(rest + i * kPass + (quad ^ i % kQuads) * 4);
+          if (whole) {
+            const uint32_t out_row = row0 + rw * 32 + i, out_node = node_of(a, out_row);
             T* to = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + out_node) * a.out_token +
                     static_cast<int64_t>(head * a.group + out_row - out_node * a.group) * a.out_head + pass * kPass + quad * 4;
-            *reinterpret_cast<u32x4_any*>(to) = S::pack(v);
-          }
-        } else {
-          for (uint32_t i = lane / kQuads; i < wave_count; i += kWave / kQuads) {
-            const uint32_t quad = lane % kQuads;
-            *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + pass * kPass + quad * 4) =
-                *reinterpret_cast<const f32x4*>(rest + i * kPass + (quad ^ i % kQuads) * 4);
+            if constexpr (kWide) {
+              typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+              *reinterpret_cast<f32x4_any*>(to) = four;
+            } else {
+              typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+              *reinterpret_cast<u32x2_any*>(to) = u32x2{pack_bf16x2(four[0], four[1]), pack_bf16x2(four[2], four[3])};
+            }
+          } else {
+            *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + pass * kPass + quad * 4) = four;
           }
         }
         ready_wave();
@@ -1019,8 +1019,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         if (++head == a.heads) {
           head = 0;
           if (at < end)
-            do s = uniform(seq_of<kRows>(a, ++seq));
-            while (s.blocks == 0);  // `at` < the total: one with tiles follows
+            do {
+              ++seq;
+              s = uniform(d.each == 1 ? seqs[seq] : seq_of<kRows>(a, seq));
+            } while (s.blocks == 0);  // `at` < the total: one with tiles follows
         }
       }
     }
@@ -1030,19 +1032,23 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 // Joins the parts of the items that were split. A workgroup takes every gridDim.x-th entry, and of its item's rows, four dims a thread,
 // every gridDim.y-th share; kSlices groups of its threads take every kSlices-th part each and join theirs through LDS, so that an item of
 // many parts is not read one after another.
-template <class S, uint32_t kRows>
+template <class S, uint32_t kRows, uint32_t kSlices>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
-  constexpr uint32_t kSlices = 4, kShare = kThreads / kSlices;
-  __shared__ float2 sums[kThreads];
-  __shared__ f32x4 rows[kThreads];
-  const uint32_t active = *a.active, quads = (a.dim + 3) / 4, lane = threadIdx.x % kWave;
-  const uint32_t slice = threadIdx.x / kShare;
+  constexpr uint32_t kShare = kThreads / kSlices;
+  __shared__ float2 sums[kSlices > 1 ? kThreads : 1];
+  __shared__ f32x4 rows[kSlices > 1 ? kThreads : 1];
+  const uint32_t quads = (a.dim + 3) / 4, lane = threadIdx.x % kWave, slice = threadIdx.x / kShare;
+  uint32_t active = a.workers;
   for (uint32_t base = blockIdx.x; base < active; base += gridDim.x * kWave) {
     const uint32_t mine = base + lane * gridDim.x;
-    for (uint64_t left = __ballot(mine < active && a.splits[min(mine, active - 1)].last != 0); left != 0; left &= left - 1) {
-      const uint32_t first = base + static_cast<uint32_t>(__builtin_ctzll(left)) * gridDim.x;
-      const Split it = a.splits[first];
-      for (uint32_t share = blockIdx.y; share * kShare < it.rows * quads; share += gridDim.y) {
+    const Split own = a.splits[min(mine, a.workers - 1)];  // with the count at once: those behind it hold anything
+    active = *a.active;
+    for (uint64_t left = __ballot(mine < active && own.last != 0); left != 0; left &= left - 1) {
+      const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left)), first = base + from * gridDim.x;
+      const auto there = [&](uint32_t v) -> uint32_t { return __builtin_amdgcn_readlane(v, from); };
+      const uint32_t last = there(own.last), slot = there(own.slot), token = there(own.token), row0 = there(own.row);
+      const uint32_t item_rows = there(own.rows), head = there(own.head);
+      for (uint32_t share = blockIdx.y; share * kShare < item_rows * quads; share += gridDim.y) {
         const uint32_t e = share * kShare + threadIdx.x % kShare, row = e / quads, dim = (e - row * quads) * 4;
         float m = -INFINITY, l = 0.0f;
         f32x4 o = {0, 0, 0, 0};
@@ -1053,22 +1059,25 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
           o = o * s0 + po * s1;
           m = top;
         };
-        if (row < it.rows) {
+        if (row < item_rows) {
 #pragma unroll 4
-          for (uint32_t w = first + slice; w <= it.last; w += kSlices) {
-            const float* part = part_at<kRows>(a, w, w == first ? it.slot : 0) + static_cast<size_t>(row) * a.part_row;
+          for (uint32_t w = first + slice; w <= last; w += kSlices) {
+            const float* part = part_at<kRows>(a, w, w == first ? slot : 0) + static_cast<size_t>(row) * a.part_row;
             add(*reinterpret_cast<const float2*>(part), *reinterpret_cast<const f32x4*>(part + 4 + dim));
           }
         }
-        __syncthreads();  // the share before is joined
-        sums[threadIdx.x] = make_float2(m, l);
-        rows[threadIdx.x] = o;
-        __syncthreads();
-        if (slice == 0 && row < it.rows) {
+        if constexpr (kSlices > 1) {
+          __syncthreads();  // the share before is joined
+          sums[threadIdx.x] = make_float2(m, l);
+          rows[threadIdx.x] = o;
+          __syncthreads();
+          if (slice == 0)
 #pragma unroll
-          for (uint32_t n = 1; n < kSlices; ++n) add(sums[threadIdx.x + n * kShare], rows[threadIdx.x + n * kShare]);
-          const uint32_t node = node_of(a, it.row + row);
-          write_row<S>(a, it.token + node, it.head * a.group + it.row + row - node * a.group, dim, m, l, o);
+            for (uint32_t n = 1; n < kSlices; ++n) add(sums[threadIdx.x + n * kShare], rows[threadIdx.x + n * kShare]);
+        }
+        if (slice == 0 && row < item_rows) {
+          const uint32_t node = node_of(a, row0 + row);
+          write_row<S>(a, token + node, head * a.group + row0 + row - node * a.group, dim, m, l, o);
         }
       }
     }
@@ -1182,10 +1191,13 @@ int launch(Attend& a, hipStream_t st) {
   attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(F::kThreads), F::kLds, st>>>(a);
   const int rc = launched();
   if (rc != ZO_OK) return rc;
-  // no more items are split than there are
+  // no more items are split than there are; slices where an item has several parts
   const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;
-  const dim3 grid(static_cast<uint32_t>(std::min<uint64_t>(a.workers, items)), std::min(16u, F::kRows * kDim / 256));
-  join_kernel<S, F::kRows><<<grid, dim3(kThreads), 0, st>>>(a);
+  const uint32_t most = static_cast<uint32_t>(std::min<uint64_t>(a.workers, items));
+  if (items * 6 <= a.workers)
+    join_kernel<S, F::kRows, 4><<<dim3(most, std::min(32u, F::kRows * kDim / 256)), dim3(kThreads), 0, st>>>(a);
+  else
+    join_kernel<S, F::kRows, 1><<<dim3(most, std::min(16u, F::kRows * kDim / 1024)), dim3(kThreads), 0, st>>>(a);
   return launched();
 }
 
@@ -1255,7 +1267,7 @@ extern "C" int zo_tree_attend(const zo_tree_attention* p, void* stream) {
   a.width = p->table.width;
   a.pages = p->cache.pages;
   a.page_tokens = p->cache.page_tokens;
-  a.page_shift = (a.page_tokens & (a.page_tokens - 1)) == 0 ? __builtin_ctz(a.page_tokens) : -1;
+  a.inv_page = 16.0 / a.page_tokens;
   a.heads = p->cache.heads;
   a.dim = p->cache.dim;
   a.workers = shape.workers;
