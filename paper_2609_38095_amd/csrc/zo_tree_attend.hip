@@ -272,7 +272,6 @@ struct Form {
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
   static constexpr bool kPiped = kRowWaves > 1 && sizeof(T) == 2 && kBlocks == 2;
   static constexpr uint32_t kSimdWaves = kRowBytes <= 256 ? 2 : 1;
-  static_assert(kRowWaves != 1 || 2 * 32 * (kDim + 4) * 4 <= kBufferBytes, "the join at an item's end has room");
   static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
 };
 
@@ -301,7 +300,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   __shared__ uint64_t before[F::kThreads];
   __shared__ Seq seqs[F::kThreads];
   __shared__ uint32_t odd_there[2];  // odd values in this item's tiles, and emptied for the next item's
-  __shared__ float2 merge_sums[2][32];
+  __shared__ float2 sums[F::kWaves][32];
 
   const uint32_t wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, r = lane % 32, g = lane / 32;
   const uint32_t rw = wave % kRowWaves, kw = wave / kRowWaves;  // which rows, which keys
@@ -885,40 +884,6 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     }
     l += __shfl_xor(l, 32, 64);
 
-    // Waves with the same rows join theirs in LDS: two and two, then the two.
-    if constexpr (F::kKeyWaves > 1) {
-      constexpr uint32_t kRow = kDim + 4;
-      float* rest = reinterpret_cast<float*>(lds);
-#pragma unroll
-      for (uint32_t n = F::kKeyWaves / 2; n > 0; n /= 2) {
-        __syncthreads();
-        if (kw >= n && kw < 2 * n) {
-          if (g == 0) merge_sums[kw - n][r] = make_float2(m, l);
-#pragma unroll
-          for (uint32_t e = 0; e < kOuts; ++e)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; i += 4)
-              *reinterpret_cast<f32x4*>(rest + ((kw - n) * 32 + r) * kRow + 32 * e + 2 * i + 4 * g) = f32x4{o[e][i], o[e][i + 1], o[e][i + 2], o[e][i + 3]};
-        }
-        __syncthreads();
-        if (kw < n) {
-          const float2 ml = merge_sums[kw][r];
-          const float all = fmaxf(m, ml.x), ref = all == -INFINITY ? 0.0f : all;
-          const float s0 = __builtin_amdgcn_exp2f(m - ref), s1 = __builtin_amdgcn_exp2f(ml.x - ref);
-          l = l * s0 + ml.y * s1;
-          m = all;
-#pragma unroll
-          for (uint32_t e = 0; e < kOuts; ++e)
-#pragma unroll
-            for (uint32_t i = 0; i < 16; i += 4) {
-              const f32x4 theirs = *reinterpret_cast<const f32x4*>(rest + (kw * 32 + r) * kRow + 32 * e + 2 * i + 4 * g);
-#pragma unroll
-              for (uint32_t n4 = 0; n4 < 4; ++n4) o[e][i + n4] = o[e][i + n4] * s0 + theirs[n4] * s1;
-            }
-        }
-      }
-    }
-
     const bool whole = t_begin == 0 && t_end == tiles;
     if (threadIdx.x == 0) {
       if (t_end == tiles && !whole) {  // so it began in another run
@@ -929,60 +894,96 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       const uint64_t item_end = item_first + tiles;
       if (item_end == end || (item_end > end && item_first < begin)) a.splits[worker].last = 0;
     }
-    if (a.lse && whole && kw == 0 && mine && g == 0)
-      a.lse[static_cast<size_t>(s.token + node) * a.heads * a.group + q_head] = any_seen(l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
-    if constexpr (kRowWaves > 1) __syncthreads();  // the last tile is read
-    // Results through LDS, for whole lines: rows of kPass dims, swizzled by 16 bytes; then each lane takes 16 bytes of a row of the output.
-    if (kw == 0 && wave_rows) {
-      constexpr uint32_t kRoom = F::kLds / (kRowWaves * 32 * 4), kPass = kDim < kRoom ? kDim : kRoom;
-      constexpr uint32_t kQuads = kPass / 4;
-      float* rest = reinterpret_cast<float*>(lds) + rw * 32 * kPass;
-      const float by = !whole ? 1.0f : any_seen(l) ? 1.0f / l : 0.0f;
-      const bool none = whole && !any_seen(l);
-      float* parts = part_at<kRows>(a, worker, at == begin ? 0 : 1) + static_cast<size_t>(rw * 32) * a.part_row;
-      if (!whole && g == 0) *reinterpret_cast<float2*>(parts + static_cast<size_t>(r) * a.part_row) = make_float2(m, l);
+    // Results through LDS, for whole lines: rows swizzled by 16 bytes, then four dims of a row for each lane.
+    float* parts = part_at<kRows>(a, worker, at == begin ? 0 : 1);
+    const auto write_four = [&](uint32_t i, uint32_t dim, f32x4 four) {  // of row i of the item
+      if (whole) {
+        const uint32_t out_row = row0 + i, out_node = node_of(a, out_row);
+        T* to = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + out_node) * a.out_token +
+                static_cast<int64_t>(head * a.group + out_row - out_node * a.group) * a.out_head + dim;
+        if constexpr (kWide) {
+          typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+          *reinterpret_cast<f32x4_any*>(to) = four;
+        } else {
+          typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+          *reinterpret_cast<u32x2_any*>(to) = u32x2{pack_bf16x2(four[0], four[1]), pack_bf16x2(four[2], four[3])};
+        }
+      } else {
+        *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + dim) = four;
+      }
+    };
+    const auto write_sums = [&](uint32_t i, uint32_t out_token, uint32_t out_head, float row_m, float row_l) {
+      if (!whole)
+        *reinterpret_cast<float2*>(parts + static_cast<size_t>(i) * a.part_row) = make_float2(row_m, row_l);
+      else if (a.lse)
+        a.lse[static_cast<size_t>(out_token) * a.heads * a.group + out_head] = any_seen(row_l) ? (row_m + log2f(row_l)) * 0.69314718055994531f : -INFINITY;
+    };
+    // What a whole row's sum is multiplied by; a row that saw nothing holds zeros.
+    const auto over = [&](float row_l) { return whole && any_seen(row_l) ? 1.0f / row_l : 1.0f; };
+    __syncthreads();  // the last tile is read
+    constexpr uint32_t kRoom = F::kLds / (F::kWaves * 32 * 4), kPass = kDim < kRoom ? kDim : kRoom;  // dims of a row at a time
+    constexpr uint32_t kQuads = kPass / 4, kEach = kWave / kQuads;                                  // rows of a wave at a time
+    float* rest = reinterpret_cast<float*>(lds) + wave * 32 * kPass;
+    float scaled = 1.0f;
+    if constexpr (F::kKeyWaves > 1) {
+      if (g == 0) sums[wave][r] = make_float2(m, l);
+    } else {
+      scaled = over(l);
+      if (mine && g == 0) write_sums(rw * 32 + r, s.token + node, q_head, m, l);
+    }
 #pragma unroll
-      for (uint32_t pass = 0; pass < kDim / kPass; ++pass) {
+    for (uint32_t pass = 0; pass < kDim / kPass; ++pass) {
+      if (wave_rows) {
 #pragma unroll
         for (uint32_t e = 0; e < kPass / 32; ++e)
 #pragma unroll
           for (uint32_t i = 0; i < 16; i += 4) {
             const f32x16& from = o[pass * (kPass / 32) + e];
-            f32x4 four = {from[i], from[i + 1], from[i + 2], from[i + 3]};
-            four = none ? f32x4{0, 0, 0, 0} : four * by;
-            const uint32_t quad = 8 * e + i / 2 + g;
-            *reinterpret_cast<f32x4*>(rest + r * kPass + (quad ^ r % kQuads) * 4) = four;
+            *reinterpret_cast<f32x4*>(rest + r * kPass + ((8 * e + i / 2 + g) ^ r % kQuads) * 4) =
+                f32x4{from[i], from[i + 1], from[i + 2], from[i + 3]} * scaled;
           }
+      }
+      const uint32_t quad = lane % kQuads;
+      if constexpr (F::kKeyWaves > 1) {  // the waves have the same rows: each joins a share of them
+        static_assert(kPass == kDim, "all rows of all waves have room");
+        __syncthreads();
+        constexpr uint32_t kShare = 32 / F::kWaves;
+        for (uint32_t i = wave * kShare + lane / kQuads; i < min((wave + 1) * kShare, in_block); i += kEach) {
+          float row_m = -INFINITY, row_l = 0.0f;
+#pragma unroll
+          for (uint32_t w = 0; w < F::kWaves; ++w) row_m = fmaxf(row_m, sums[w][i].x);
+          const float ref = row_m == -INFINITY ? 0.0f : row_m;
+          f32x4 four = {0, 0, 0, 0};
+#pragma unroll
+          for (uint32_t w = 0; w < F::kWaves; ++w) {
+            const float by = __builtin_amdgcn_exp2f(sums[w][i].x - ref);
+            row_l += sums[w][i].y * by;
+            four += *reinterpret_cast<const f32x4*>(reinterpret_cast<float*>(lds) + (w * 32 + i) * kPass + (quad ^ i % kQuads) * 4) * by;
+          }
+          write_four(i, quad * 4, four * over(row_l));
+          if (quad == 0) {
+            const uint32_t out_row = row0 + i, out_node = node_of(a, out_row);
+            write_sums(i, s.token + out_node, head * a.group + out_row - out_node * a.group, row_m, row_l);
+          }
+        }
+      } else {
         ready_wave();
-        const uint32_t wave_count = min(32u, in_block - rw * 32);
-        constexpr uint32_t kEach = kWave / kQuads;  // rows at a time
-        const uint32_t quad = lane % kQuads;
+        const uint32_t count = wave_rows ? min(32u, in_block - rw * 32) : 0u;
 #pragma unroll 2
-        for (uint32_t i = lane / kQuads; i < wave_count; i += kEach) {
-          const f32x4 four = *reinterpret_cast<const f32x4*>(rest + i * kPass + (quad ^ i % kQuads) * 4);
-          if (whole) {
-            const uint32_t out_row = row0 + rw * 32 + i, out_node = node_of(a, out_row);
-            T* to = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + out_node) * a.out_token +
-                    static_cast<int64_t>(head * a.group + out_row - out_node * a.group) * a.out_head + pass * kPass + quad * 4;
-            if constexpr (kWide) {
-              typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-              *reinterpret_cast<f32x4_any*>(to) = four;
-            } else {
-              typedef u32x2 __attribute__((aligned(2))) u32x2_any;
-              *reinterpret_cast<u32x2_any*>(to) = u32x2{pack_bf16x2(four[0], four[1]), pack_bf16x2(four[2], four[3])};
-            }
-          } else {
-            *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + pass * kPass + quad * 4) = four;
-          }
+        for (uint32_t i = lane / kQuads; i < count; i += kEach) {
+          write_four(rw * 32 + i, pass * kPass + quad * 4, *reinterpret_cast<const f32x4*>(rest + i * kPass + (quad ^ i % kQuads) * 4));
         }
         ready_wave();
       }
     }
     // Infinities and NaN in tiles that only some rows see, to the results of the rows that see them. (The waves have passed a barrier
     // since the last one was found.)
-    if (kw == 0 && wave_rows && odd_there[turn] != 0) {
+    if (odd_there[turn] != 0) {
       asm volatile("s_waitcnt vmcnt(0)" : : : "memory");  // the results are written
-      float* part = part_at<kRows>(a, worker, at == begin ? 0 : 1) + static_cast<size_t>(rw * 32 + r) * a.part_row + 4;
+      if constexpr (F::kKeyWaves > 1) __syncthreads();      // by all waves
+    }
+    if (kw == 0 && wave_rows && odd_there[turn] != 0) {
+      float* part = parts + static_cast<size_t>(rw * 32 + r) * a.part_row + 4;
       T* result = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + node) * a.out_token + static_cast<int64_t>(q_head) * a.out_head;
       const auto odd = [](float v) { return !(fabsf(v) <= 3.402823466e38f); };
       for (uint32_t j = t_begin * kTile; j < min(t_end * kTile, wave_end); ++j) {
