@@ -210,7 +210,7 @@ __device__ __forceinline__ int64_t row_at(const Keep& k, uint32_t seq, int64_t t
 
 // Tensors of a workgroup: as many as give its threads a vector each, more where there are workgroups enough.
 uint32_t tensors_each(uint32_t seqs, uint32_t tensors, uint32_t vecs) {
-  const uint64_t enough = (static_cast<uint64_t>(seqs) * tensors + 2047) / 2048, full = (kKeepThreads + vecs - 1) / vecs;
+  const uint64_t enough = (static_cast<uint64_t>(seqs) * tensors + 8191) / 8192, full = (kKeepThreads + vecs - 1) / vecs;
   return static_cast<uint32_t>(std::min<uint64_t>(tensors, std::max(enough, full)));
 }
 
