@@ -95,6 +95,7 @@ int zo_tree_attend(const zo_tree_attention* a, void* stream);
  * zo_tree_accept -- the walk along the drafted tokens that the draws agree with. drafted[t] is the token of row t, drawn[t] the
  * token drawn behind it. Sequence s walks from its new token 0 (a token that is certain): from the one it is at to the
  * first new token that comes behind it and whose drafted token is the one drawn there; until there is none, or `most` tokens are walked.
+ * A negative token (zo_draw's for logits without any weight, or a place of a tree that is not used) agrees with none.
  * path[s][i] is the index (within the sequence) of the walk's i-th token, tokens_out[s][i] the token drawn behind it, both
  * -1 behind the walk's end; counts[s] the tokens walked (0 for a sequence without new ones): as many are won, and the last is the
  * next step's token 0. path and tokens_out: [seqs, most], contiguous. The outputs do not overlap each other or the inputs.

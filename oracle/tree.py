@@ -90,7 +90,7 @@ def accept(drafted, drawn, starts, most, parents=None):
             path[s, counts[s]], won[s, counts[s]] = i, drawn[first + i]
             counts[s] += 1
             behind = [j for j in range(i + 1, count) if (j - 1 if parents is None else parents[first + j]) == i]
-            i = next((j for j in behind if drafted[first + j] == drawn[first + i]), None)
+            i = next((j for j in behind if drafted[first + j] == drawn[first + i] >= 0), None)
     return path, won, counts
 
 

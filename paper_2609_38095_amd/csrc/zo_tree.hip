@@ -129,7 +129,7 @@ __global__ void __launch_bounds__(kWalkThreads) accept_kernel(const zo_tree_walk
     for (uint32_t i = threadIdx.x; i < count; i += kWalkThreads) {
       const uint32_t j = base + i, row = sp.begin + j;
       const uint32_t parent = w.parents ? static_cast<uint32_t>(w.parents[row]) : j - 1;
-      const bool offers = j > 0 && parent < j && w.drafted[row] == w.drawn[sp.begin + parent];
+      const bool offers = j > 0 && parent < j && w.drafted[row] >= 0 && w.drafted[row] == w.drawn[sp.begin + parent];
       if (w.parents == nullptr) {
         if (j > 0 && !offers) atomicMin(&first, i);
       } else if (offers) {

@@ -26,10 +26,10 @@ EXPORTS = ("zo_tree_lay", "zo_norm_rotate_put_at", "zo_tree_attend", "zo_tree_at
 
 def zo_tree_lay(starts, lengths, tokens, parents=None, words=None, stream=None):
     """(seq_of, positions, places, seen) of the new tokens: int32 [tokens] each, and masks int64 [tokens, words] whose bit 64 w + b
-    says that a token sees new token 64 w + b of its sequence. words: as many as the largest tree needs (64 tokens each; 1 by
-    default with parents), 0 for chains, whose seen is None."""
+    says that a token sees new token 64 w + b of its sequence. words: as many as the largest tree needs, 64 tokens each (by
+    default what a tree of all the tokens needs, at most ZO_TREE_WORDS); 0 for chains (their default), whose seen is None."""
     if words is None:
-        words = 0 if parents is None else 1
+        words = 0 if parents is None else min(ZO_TREE_WORDS, max(1, -(-tokens // 64)))
     return decode._call((decode._TENSORS or decode._tensors()).tree_lay, stream, starts, starts, lengths, tokens, parents, words)
 
 

@@ -97,6 +97,14 @@ def test_lay(case, kind):
         assert g is None or np.array_equal(g.cpu().numpy(), w)
 
 
+def test_lay_has_room_for_any_tree_by_default():
+    n, parents = 300, trees([300], 2)
+    got = zo.zo_tree_lay(ints([0, n]), ints([9]), n, dev(parents))
+    for g, w in zip(got, oracle.lay(np.array([0, n]), [9], n, parents, 5)):
+        assert np.array_equal(g.cpu().numpy(), w)
+    assert zo.zo_tree_lay(ints([0, 0]), ints([9]), 0, ints([]))[3].shape == (0, 1)
+
+
 def test_lay_takes_any_parents():
     """Parents that are not below their token, or negative, count as none; so the masks are those of the trees without them."""
     rng = np.random.default_rng(4)
@@ -420,6 +428,14 @@ def test_accept_takes_the_first_of_equal_tokens():
     assert path.tolist() == [[0, 2, 4, -1, -1]] and tokens.tolist() == [[8, 1, 2, -1, -1]] and counts.tolist() == [3]
 
 
+@pytest.mark.parametrize("parents", [None, [-1, 0, 1, 1, 3]])
+def test_accept_takes_no_negative_token(parents):
+    """Places of a padded tree, behind a row that zo_draw found no token for."""
+    drafted, drawn = [5, 7, -1, -1, -1], [7, -1, -1, -1, -1]
+    got = zo.zo_tree_accept(ints(drafted), ints(drawn), ints([0, 5]), 5, None if parents is None else ints(parents))
+    assert [g.tolist() for g in got] == [[[0, 1, -1, -1, -1]], [[7, -1, -1, -1, -1]], [2]]
+
+
 def test_accept_walks_over_windows():
     """Branches whose tokens lie thousands of indices apart: a child behind the window of its parent."""
     n = 5000
@@ -554,6 +570,35 @@ def test_two_graphs_and_a_given_workspace():
         torch.cuda.synchronize()
         assert torch.equal(held[0], wants[0]) and torch.equal(held[1], wants[1])
         held[0].zero_(), held[1].zero_()
+
+
+@pytest.mark.parametrize("dtype,dim,counts", [("bf16", 128, [300]), ("bf16", 256, [3, 2]), ("bf16", 256, [90]), ("f32", 128, [3, 2]), ("f32", 128, [90]),
+                                              ("f32", 256, [50, 20]), ("f32", 96, [9])])
+def test_every_form_in_graphs_and_at_once(dtype, dim, counts):
+    """Each form of the kernel, first called inside a capture: its replays, and calls on two streams at once."""
+    q, kc, vc, table, _ = attend_case([70] * len(counts), counts, 4, 2, dim, 16, "heads", dtype)
+    args = (kc, vc, dev(table), ints([70] * len(counts)), dev(starts_of(counts)))
+    qs = [q, q.flip(0).contiguous()]
+    graphs, held = [], []
+    for x in qs:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            held.append(zo.zo_tree_attend(x, *args))
+    wants = [zo.zo_tree_attend(x, *args) for x in qs]
+    for _ in range(3):
+        for g, h in zip(graphs, held):
+            h.zero_()
+            g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(h, w) for h, w in zip(held, wants))
+    streams, got = [torch.cuda.Stream() for _ in qs], []
+    for _ in range(5):
+        for x, stream in zip(qs, streams):
+            stream.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(stream):
+                got.append(zo.zo_tree_attend(x, *args))
+    torch.cuda.synchronize()
+    assert all(torch.equal(g, wants[i % 2]) for i, g in enumerate(got))
 
 
 def test_drafted_trees_give_the_answers_of_single_tokens():

@@ -122,6 +122,7 @@ def test_oracle_of_the_walk_and_its_moves():
     path, won, counts = oracle.accept([9, 4, 7, 1, 2, 8, 8], [7, 0, 2, 0, 5, 8, 3], [0, 5, 5, 7], 4, parents)
     assert path.tolist() == [[0, 2, 4, -1], [-1] * 4, [0, 1, -1, -1]]
     assert won.tolist() == [[7, 2, 5, -1], [-1] * 4, [8, 3, -1, -1]] and counts.tolist() == [3, 0, 2]
+    assert oracle.accept([9, -1, 7], [-1, -1, 1], [0, 3], 4)[2].tolist() == [1]  # not a token
     path, won, counts = oracle.accept([9, 4, 7], [4, 6, 1], [0, 3], 4)
     assert path.tolist() == [[0, 1, -1, -1]] and won.tolist() == [[4, 6, -1, -1]] and counts.tolist() == [2]
     c = np.arange(6 * 1 * 2 * 1.0).reshape(6, 1, 2, 1)
