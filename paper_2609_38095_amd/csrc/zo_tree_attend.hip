@@ -1085,20 +1085,24 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
   }
 }
 
-// Any head size, page size and alignment: a wave has a row at a time. 64 keys' scores at once, one in each lane, then their
-// values one by one, a dim in each lane (and the dims 64, 128 and 192 behind it); each 64's sum is added to what was
-// there. A token that the row does not see is not read. 40 new tokens of 4 heads of 96 behind 1,000: 110 us.
+// Any head size, page size and alignment: a workgroup has a row at a time, its waves every fourth 64 keys. 64 keys' scores at once, one
+// in each lane, then their values, a dim in each lane (and the dims 64, 128 and 192 behind it); each 64's sum is added to what was
+// there, and the waves join at the end. A token that the row does not see is not read. Every row reads its keys anew.
 template <class S>
 __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
   typedef typename S::storage T;
-  __shared__ float queries[kWaves][ZO_DIM_MAX];
-  __shared__ float weights[kWaves][kWave];
+  constexpr uint32_t kVec = 16 / sizeof(T), kDims = ZO_DIM_MAX / kWave, kTogether = 16;
+  __shared__ float queries[ZO_DIM_MAX], outs[kWaves][ZO_DIM_MAX], weights[kWaves][kWave];
+  __shared__ float2 sums[kWaves];
   __shared__ int64_t places[kWaves][kWave];
-  const uint32_t wave = threadIdx.x / kWave, lane = threadIdx.x % kWave, q_heads = a.heads * a.group;
-  const uint32_t rows = a.tokens * q_heads, blocks = (rows - 1) / kWaves + 1;
-  for (uint32_t block = blockIdx.x; block < blocks; block += gridDim.x) {
-    const uint32_t row = block * kWaves + wave;
-    const uint32_t token = min(row, rows - 1) / q_heads, q_head = min(row, rows - 1) - token * q_heads, head = q_head / a.group;
+  const uint32_t wave = uniform(threadIdx.x / kWave), lane = threadIdx.x % kWave, q_heads = a.heads * a.group, rows = a.tokens * q_heads;
+  const auto ready_wave = [] {  // what the wave put is there for its lanes
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  for (uint32_t row = blockIdx.x; row < rows; row += gridDim.x) {
+    const uint32_t token = row / q_heads, q_head = row - token * q_heads, head = q_head / a.group;
     // the last sequence that begins at or before the token; with `starts` as they should be it is the token's, if any is
     uint32_t low = 0, high = a.seqs;
     while (low + 1 < high) {
@@ -1109,22 +1113,17 @@ __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
         high = middle;
     }
     const Seq s = seq_of<32>(a, low);
-    const bool mine = row < rows && token >= s.token && token - s.token < s.count;
-    const uint32_t node = token - s.token, sees = !mine ? 0u : a.seen ? s.len : min(s.len, s.cached + node + 1);
+    if (token < s.token || token - s.token >= s.count) continue;
+    const uint32_t node = token - s.token, sees = a.seen ? s.len : min(s.len, s.cached + node + 1);
     const T* qp = reinterpret_cast<const T*>(a.q) + static_cast<int64_t>(token) * a.q_token + static_cast<int64_t>(q_head) * a.q_head;
-    __syncthreads();  // the queries of the row before are read
-    for (uint32_t d = lane; d < a.dim; d += kWave) queries[wave][d] = S::load1(qp + d);
+    __syncthreads();  // the row before is done with the LDS
+    for (uint32_t d = threadIdx.x; d < a.dim; d += kThreads) queries[d] = S::load1(qp + d);
     __syncthreads();
     const int32_t* ids = a.ids + static_cast<int64_t>(low) * a.table_stride;
     const char* kp = a.k + head * a.head_bytes;
     const char* vp = a.v + head * a.head_bytes;
-    float m = -INFINITY, l = 0.0f, o[ZO_DIM_MAX / kWave] = {};
-    uint32_t most = sees;  // of the workgroup's rows: its barriers are everyone's
-    __shared__ uint32_t wave_sees[kWaves];
-    if (lane == 0) wave_sees[wave] = sees;
-    __syncthreads();
-    for (uint32_t w = 0; w < kWaves; ++w) most = max(most, wave_sees[w]);
-    for (uint32_t base = 0; base < most; base += kWave) {
+    float m = -INFINITY, l = 0.0f, o[kDims] = {};
+    for (uint32_t base = wave * kWave; base < sees; base += kThreads) {
       const uint32_t j = base + lane;
       bool live = j < sees;
       if (live && a.seen && j >= s.cached) {
@@ -1141,7 +1140,21 @@ __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
       if (place >= 0) {
         const T* key = reinterpret_cast<const T*>(kp + place);
         float sum = 0.0f;
-        for (uint32_t d = 0; d < a.dim; ++d) sum = __builtin_fmaf(queries[wave][d], S::load1(key + d), sum);
+        uint32_t d = 0;
+#pragma unroll 4
+        for (; d + kVec <= a.dim; d += kVec) {
+          const u32x4 four = *reinterpret_cast<const u32x4_any*>(key + d);
+#pragma unroll
+          for (uint32_t i = 0; i < 4; ++i) {
+            if constexpr (kVec == 8) {
+              sum = __builtin_fmaf(queries[d + 2 * i], __uint_as_float(four[i] << 16), sum);
+              sum = __builtin_fmaf(queries[d + 2 * i + 1], __uint_as_float(four[i] & 0xFFFF0000u), sum);
+            } else {
+              sum = __builtin_fmaf(queries[d + i], __uint_as_float(four[i]), sum);
+            }
+          }
+        }
+        for (; d < a.dim; ++d) sum = __builtin_fmaf(queries[d], S::load1(key + d), sum);
         score = sum * a.scale;
       }
       float top = score;
@@ -1157,30 +1170,54 @@ __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
       m = top;
       weights[wave][lane] = weight;
       places[wave][lane] = place;
-      __syncthreads();
-      float sums[ZO_DIM_MAX / kWave] = {};
-      for (uint32_t i = 0; i < kWave; ++i) {
-        const int64_t from = places[wave][i];
-        if (from < 0) continue;
-        const T* value = reinterpret_cast<const T*>(vp + from);
-        const float w = weights[wave][i];
+      const uint64_t there = __ballot(place >= 0);
+      ready_wave();
+      float part[kDims] = {};
+      for (uint32_t i0 = 0; i0 < kWave; i0 += kTogether) {
+        if ((there >> i0 & ((1ull << kTogether) - 1)) == 0) continue;
 #pragma unroll
-        for (uint32_t c = 0; c < ZO_DIM_MAX / kWave; ++c)
-          if (c * kWave + lane < a.dim) sums[c] = __builtin_fmaf(w, S::load1(value + c * kWave + lane), sums[c]);
+        for (uint32_t c = 0; c < kDims; ++c) {
+          if (c * kWave >= a.dim) break;
+          const bool in = c * kWave + lane < a.dim;
+          float v[kTogether];
+#pragma unroll
+          for (uint32_t i = 0; i < kTogether; ++i) {
+            const int64_t from = places[wave][i0 + i];
+            v[i] = in && from >= 0 ? S::load1(reinterpret_cast<const T*>(vp + from) + c * kWave + lane) : 0.0f;
+          }
+#pragma unroll
+          for (uint32_t i = 0; i < kTogether; ++i) part[c] = __builtin_fmaf(weights[wave][i0 + i], v[i], part[c]);
+        }
       }
 #pragma unroll
-      for (uint32_t c = 0; c < ZO_DIM_MAX / kWave; ++c) o[c] = o[c] * by + sums[c];
-      __syncthreads();
+      for (uint32_t c = 0; c < kDims; ++c) o[c] = o[c] * by + part[c];
+      ready_wave();
     }
-    if (!mine) continue;
-    const bool any = l > 0.0f || l != l;
-    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(token) * a.out_token + static_cast<int64_t>(q_head) * a.out_head;
+    if (lane == 0) sums[wave] = make_float2(m, l);
 #pragma unroll
-    for (uint32_t c = 0; c < ZO_DIM_MAX / kWave; ++c)
-      if (c * kWave + lane < a.dim) S::store1(op + c * kWave + lane, any ? o[c] / l : 0.0f);
-    if (a.lse && lane == 0) a.lse[static_cast<size_t>(token) * q_heads + q_head] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+    for (uint32_t c = 0; c < kDims; ++c) outs[wave][c * kWave + lane] = o[c];
+    __syncthreads();
+    float top = -INFINITY, total = 0.0f;
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) top = fmaxf(top, sums[w].x);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float by[kWaves];
+#pragma unroll
+    for (uint32_t w = 0; w < kWaves; ++w) {
+      by[w] = __builtin_amdgcn_exp2f(sums[w].x - ref);
+      total += sums[w].y * by[w];
+    }
+    T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(token) * a.out_token + static_cast<int64_t>(q_head) * a.out_head;
+    if (threadIdx.x < a.dim) {
+      float out = 0.0f;
+#pragma unroll
+      for (uint32_t w = 0; w < kWaves; ++w) out += outs[w][threadIdx.x] * by[w];
+      S::store1(op + threadIdx.x, any_seen(total) ? out / total : 0.0f);
+    }
+    if (a.lse && threadIdx.x == 0) a.lse[row] = any_seen(total) ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
   }
 }
+static_assert(ZO_DIM_MAX == kThreads, "a thread writes a dim");
 
 template <class S, uint32_t kDim, uint32_t kRowWaves>
 int launch(Attend& a, hipStream_t st) {
@@ -1222,7 +1259,7 @@ int attend(Attend& a, uint32_t row_waves, hipStream_t st) {
     if (a.dim == 128) return rows<S, 128>(a, row_waves, st);
     if (a.dim == 256) return rows<S, 256>(a, row_waves, st);
   }
-  plain_kernel<S><<<dim3(std::min((a.tokens * a.heads * a.group - 1) / kWaves + 1, 4096u)), dim3(kThreads), 0, st>>>(a);
+  plain_kernel<S><<<dim3(std::min(a.tokens * a.heads * a.group, 65536u)), dim3(kThreads), 0, st>>>(a);
   return launched();
 }
 
