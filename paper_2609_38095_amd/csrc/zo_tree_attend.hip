@@ -1030,8 +1030,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   }
 }
 
-// Joins the parts of the items that were split. A workgroup takes every gridDim.x-th entry, and of its item's rows, four dims a thread,
-// every gridDim.y-th share; kSlices groups of its threads take every kSlices-th part each and join theirs through LDS, so that an item of
+// Joins the parts of the items that were split. A workgroup takes a run of entries (few items lie evenly among these, so that
+// every n-th entry would be all items to one), and of its items' rows, four dims a thread, every gridDim.y-th share; kSlices groups of its threads take every kSlices-th part each and join theirs through LDS, so that an item of
 // many parts is not read one after another.
 template <class S, uint32_t kRows, uint32_t kSlices>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
@@ -1040,12 +1040,14 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
   __shared__ f32x4 rows[kSlices > 1 ? kThreads : 1];
   const uint32_t quads = (a.dim + 3) / 4, lane = threadIdx.x % kWave, slice = threadIdx.x / kShare;
   uint32_t active = a.workers;
-  for (uint32_t base = blockIdx.x; base < active; base += gridDim.x * kWave) {
-    const uint32_t mine = base + lane * gridDim.x;
-    const Split own = a.splits[min(mine, a.workers - 1)];  // with the count at once: those behind it hold anything
+  for (uint32_t i0 = 0; i0 < (active + gridDim.x - 1) / gridDim.x; i0 += kWave) {
+    const Split guess = a.splits[min(blockIdx.x, a.workers - 1)];  // where each workgroup has one entry, with the count at once
     active = *a.active;
-    for (uint64_t left = __ballot(mine < active && own.last != 0); left != 0; left &= left - 1) {
-      const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left)), first = base + from * gridDim.x;
+    const uint32_t each = (active + gridDim.x - 1) / gridDim.x, mine = blockIdx.x * each + i0 + lane;
+    const bool have = i0 + lane < each && mine < active;
+    const Split own = each == 1 ? guess : a.splits[have ? mine : 0];
+    for (uint64_t left = __ballot(have && own.last != 0); left != 0; left &= left - 1) {
+      const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left)), first = blockIdx.x * each + i0 + from;
       const auto there = [&](uint32_t v) -> uint32_t { return __builtin_amdgcn_readlane(v, from); };
       const uint32_t last = there(own.last), slot = there(own.slot), token = there(own.token), row0 = there(own.row);
       const uint32_t item_rows = there(own.rows), head = there(own.head);
