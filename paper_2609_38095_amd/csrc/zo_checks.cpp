@@ -453,9 +453,18 @@ TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t 
   TreeShape s = {};
   if (heads == 0 || q_heads % heads != 0 || q_heads == 0 || seqs == 0 || tokens == 0) return s;
   const uint64_t group = q_heads / heads, rows = (tokens * group + seqs - 1) / seqs;  // of a sequence, on average
-  // keys and values of four waves' own tiles have to fit the LDS
-  const bool own_tiles = dim * elem_bytes(dtype) <= 512;
-  s.row_waves = rows <= 32 && own_tiles ? 1 : rows > 128 && dtype == ZO_BF16 && dim <= 128 ? 8 : 4;
+  // One row wave or more, us for 48 sequences of 500 to 4,000 tokens: bf16, heads of 128, 32 rows 104 | 120, 40 rows 134 | 123; of 64, 32
+  // rows 52 | 54, 40 rows 78 | 59; of 256, 32 rows 153 | 165, 40 rows 217 | 170; fp32, heads of 128, 64 rows 208 | 278, 96 rows 302 | 292;
+  // of 64, 64 rows 96 | 142, 128 rows 175 | 156. Keys and values of four waves' own tiles have to fit the LDS.
+  const uint64_t few = dtype == ZO_F32 ? 64 : 32;
+  // Eight row waves or four, bf16: heads of 128, 48 sequences, 40 rows 125 | 123, 128 rows 143 | 142, 384 rows 277 | 314; four sequences of
+  // 2,000 tokens, 128 rows 26 | 39 (fewer parts to join); of 64, 48 sequences, 128 rows 86 | 80, 384 rows 182 | 174, eight prompts of 4,096
+  // rows 94 | 107.
+  const uint64_t many = dim > 64 ? 0 : 1024;
+  if (rows <= few && dim * elem_bytes(dtype) <= 512)
+    s.row_waves = 1;
+  else
+    s.row_waves = rows > many && dtype == ZO_BF16 && dim <= 128 ? 8 : 4;
   s.rows = 32 * s.row_waves;
   s.workers = dim * elem_bytes(dtype) <= 256 && s.row_waves < 8 ? 512 : 256;
   return s;

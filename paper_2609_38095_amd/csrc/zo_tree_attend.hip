@@ -1246,10 +1246,14 @@ int rows(Attend& a, uint32_t row_waves, hipStream_t st) {
   if constexpr (kDim * sizeof(typename S::storage) <= 512) {
     if (row_waves == 1) return launch<S, kDim, 1>(a, st);
   }
-  if constexpr (Form<S, kDim, 8>::kPiped) {
-    if (row_waves == 8) return launch<S, kDim, 8>(a, st);
+  if constexpr (Form<S, kDim, 8>::kPiped && kDim > 64) {
+    return launch<S, kDim, 8>(a, st);
+  } else {
+    if constexpr (Form<S, kDim, 8>::kPiped) {
+      if (row_waves == 8) return launch<S, kDim, 8>(a, st);
+    }
+    return launch<S, kDim, 4>(a, st);
   }
-  return launch<S, kDim, 4>(a, st);
 }
 
 template <class S>

@@ -572,11 +572,12 @@ def test_two_graphs_and_a_given_workspace():
         held[0].zero_(), held[1].zero_()
 
 
-@pytest.mark.parametrize("dtype,dim,counts", [("bf16", 128, [300]), ("bf16", 256, [3, 2]), ("bf16", 256, [90]), ("f32", 128, [3, 2]), ("f32", 128, [90]),
-                                              ("f32", 256, [50, 20]), ("f32", 96, [9])])
+@pytest.mark.parametrize("dtype,dim,counts", [("bf16", 128, [300]), ("bf16", 64, [40]), ("bf16", 64, [600]), ("bf16", 256, [3, 2]), ("bf16", 256, [90]), ("f32", 128, [3, 2]), ("f32", 128, [90]),
+                                              ("f32", 256, [50, 20]), ("f32", 64, [90]), ("f32", 64, [3]), ("bf16", 128, [3]), ("bf16", 64, [3]),
+                                              ("f32", 96, [9])])
 def test_every_form_in_graphs_and_at_once(dtype, dim, counts):
     """Each form of the kernel, first called inside a capture: its replays, and calls on two streams at once."""
-    q, kc, vc, table, _ = attend_case([70] * len(counts), counts, 4, 2, dim, 16, "heads", dtype)
+    q, kc, vc, table, _ = attend_case([70] * len(counts), counts, 4, 2, dim, 16, "heads", dtype, 700)
     args = (kc, vc, dev(table), ints([70] * len(counts)), dev(starts_of(counts)))
     qs = [q, q.flip(0).contiguous()]
     graphs, held = [], []
