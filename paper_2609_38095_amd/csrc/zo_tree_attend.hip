@@ -210,7 +210,7 @@ struct Runs {
   }
 };
 
-// A part in the workspace: for each row [m, l, -, -, o[dim rounded up to 4]].
+// A part in the workspace: for each row [m, l, -, -, o[dim]].
 template <uint32_t kRows>
 __device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint32_t slot) {
   return a.parts + (static_cast<size_t>(worker) * 2 + slot) * kRows * a.part_row;
@@ -219,18 +219,20 @@ __device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint
 // Whether a row with the sum l of weights saw anything (a NaN among its scores counts).
 __device__ __forceinline__ bool any_seen(float l) { return l > 0.0f || l != l; }
 
-// Four dims of a row's output from its sums, and its log-sum once.
-template <class S>
-__device__ __forceinline__ void write_row(const Attend& a, uint32_t token, uint32_t q_head, uint32_t dim, float m, float l, f32x4 o) {
-  typedef typename S::storage T;
-  const bool any = any_seen(l);
-  T* op = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(token) * a.out_token + static_cast<int64_t>(q_head) * a.out_head;
-#pragma unroll
-  for (uint32_t i = 0; i < 4; ++i)
-    if (dim + i < a.dim) S::store1(op + dim + i, any ? o[i] / l : 0.0f);
-  if (a.lse && dim == 0)
-    a.lse[static_cast<size_t>(token) * a.heads * a.group + q_head] = any ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY;
+// Four dims of a row's output.
+template <class T>
+__device__ __forceinline__ void store_four(T* to, f32x4 four) {
+  if constexpr (sizeof(T) == 4) {
+    typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+    *reinterpret_cast<f32x4_any*>(to) = four;
+  } else {
+    typedef u32x2 __attribute__((aligned(2))) u32x2_any;
+    *reinterpret_cast<u32x2_any*>(to) = u32x2{pack_bf16x2(four[0], four[1]), pack_bf16x2(four[2], four[3])};
+  }
 }
+
+// The log-sum of a row's scores.
+__device__ __forceinline__ float log_sum(float m, float l) { return any_seen(l) ? (m + log2f(l)) * 0.69314718055994531f : -INFINITY; }
 
 // Sixteen bytes of values with zeros for those that are infinite or NaN.
 template <class T>
@@ -901,13 +903,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         const uint32_t out_row = row0 + i, out_node = node_of(a, out_row);
         T* to = reinterpret_cast<T*>(a.out) + static_cast<int64_t>(s.token + out_node) * a.out_token +
                 static_cast<int64_t>(head * a.group + out_row - out_node * a.group) * a.out_head + dim;
-        if constexpr (kWide) {
-          typedef f32x4 __attribute__((aligned(4))) f32x4_any;
-          *reinterpret_cast<f32x4_any*>(to) = four;
-        } else {
-          typedef u32x2 __attribute__((aligned(2))) u32x2_any;
-          *reinterpret_cast<u32x2_any*>(to) = u32x2{pack_bf16x2(four[0], four[1]), pack_bf16x2(four[2], four[3])};
-        }
+        store_four(to, four);
       } else {
         *reinterpret_cast<f32x4*>(parts + static_cast<size_t>(i) * a.part_row + 4 + dim) = four;
       }
@@ -916,7 +912,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       if (!whole)
         *reinterpret_cast<float2*>(parts + static_cast<size_t>(i) * a.part_row) = make_float2(row_m, row_l);
       else if (a.lse)
-        a.lse[static_cast<size_t>(out_token) * a.heads * a.group + out_head] = any_seen(row_l) ? (row_m + log2f(row_l)) * 0.69314718055994531f : -INFINITY;
+        a.lse[static_cast<size_t>(out_token) * a.heads * a.group + out_head] = log_sum(row_m, row_l);
     };
     // What a whole row's sum is multiplied by; a row that saw nothing holds zeros.
     const auto over = [&](float row_l) { return whole && any_seen(row_l) ? 1.0f / row_l : 1.0f; };
@@ -1033,12 +1029,13 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 // Joins the parts of the items that were split. A workgroup takes a run of entries (few items lie evenly among these, so that
 // every n-th entry would be all items to one), and of its items' rows, four dims a thread, every gridDim.y-th share; kSlices groups of its threads take every kSlices-th part each and join theirs through LDS, so that an item of
 // many parts is not read one after another.
-template <class S, uint32_t kRows, uint32_t kSlices>
+template <class S, uint32_t kDim, uint32_t kRows, uint32_t kSlices>
 __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
-  constexpr uint32_t kShare = kThreads / kSlices;
+  typedef typename S::storage T;
+  constexpr uint32_t kShare = kThreads / kSlices, kQuads = kDim / 4;
   __shared__ float2 sums[kSlices > 1 ? kThreads : 1];
   __shared__ f32x4 rows[kSlices > 1 ? kThreads : 1];
-  const uint32_t quads = (a.dim + 3) / 4, lane = threadIdx.x % kWave, slice = threadIdx.x / kShare;
+  const uint32_t lane = threadIdx.x % kWave, slice = threadIdx.x / kShare;
   uint32_t active = a.workers;
   for (uint32_t i0 = 0; i0 < (active + gridDim.x - 1) / gridDim.x; i0 += kWave) {
     const Split guess = a.splits[min(blockIdx.x, a.workers - 1)];  // where each workgroup has one entry, with the count at once
@@ -1051,8 +1048,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
       const auto there = [&](uint32_t v) -> uint32_t { return __builtin_amdgcn_readlane(v, from); };
       const uint32_t last = there(own.last), slot = there(own.slot), token = there(own.token), row0 = there(own.row);
       const uint32_t item_rows = there(own.rows), head = there(own.head);
-      for (uint32_t share = blockIdx.y; share * kShare < item_rows * quads; share += gridDim.y) {
-        const uint32_t e = share * kShare + threadIdx.x % kShare, row = e / quads, dim = (e - row * quads) * 4;
+      for (uint32_t share = blockIdx.y; share * kShare < item_rows * kQuads; share += gridDim.y) {
+        const uint32_t e = share * kShare + threadIdx.x % kShare, row = e / kQuads, dim = e % kQuads * 4;
         float m = -INFINITY, l = 0.0f;
         f32x4 o = {0, 0, 0, 0};
         const auto add = [&](float2 ml, f32x4 po) {
@@ -1079,8 +1076,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
             for (uint32_t n = 1; n < kSlices; ++n) add(sums[threadIdx.x + n * kShare], rows[threadIdx.x + n * kShare]);
         }
         if (slice == 0 && row < item_rows) {
-          const uint32_t node = node_of(a, row0 + row);
-          write_row<S>(a, token + node, head * a.group + row0 + row - node * a.group, dim, m, l, o);
+          const uint32_t node = node_of(a, row0 + row), q_head = head * a.group + row0 + row - node * a.group;
+          store_four(reinterpret_cast<T*>(a.out) + static_cast<int64_t>(token + node) * a.out_token + static_cast<int64_t>(q_head) * a.out_head + dim,
+                     o * (any_seen(l) ? 1.0f / l : 0.0f));
+          if (a.lse && dim == 0) a.lse[static_cast<size_t>(token + node) * a.heads * a.group + q_head] = log_sum(m, l);
         }
       }
     }
@@ -1216,7 +1215,7 @@ __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
       for (uint32_t w = 0; w < kWaves; ++w) out += outs[w][threadIdx.x] * by[w];
       S::store1(op + threadIdx.x, any_seen(total) ? out / total : 0.0f);
     }
-    if (a.lse && threadIdx.x == 0) a.lse[row] = any_seen(total) ? (top + log2f(total)) * 0.69314718055994531f : -INFINITY;
+    if (a.lse && threadIdx.x == 0) a.lse[row] = log_sum(top, total);
   }
 }
 static_assert(ZO_DIM_MAX == kThreads, "a thread writes a dim");
@@ -1235,9 +1234,9 @@ int launch(Attend& a, hipStream_t st) {
   const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;
   const uint32_t most = static_cast<uint32_t>(std::min<uint64_t>(a.workers, items));
   if (items * 6 <= a.workers)
-    join_kernel<S, F::kRows, 4><<<dim3(most, std::min(32u, F::kRows * kDim / 256)), dim3(kThreads), 0, st>>>(a);
+    join_kernel<S, kDim, F::kRows, 4><<<dim3(most, std::min(32u, F::kRows * kDim / 256)), dim3(kThreads), 0, st>>>(a);
   else
-    join_kernel<S, F::kRows, 1><<<dim3(most, std::min(16u, F::kRows * kDim / 1024)), dim3(kThreads), 0, st>>>(a);
+    join_kernel<S, kDim, F::kRows, 1><<<dim3(most, std::min(16u, F::kRows * kDim / 1024)), dim3(kThreads), 0, st>>>(a);
   return launched();
 }
 
@@ -1315,7 +1314,7 @@ extern "C" int zo_tree_attend(const zo_tree_attention* p, void* stream) {
   a.heads = p->cache.heads;
   a.dim = p->cache.dim;
   a.workers = shape.workers;
-  a.part_row = (a.dim + 3) / 4 * 4 + 4;
+  a.part_row = a.dim + 4;
   a.scale = p->scale * 1.4426950408889634f;
   (void)hipGetLastError();
   hipStream_t st = static_cast<hipStream_t>(stream);
