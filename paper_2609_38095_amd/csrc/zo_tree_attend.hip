@@ -41,13 +41,13 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr uint32_t kThreads = 256, kWave = 64, kWaves = kThreads / kWave, kXcds = 8;
 constexpr float kLazy = 8.0f;  // how far (in powers of two) the bound of the scores is set above their maximum
 
-// An item that was split: its parts are those of the workgroup that this is the entry of, in slot `slot`, and of the ones up to `last`, in
+// An item that was split: its parts are those of the workgroup that this is the entry of, in slot 1, and of the ones up to `last`, in
 // slot 0. At most one item that is split begins in a workgroup's run. last = 0: none does. Written by the workgroup of the item's last
 // tile, or by the entry's own workgroup where none is split.
 struct Split {
-  uint32_t last, slot;
+  uint32_t last;
   uint32_t token, row, rows, head;  // the sequence's first new token; the item's first row and their number; key head
-  uint32_t unused[2];
+  uint32_t unused[3];
 };
 static_assert(sizeof(Split) == kTreeSplitWords * 4, "the workspace holds entries of this size");
 
@@ -62,7 +62,7 @@ struct Attend {
   const uint64_t* seen;
   int64_t seen_stride, q_token, q_head, out_token, out_head, page_bytes, head_bytes, token_bytes, table_stride;
   double inv_group, inv_page;  // of a group's query heads; of a page's sixteens
-  uint32_t tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row;
+  uint32_t tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row, visit;
   float scale;         // times log2(e)
 };
 
@@ -116,10 +116,14 @@ __device__ __forceinline__ uint32_t visible(const Attend& a, const Seq& s, uint3
   return min(s.len, s.cached + node_of(a, min(row, rows) - 1) + 1);
 }
 
-// Tiles of an item; at least one, which writes the rows that see nothing.
+// Tiles of an item; at least one, which writes the rows that see nothing. Its cost is a.visit tiles more.
 template <uint32_t kRows, uint32_t kTile>
 __device__ __forceinline__ uint32_t tiles_of(const Attend& a, const Seq& s, uint32_t block) {
   return max(1u, (visible(a, s, (block + 1) * kRows) + kTile - 1) / kTile);
+}
+template <uint32_t kRows, uint32_t kTile>
+__device__ __forceinline__ uint32_t cost_of(const Attend& a, const Seq& s, uint32_t block) {
+  return tiles_of<kRows, kTile>(a, s, block) + a.visit;
 }
 
 // The sum over a wave of a value of each lane, and the sums up to each lane.
@@ -132,16 +136,16 @@ __device__ __forceinline__ uint64_t sums_upto(uint64_t v, uint32_t lane) {
   return v;
 }
 
-// Tiles of one key head of a sequence, by all lanes together.
+// The cost of one key head of a sequence, by all lanes together.
 template <uint32_t kRows, uint32_t kTile>
-__device__ uint64_t head_tiles(const Attend& a, const Seq& s, uint32_t lane) {
-  if (a.seen) return static_cast<uint64_t>(s.blocks) * tiles_of<kRows, kTile>(a, s, 0);
+__device__ uint64_t head_cost(const Attend& a, const Seq& s, uint32_t lane) {
+  if (a.seen) return static_cast<uint64_t>(s.blocks) * cost_of<kRows, kTile>(a, s, 0);
   uint64_t mine = 0;
-  for (uint32_t b = lane; b < s.blocks; b += kWave) mine += tiles_of<kRows, kTile>(a, s, b);
+  for (uint32_t b = lane; b < s.blocks; b += kWave) mine += cost_of<kRows, kTile>(a, s, b);
   return uniform(__shfl(sums_upto(mine, lane), 63, 64));
 }
 
-// Tiles before each thread's sequences, and the sequences where each thread has one. Thread t counts sequences [t each, (t + 1) each).
+// The cost before each thread's sequences, and the sequences where each thread has one. Thread t counts sequences [t each, (t + 1) each).
 struct Deal {
   uint64_t total;
   uint32_t each;
@@ -150,11 +154,11 @@ struct Deal {
 template <uint32_t kRows, uint32_t kTile, uint32_t kThreads>
 __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
   constexpr uint32_t kWaves = kThreads / kWave;
-  __shared__ uint64_t wave_tiles[kWaves];
+  __shared__ uint64_t wave_cost[kWaves];
   const uint32_t lane = threadIdx.x % kWave;
   Deal d;
   d.each = (a.seqs + kThreads - 1) / kThreads;
-  uint64_t tiles = 0;
+  uint64_t cost = 0;
   for (uint32_t i = 0; i < d.each; ++i) {
     const uint32_t seq = threadIdx.x * d.each + i;
     Seq s = {};
@@ -162,10 +166,10 @@ __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
     if (d.each == 1) seqs[threadIdx.x] = s;
     constexpr uint32_t kFew = 8;  // blocks that a thread counts by itself; a longer sequence's by the whole wave
     if (a.seen) {
-      if (s.blocks) tiles += static_cast<uint64_t>(s.blocks) * tiles_of<kRows, kTile>(a, s, 0);
+      if (s.blocks) cost += static_cast<uint64_t>(s.blocks) * cost_of<kRows, kTile>(a, s, 0);
     } else {
       if (s.blocks <= kFew)
-        for (uint32_t b = 0; b < s.blocks; ++b) tiles += tiles_of<kRows, kTile>(a, s, b);
+        for (uint32_t b = 0; b < s.blocks; ++b) cost += cost_of<kRows, kTile>(a, s, b);
       for (uint64_t left = __ballot(s.blocks > kFew); left != 0; left &= left - 1) {
         const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left));
         Seq one;
@@ -174,26 +178,26 @@ __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
         one.cached = __builtin_amdgcn_readlane(s.cached, from);
         one.len = __builtin_amdgcn_readlane(s.len, from);
         one.blocks = __builtin_amdgcn_readlane(s.blocks, from);
-        const uint64_t all = head_tiles<kRows, kTile>(a, one, lane);
-        if (lane == from) tiles += all;
+        const uint64_t all = head_cost<kRows, kTile>(a, one, lane);
+        if (lane == from) cost += all;
       }
     }
   }
-  const uint64_t upto = sums_upto(tiles, lane);
-  if (lane == 63) wave_tiles[threadIdx.x / kWave] = upto;
+  const uint64_t upto = sums_upto(cost, lane);
+  if (lane == 63) wave_cost[threadIdx.x / kWave] = upto;
   __syncthreads();
   uint64_t at = 0, all = 0;
   for (uint32_t w = 0; w < kWaves; ++w) {
-    if (w < threadIdx.x / kWave) at += wave_tiles[w];
-    all += wave_tiles[w];
+    if (w < threadIdx.x / kWave) at += wave_cost[w];
+    all += wave_cost[w];
   }
-  before[threadIdx.x] = (at + upto - tiles) * a.heads;
+  before[threadIdx.x] = (at + upto - cost) * a.heads;
   d.total = uniform(all * a.heads);
   __syncthreads();
   return d;
 }
 
-// The first tile of each worker: total tiles in equal runs, the first ones a tile longer.
+// The run of each worker: the total cost in equal parts, the first ones longer by one.
 struct Runs {
   uint64_t each, longer;
   uint32_t workers;
@@ -204,9 +208,9 @@ struct Runs {
     longer = total - each * workers;
   }
   __device__ uint64_t first(uint32_t w) const { return w * each + (w < longer ? w : longer); }
-  __device__ uint32_t worker_of(uint64_t tile) const {
-    const uint64_t head = longer * (each + 1);  // tiles of the longer runs
-    return static_cast<uint32_t>(tile < head ? quotient(tile, each + 1) : longer + quotient(tile - head, each));
+  __device__ uint32_t worker_of(uint64_t place) const {
+    const uint64_t head = longer * (each + 1);  // of the longer runs
+    return static_cast<uint32_t>(place < head ? quotient(place, each + 1) : longer + quotient(place - head, each));
   }
 };
 
@@ -273,6 +277,7 @@ struct Form {
   static constexpr uint32_t kBufferBytes = 2 * kTile * kRowBytes;
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
   static constexpr bool kPiped = kRowWaves > 1 && sizeof(T) == 2 && kBlocks == 2;
+  static constexpr uint32_t kVisit = kRowWaves > 1 ? 4 : 1;
   static constexpr uint32_t kSimdWaves = kRowBytes <= 256 ? 2 : 1;
   static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
 };
@@ -323,9 +328,9 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   uint64_t at = begin;
   if (at >= end) return;
 
-  // the sequence, key head and block that tile `at` lies in
+  // the sequence, key head and block that `at` lies in
   uint32_t seq, head, block;
-  uint64_t item_first;
+  uint64_t item_first;  // the item's first tile, behind its own cost
   Seq s;
   {
     const Attend a = arguments();
@@ -335,23 +340,23 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       if (before[chunk + step] <= at) chunk += step;
     chunk = uniform(chunk);
     seq = chunk * d.each;
-    uint64_t first = uniform(before[chunk]), tiles;
+    uint64_t first = uniform(before[chunk]), cost;
     for (;; ++seq) {  // `at` < the total: a sequence holds it
       s = uniform(d.each == 1 ? seqs[seq] : seq_of<kRows>(a, seq));
-      tiles = s.blocks ? head_tiles<kRows, kTile>(a, s, lane) : 0;
-      if (at < first + tiles * a.heads) break;
-      first += tiles * a.heads;
+      cost = s.blocks ? head_cost<kRows, kTile>(a, s, lane) : 0;
+      if (at < first + cost * a.heads) break;
+      first += cost * a.heads;
     }
-    head = uniform(static_cast<uint32_t>(quotient(at - first, tiles)));
-    first += tiles * head;
+    head = uniform(static_cast<uint32_t>(quotient(at - first, cost)));
+    first += cost * head;
     uint64_t rest = at - first;
     if (a.seen) {
-      const uint32_t each = tiles_of<kRows, kTile>(a, s, 0);
+      const uint32_t each = cost_of<kRows, kTile>(a, s, 0);
       block = uniform(static_cast<uint32_t>(quotient(rest, each)));
       item_first = first + static_cast<uint64_t>(block) * each;
     } else {
       for (block = 0;; block += kWave) {
-        const uint32_t mine = block + lane < s.blocks ? tiles_of<kRows, kTile>(a, s, block + lane) : 0;
+        const uint32_t mine = block + lane < s.blocks ? cost_of<kRows, kTile>(a, s, block + lane) : 0;
         const uint64_t upto = sums_upto(mine, lane);
         const uint64_t over = __ballot(upto > rest);
         if (over != 0) {
@@ -365,7 +370,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         rest -= all;
       }
     }
-    item_first = uniform(item_first);
+    item_first = uniform(item_first + a.visit);
     block = uniform(block);
   }
 
@@ -388,12 +393,12 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   }
 
   if (threadIdx.x == 0) odd_there[0] = 0;
-  for (uint32_t turn = 0; at < end; turn ^= 1) {
+  for (uint32_t turn = 0; at < end && item_first < end; turn ^= 1) {
     const Attend a = arguments();
     const uint32_t rows = s.count * a.group, row0 = block * kRows, in_block = min(kRows, rows - row0);
     const uint32_t sees = uniform(visible(a, s, row0 + kRows));
     const uint32_t tiles = max(1u, (sees + kTile - 1) / kTile);
-    const uint32_t t_begin = uniform(static_cast<uint32_t>(at - item_first));
+    const uint32_t t_begin = uniform(at <= item_first ? 0u : static_cast<uint32_t>(at - item_first));
     const uint32_t t_end = uniform(end - item_first < tiles ? static_cast<uint32_t>(end - item_first) : tiles);
     // the lane's row, and what all rows of the workgroup and of the wave see for certain
     const uint32_t row = row0 + rw * 32 + r;
@@ -887,17 +892,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     l += __shfl_xor(l, 32, 64);
 
     const bool whole = t_begin == 0 && t_end == tiles;
-    if (threadIdx.x == 0) {
-      if (t_end == tiles && !whole) {  // so it began in another run
-        const uint32_t first = runs.worker_of(item_first);
-        a.splits[first] = Split{worker, runs.first(first) == item_first ? 0u : 1u, s.token, row0, in_block, head, {0, 0}};
-      }
-      // at the run's end: unless an item goes on that began in it
-      const uint64_t item_end = item_first + tiles;
-      if (item_end == end || (item_end > end && item_first < begin)) a.splits[worker].last = 0;
-    }
+    if (threadIdx.x == 0 && t_end == tiles && !whole)  // so it began in another run
+      a.splits[runs.worker_of(item_first)] = Split{worker, s.token, row0, in_block, head, {0, 0, 0}};
     // Results through LDS, for whole lines: rows swizzled by 16 bytes, then four dims of a row for each lane.
-    float* parts = part_at<kRows>(a, worker, at == begin ? 0 : 1);
+    float* parts = part_at<kRows>(a, worker, t_begin == 0 ? 1 : 0);
     const auto write_four = [&](uint32_t i, uint32_t dim, f32x4 four) {  // of row i of the item
       if (whole) {
         const uint32_t out_row = row0 + i, out_node = node_of(a, out_row);
@@ -1010,7 +1008,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     // the next item
     at = item_first + t_end;
     if (t_end == tiles) {
-      item_first += tiles;
+      item_first = at + a.visit;
       if (++block == s.blocks) {
         block = 0;
         if (++head == a.heads) {
@@ -1024,6 +1022,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       }
     }
   }
+  // unless the last item goes on that began in this run
+  if (threadIdx.x == 0 && !(item_first >= runs.first(worker) && item_first < at)) arguments().splits[worker].last = 0;
 }
 
 // Joins the parts of the items that were split. A workgroup takes a run of entries (few items lie evenly among these, so that
@@ -1046,7 +1046,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
     for (uint64_t left = __ballot(have && own.last != 0); left != 0; left &= left - 1) {
       const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left)), first = blockIdx.x * each + i0 + from;
       const auto there = [&](uint32_t v) -> uint32_t { return __builtin_amdgcn_readlane(v, from); };
-      const uint32_t last = there(own.last), slot = there(own.slot), token = there(own.token), row0 = there(own.row);
+      const uint32_t last = there(own.last), token = there(own.token), row0 = there(own.row);
       const uint32_t item_rows = there(own.rows), head = there(own.head);
       for (uint32_t share = blockIdx.y; share * kShare < item_rows * kQuads; share += gridDim.y) {
         const uint32_t e = share * kShare + threadIdx.x % kShare, row = e / kQuads, dim = e % kQuads * 4;
@@ -1062,7 +1062,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
         if (row < item_rows) {
 #pragma unroll 4
           for (uint32_t w = first + slice; w <= last; w += kSlices) {
-            const float* part = part_at<kRows>(a, w, w == first ? slot : 0) + static_cast<size_t>(row) * a.part_row;
+            const float* part = part_at<kRows>(a, w, w == first ? 1 : 0) + static_cast<size_t>(row) * a.part_row;
             add(*reinterpret_cast<const float2*>(part), *reinterpret_cast<const f32x4*>(part + 4 + dim));
           }
         }
@@ -1227,11 +1227,12 @@ int launch(Attend& a, hipStream_t st) {
       hipFuncSetAttribute(reinterpret_cast<const void*>(&attend_kernel<S, kDim, kRowWaves>), hipFuncAttributeMaxDynamicSharedMemorySize,
                           F::kLds) != hipSuccess)
     return ZO_ERR_HIP;
+  const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;  // there are no more
+  a.visit = items * 2 >= a.workers ? F::kVisit : 0;
   attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(F::kThreads), F::kLds, st>>>(a);
   const int rc = launched();
   if (rc != ZO_OK) return rc;
-  // no more items are split than there are; slices where an item has several parts
-  const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;
+  // slices where an item has several parts
   const uint32_t most = static_cast<uint32_t>(std::min<uint64_t>(a.workers, items));
   if (items * 6 <= a.workers)
     join_kernel<S, kDim, F::kRows, 4><<<dim3(most, std::min(32u, F::kRows * kDim / 256)), dim3(kThreads), 0, st>>>(a);
