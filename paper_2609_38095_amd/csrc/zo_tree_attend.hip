@@ -6,21 +6,32 @@
 //
 // Split. An item is a sequence, a key head and kRows rows; it is cut into tiles of kTile tokens up to the last one that a row of
 // it can see. The tiles of all items, in order, are dealt out in equal runs to the workgroups, which find theirs from
-// lengths and starts by themselves. A run that covers an item writes its output, others leave (m, l, o) in the workspace, at most
-// two parts for each workgroup, and join_kernel joins them. Runs that follow each other, which read the same keys, lie on one XCD.
+// lengths and starts by themselves; an item's own time (first loads, results) counts as a few tiles more. A run that covers an item writes
+// its output, others leave (m, l, o) in the workspace, at most two parts for each workgroup, and join_kernel joins them. Runs
+// that follow each other, which read the same keys, lie on one XCD.
 //
 // Tile. S^T = K Q^T and O^T = V^T P^T in 32 x 32 products, a row in each lane (r = lane % 32), so a row's bound and sum stay in
-// its two lanes (g = lane / 32). A wave has 32 rows. kRowWaves = 4: four waves have different rows and share a tile's keys and
+// its two lanes (g = lane / 32). A wave has 32 rows. kRowWaves = 8 or 4: the waves have different rows and share a tile's keys and
 // values, two buffers of them in LDS; kRowWaves = 1 (sequences of few rows): four waves have the same rows and a quarter of the
-// tile's keys each, in LDS of their own, without a barrier; they join at an item's end. The next tile waits in
-// registers while one is used.
-//   - LDS rows are swizzled by 16-byte chunks, so that neither product's reads meet in a bank;
+// tile's keys each, in LDS of their own, without a barrier; they join at an item's end. Which form is taken is measured in tree_shape().
+//   - Keys and values go straight into LDS, 16 bytes a lane, a tile ahead of their use (through registers: prompts 2,198 us, this way
+//     1,847 at that step). LDS rows are swizzled by 16-byte chunks, so that neither product's reads meet in a bank;
 //   - S^T leaves in lane (r, g) the keys 8 i + 4 g .. + 3: the second product's operand as it is, if the contraction's index
 //     is permuted alike; the values' operand is read by the transposing LDS read (bf16), four keys of 16 dims at a time.
+//   - bf16 heads of 64 and 128 in more than one row wave run as a pipeline of 32 keys (step()): the products of one block's scores and of
+//     another's weights with the values lie under the exponentials of the one between, one barrier a tile (1,847 -> 1,263 us).
 //
 // What a row does not see. Scores are masked, and values that no row of the call may use are zeros in LDS. A value that is infinite or
 // NaN in a tile that only some of the rows see would reach the others as 0 times itself: it is a zero in LDS too, and is
 // added to the results of the rows that see it after these are written.
+//
+// Rounding. fp32 sums and bounds. The pipeline rounds bf16 weights once, an error of up to 2^-8 of the weighted magnitudes before the output's
+// own rounding; weights of two parts bound that form by the matrix cores (1,847 us). Outputs and log-sums go by the sum of the weights before
+// they are rounded; a second sum, of the rounded ones, would give a row that sees one key that key's value, and costs 3 % (prompts
+// 1,051 -> 1,078 us, 48 trees 173 -> 178). The other bf16 forms take weights as a sum of two bf16.
+//
+// Measured: prompts (8 of 2,048 heads' rows and more) @PROMPTS@; 48 trees @BATCH@; fp32 trees @F32@; one answer's tree @ONE@, most
+// of which is latency: the deal 2 us, first loads 3, results 3, the join 4.
 
 #include <algorithm>
 #include <cmath>
@@ -277,6 +288,8 @@ struct Form {
   static constexpr uint32_t kBufferBytes = 2 * kTile * kRowBytes;
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
   static constexpr bool kPiped = kRowWaves > 1 && sizeof(T) == 2 && kBlocks == 2;
+  // An item's own time in tiles. 0: prompts 1,082 us, 48 trees 190, fp32 trees (one row wave) 91; 2: 1,069, 180, 86; 4: 1,038, 171, 90;
+  // 6: 1,045, 171, 91; 1: fp32 trees 85.
   static constexpr uint32_t kVisit = kRowWaves > 1 ? 4 : 1;
   static constexpr uint32_t kSimdWaves = kRowBytes <= 256 ? 2 : 1;
   static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
@@ -293,6 +306,9 @@ __device__ __forceinline__ void load_to_lds(uint32_t to, uint64_t base, uint32_t
 template <int kLeft>
 __device__ __forceinline__ void loads_left() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
+  // The same, for the compiler: what it brought back from scratch memory before a loop is there as well, and it adds no waits inside the
+  // loop, which would be for all of the wave's loads (48 trees 199 -> 173 us).
+  __builtin_amdgcn_s_waitcnt(kLeft % 16 | 7 << 4 | 15 << 8 | kLeft / 16 << 14);
 }
 
 // Heads of kDim, pages of whole sixteens of tokens, rows at 16-byte aligned places.
@@ -654,18 +670,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
           }
           const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], scale, -ref));
           const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], scale, -ref));
-          now[n] = pack_bf16x2(p0, p1);
-          asm volatile("" : "+v"(now[n]));  // here, under the products, and not where it is used
+          l += p0 + p1;
+          now[n] = pack_bf16x2(p0, p1);  // one rounding
+          asm volatile("" : "+v"(now[n]), "+v"(l));  // here, under the products, and not where they are used
         }
-        // weights are rounded to bf16 once, and l is the sum of the rounded ones
-        float sum0 = 0.0f, sum1 = 0.0f;
-        const bf16x2 ones = {static_cast<__bf16>(1.0f), static_cast<__bf16>(1.0f)};
-#pragma unroll
-        for (uint32_t n = 0; n < 8; n += 2) {
-          sum0 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, now[n]), ones, sum0, false);
-          sum1 = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, now[n + 1]), ones, sum1, false);
-        }
-        l += sum0 + sum1;
 #pragma unroll
         for (int n = 0; n < 8; ++n) weights[n] = now[n];
         if constexpr (kScores) x = y;
@@ -1088,7 +1096,8 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
 
 // Any head size, page size and alignment: a workgroup has a row at a time, its waves every fourth 64 keys. 64 keys' scores at once, one
 // in each lane, then their values, a dim in each lane (and the dims 64, 128 and 192 behind it); each 64's sum is added to what was
-// there, and the waves join at the end. A token that the row does not see is not read. Every row reads its keys anew.
+// there, and the waves join at the end. A token that the row does not see is not read. Every row reads its keys anew. 40 new tokens of
+// 4 heads of 96 behind 1,000: 73 us in bf16, 47 in fp32 (heads of 128 by the other kernel: 17 and 21).
 template <class S>
 __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
   typedef typename S::storage T;
@@ -1228,6 +1237,7 @@ int launch(Attend& a, hipStream_t st) {
                           F::kLds) != hipSuccess)
     return ZO_ERR_HIP;
   const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;  // there are no more
+  // with few items all workgroups have one or two, and what an item costs would only leave some without a tile
   a.visit = items * 2 >= a.workers ? F::kVisit : 0;
   attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(F::kThreads), F::kLds, st>>>(a);
   const int rc = launched();
