@@ -234,9 +234,14 @@ __device__ __forceinline__ float* part_at(const Attend& a, uint32_t worker, uint
 // Whether a row with the sum l of weights saw anything (a NaN among its scores counts).
 __device__ __forceinline__ bool any_seen(float l) { return l > 0.0f || l != l; }
 
-// Four dims of a row's output.
+// Four dims of a row's output. Where weights were rounded a mean of the largest bf16 values can come out above them: it is the largest one.
 template <class T>
 __device__ __forceinline__ void store_four(T* to, f32x4 four) {
+  if constexpr (sizeof(T) == 2) {
+    constexpr float kMost = 3.3895313892515355e38f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) four[i] = fabsf(four[i]) <= 3.402823466e38f ? __builtin_amdgcn_fmed3f(four[i], -kMost, kMost) : four[i];
+  }
   if constexpr (sizeof(T) == 4) {
     typedef f32x4 __attribute__((aligned(4))) f32x4_any;
     *reinterpret_cast<f32x4_any*>(to) = four;
@@ -1170,7 +1175,7 @@ __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
       float top = score;
 #pragma unroll
       for (uint32_t n = 1; n < kWave; n *= 2) top = fmaxf(top, __shfl_xor(top, n, 64));
-      top = fmaxf(top, m);
+      top = top > m ? top + kLazy : m;
       const float ref = top == -INFINITY ? 0.0f : top, by = __builtin_amdgcn_exp2f(m - ref);
       const float weight = place >= 0 ? __builtin_amdgcn_exp2f(score - ref) : 0.0f;
       float all = weight;

@@ -340,6 +340,19 @@ def test_the_largest_finite_values_stay_finite(dim, page, nodes, dtype):
     assert bool(((out > 0.99 * most) & (out < most)).all())
 
 
+@pytest.mark.parametrize("dim,group", [(64, 1), (64, 16), (128, 2), (256, 2), (96, 2)])
+def test_means_of_the_largest_values_stay_finite(dim, group):
+    """Every value the largest bf16 one: so is every mean, whatever the weights round to (2^-8 of it below at most, and its own rounding).
+    Not so in fp32: a mean is off by a few e there, and the largest fp32 number times 1 + e is infinite."""
+    most = torch.finfo(torch.bfloat16).max
+    q, kc, vc, table, _ = attend_case([0, 200], [90, 70], 2 * group, 2, dim, 16, "heads", "bf16")
+    vc.fill_(most)
+    vc[..., 1::2] = -most
+    for starts in ([0, 90, 160], [0, 1, 160]):
+        out = zo.zo_tree_attend(q, kc, vc, dev(table), ints([0, 200]), ints(starts)).float()
+        assert bool(((out.abs() <= most) & (out.abs() >= most * (1 - 2.0 ** -7))).all()) and bool((out[..., 0] > 0).all())
+
+
 def test_attend_leaves_other_rows():
     """Rows in front of the first sequence's and behind the last one's stay as they were; starts outside the rows count as the
     nearest; the result may be a view."""
