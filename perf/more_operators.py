@@ -424,7 +424,7 @@ def _plain_keep(s):
 def _own(s):
     import paper_2609_38095_amd as zo
     if s["op"] == "lay":
-        seqs, positions, places, seen = zo.zo_tree_lay(s["starts"], s["lengths"], s["tokens"], s["parents"], s["words"])
+        seqs, positions, places, seen = zo.zo_tree_lay(s["starts"], s["lengths"], s["tokens"], s["parents"], s["words"] if s["parents"] is not None else 0)
         return (seqs, positions, places) if seen is None else (seqs, positions, places, seen)
     if s["op"] == "put":
         q = zo.zo_norm_rotate_put(s["q"], s["k"], s["v"], s["k_cache"], s["v_cache"], s["table"], s["positions"], s["turns"],
