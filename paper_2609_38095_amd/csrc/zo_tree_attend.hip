@@ -15,7 +15,7 @@
 // values, two buffers of them in LDS; kRowWaves = 1 (sequences of few rows): four waves have the same rows and a quarter of the
 // tile's keys each, in LDS of their own, without a barrier; they join at an item's end. Which form is taken is measured in tree_shape().
 //   - Keys and values go straight into LDS, 16 bytes a lane, a tile ahead of their use (through registers: prompts 2,198 us, this way
-//     1,847 at that step). LDS rows are swizzled by 16-byte chunks, so that neither product's reads meet in a bank;
+//     1,847 at that step). LDS rows are swizzled by 16-byte chunks, so that few reads meet in a bank;
 //   - S^T leaves in lane (r, g) the keys 8 i + 4 g .. + 3: the second product's operand as it is, if the contraction's index
 //     is permuted alike; the values' operand is read by the transposing LDS read (bf16), four keys of 16 dims at a time.
 //   - bf16 heads of 64 and 128 in more than one row wave run as a pipeline of 32 keys (step()): the products of one block's scores and of
@@ -401,7 +401,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   const uint32_t stage_row = rw * F::kStageRows, load_row = lane / kChunks, load_chunk = lane % kChunks;
   char* own = lds + kw * 2 * kKeys * kRowBytes;  // the keys of the waves that share them, and their values behind these
   // Rows are swizzled by 16-byte chunks: eight neighbouring rows' same chunks (the keys' reads), and four rows' four chunks (the values')
-  // lie in different banks.
+  // lie in different banks. The keys' still meet a third of the time: lanes are served in groups of rows 0-3, 12-15, 20-23 and 24-27. A swizzle of
+  // theirs over sixteen rows ends that, and the offsets of two swizzles cost registers: prompts 1,074 -> 1,069 us, 48 trees 175 -> 178.
   const auto swizzle = [](uint32_t row) {
     return kChunks >= 16 ? row % 4 * 4 + row / 4 % 2 : row / 2 % 2 * 4 + row / 4 % 2;
   };
