@@ -746,12 +746,16 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         }
       }
     } else {
+      // a wave that has keys of its own leaves out a last tile that ends before them
+      const uint32_t t_last = kRowWaves > 1 ? t_end : uniform(min(t_end, sees > kw * kKeys ? (sees - kw * kKeys + kTile - 1) / kTile : 0u));
       find_sixteens(sixteen_of(t_begin) / 64, sixteens_id(sixteen_of(t_begin) / 64));
       Places now_at = places_of(t_begin), next_at = now_at;
       __syncthreads();  // the item before is done with the LDS
       if (threadIdx.x == 0) odd_there[turn ^ 1] = 0;
-      bring_keys(now_at, 0);
-      bring_values(now_at, 0);
+      if (t_begin < t_last) {
+        bring_keys(now_at, 0);
+        bring_values(now_at, 0);
+      }
       if constexpr (kRowWaves > 1) {
         loads_left<0>();
         mend(t_begin, 0, now_at.live);
@@ -759,8 +763,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       ready();
 
       uint32_t buffer = 0;
-      for (uint32_t t = t_begin; t < t_end; ++t) {
-        const bool more = t + 1 < t_end;
+      for (uint32_t t = t_begin; t < t_last; ++t) {
+        const bool more = t + 1 < t_last;
         const uint32_t other = (buffer + 1) % F::kBuffers;
         if constexpr (kRowWaves > 1) {
           if (more) {
