@@ -69,9 +69,7 @@ int zo_norm_rotate_put_at(const zo_rotate_put* p, const int32_t* places, void* s
  * second launch. work: device memory of zo_tree_attend_work() bytes, aligned to 16, contents irrelevant, one
  * for each call in flight. Heads of 64, 128 and 256 in pages of whole sixteens of tokens, whose rows begin at multiples of 16 bytes (below
  * 2^28 bytes apart in a page), run on the matrix cores; every other size, page and stride takes a kernel that is several times slower.
- * Arithmetic as in zo_cache_attend, except that weights of bf16 heads of 64 and 128 are rounded to bf16 once where sequences have more than 32
- * rows on average (a new token and a query head of one key head's): out is then within 2^-8 of the weighted magnitudes before its own
- * rounding. A value that is infinite or NaN reaches the outputs of the tokens that see it and of no other.
+ * Arithmetic as in zo_cache_attend. A value that is infinite or NaN reaches the outputs of the tokens that see it and of no other.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (dtype, alignment, dim = 0 or above ZO_DIM_MAX, heads, pages or page_tokens 0, heads above 65,535, an out
  * that shares an element with q or lies in the memory that the keys or the values span, too little work, words above 2^20, tokens
  * times q_heads 2^24 or more, sequences times heads 2^23 or more, 2^31 tokens or more in a row of the table); ZO_ERR_NONFINITE

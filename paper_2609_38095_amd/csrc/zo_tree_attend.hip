@@ -19,21 +19,19 @@
 //   - S^T leaves in lane (r, g) the keys 8 i + 4 g .. + 3: the second product's operand as it is, if the contraction's index
 //     is permuted alike; the values' operand is read by the transposing LDS read (bf16), four keys of 16 dims at a time.
 //   - bf16 heads of 64 and 128 in more than one row wave run as a pipeline of 32 keys (step()): the products of one block's scores and of
-//     another's weights with the values lie under the exponentials of the one between, one barrier a tile (1,847 -> 1,263 us).
+//     another's weights with the values lie under the exponentials of the one between, one barrier a tile (prompts 1,847 -> 1,342 us).
 //
 // What a row does not see. Scores are masked, and values that no row of the call may use are zeros in LDS. A value that is infinite or
 // NaN in a tile that only some of the rows see would reach the others as 0 times itself: it is a zero in LDS too, and is
 // added to the results of the rows that see it after these are written.
 //
-// Rounding. fp32 sums and bounds. The pipeline rounds bf16 weights once, an error of up to 2^-8 of the weighted magnitudes before the output's
-// own rounding; weights of two parts bound that form by the matrix cores (1,847 us). Outputs and log-sums go by the sum of the weights before
-// they are rounded; a second sum, of the rounded ones, would give a row that sees one key that key's value, and costs 3 % (prompts
-// 1,051 -> 1,078 us, 48 trees 173 -> 178). The other bf16 forms take weights as a sum of two bf16.
+// Rounding. fp32 sums and bounds. bf16 weights are a sum of two bf16 (2^-16 of a weight is lost), two products with the values each: weights
+// rounded once would be 2^-8 of the weighted magnitudes, as much as the output's own rounding, for 1,060 instead of 1,342 us (prompts).
 //
-// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,051 to 1,094 us (0.8 of the rate of a large
-// matrix product; units 0.45 busy each); 48 trees of up to 64 behind up to 4,096, 171 to 177 us (3.4 TB/s: 1.8 to 2.6 us a tile, 11 an
-// item, 16 the join); one tree of 12 behind 1,037, 16 us (latencies: the deal 2 us, first loads 3, results 3, the join 4). fp32 trees, 16 of up to
-// 23, 32 heads of 64 behind up to 2,050: 85 us (4.4 TB/s).
+// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,342 us (1.16 PFLOP/s with the second
+// parts' products, what a large matrix product reaches); 48 trees of up to 64 behind up to 4,096, 205 us (2.9 TB/s); one tree of 12 behind
+// 1,037, 16.5 us (latencies: the deal 2 us, first loads 3, results 3, the join 4). fp32 trees, 16 of up to 23, 32 heads of 64 behind up to
+// 2,050: 85 us (4.4 TB/s).
 
 #include <algorithm>
 #include <cmath>
@@ -269,6 +267,14 @@ __device__ __forceinline__ u32x4 without_odd(u32x4 v) {
     }
   }
   return v;
+}
+
+// A weight as a sum of two bf16, 16 bits of it, so that only the output is rounded to 8. Both parts are positive: the largest bf16 below
+// the weight and what is left of it. A signed or empty rest would make a NaN of an infinite value. below(p) holds the first part's bits.
+__device__ __forceinline__ uint32_t below(float p) { return __builtin_elementwise_sub_sat(__float_as_uint(p), 1u); }
+__device__ __forceinline__ uint32_t first_parts(uint32_t b0, uint32_t b1) { return __builtin_amdgcn_perm(b1, b0, 0x07060302u); }
+__device__ __forceinline__ uint32_t rests_of(float p0, float p1, uint32_t b0, uint32_t b1) {
+  return pack_bf16x2(p0 - __uint_as_float(b0 & 0xFFFF0000u), p1 - __uint_as_float(b1 & 0xFFFF0000u));
 }
 
 // The kernel's arguments read anew: a copy of its own for each part of the kernel, so that those of one part do not hold (and spill) the
@@ -595,9 +601,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       __syncthreads();
 
       f32x16 x;                  // this block's scores
-      uint32_t weights[8] = {};  // the block before's, bf16 in pairs
-      // Operands are read four products (of each kind) ahead, into the registers that a product has left.
-      constexpr uint32_t kAhead = 4 < kSteps ? 4 : kSteps;
+      uint32_t weights[8] = {}, rests[8] = {};  // the block before's in two parts, bf16 in pairs
+      // Operands are read ahead of their products, into the registers that a product has left: keys two products ahead (four spill 22
+      // more registers: 48 trees 215 us instead of 205, prompts 1,380 instead of 1,342, one answer's tree 19 instead of 16.5).
+      constexpr uint32_t kAhead = 2;
       u32x4 kf[kAhead], vf[kOuts];
       // Where the lane's operands are, in the buffer in turn; blocks and sixteens are constant offsets behind it.
       uint32_t key_from[kSteps], value_from[kOuts];
@@ -627,9 +634,9 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
       const auto score = [&](f32x16& y, uint32_t n) {
         y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[n % kAhead]), __builtin_bit_cast(bf16x8, q[n]), y, 0, 0, 0);
       };
-      const auto weigh = [&](uint32_t n) {
+      const auto weigh = [&](uint32_t n, const uint32_t (&part)[8]) {
         const uint32_t e = n % kOuts, c = n / kOuts;
-        const u32x4 w = {weights[4 * c], weights[4 * c + 1], weights[4 * c + 2], weights[4 * c + 3]};
+        const u32x4 w = {part[4 * c], part[4 * c + 1], part[4 * c + 2], part[4 * c + 3]};
         o[e] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[e]), __builtin_bit_cast(bf16x8, w), o[e], 0, 0, 0);
       };
       // The bound of the scores: above them by 8, a whole number, so that rescaling is exact also for the weights that wait.
@@ -647,18 +654,20 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
           for (uint32_t e = 0; e < kOuts; ++e) o[e] *= by;
 #pragma unroll
-          for (int i = 0; i < 8; ++i)
+          for (int i = 0; i < 8; ++i) {
             weights[i] = pack_bf16x2(__uint_as_float(weights[i] << 16) * by, __uint_as_float(weights[i] & 0xFFFF0000u) * by);
+            rests[i] = pack_bf16x2(__uint_as_float(rests[i] << 16) * by, __uint_as_float(rests[i] & 0xFFFF0000u) * by);
+          }
           m = top;
         }
       };
       // One step: the scores of block kb of a tile, the products of the waiting weights with the values of block vb of a tile (kValues),
-      // this block's weights. The first operands are there; the next step's first ones (of blocks kb + 1 and vb + 1) are read at its end
+      // this block's weights. A third of two weights' arithmetic lies behind each product (in the compiler's own order 3 % more). The first operands are there; the next step's first ones (of blocks kb + 1 and vb + 1) are read at its end
       // (kNext).
       const auto step = [&](auto scores, auto values, auto next, uint32_t kb, uint32_t vb) {
         constexpr bool kScores = scores.value, kValues = values.value, kNext = next.value;
         f32x16 y = {};
-        uint32_t now[8];
+        uint32_t now[8], rest[8];
         const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
         for (uint32_t n = 0; n < 8; ++n) {
@@ -669,21 +678,30 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
             else if (kNext)
               kf[n % kAhead] = read_key(kb + 1, n + kAhead - kSteps);
           }
-          if (kValues && n < 2 * kOuts) {
-            weigh(n);
+          const bool weighs = kValues && n < 2 * kOuts;
+          float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], scale, -ref));
+          float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], scale, -ref));
+          asm volatile("" : "+v"(p0), "+v"(p1));  // here, under the products, and not where they are used
+          __builtin_amdgcn_sched_barrier(0);
+          if (weighs) weigh(n, weights);
+          l += p0 + p1;
+          uint32_t b0 = below(p0), b1 = below(p1);
+          now[n] = first_parts(b0, b1);
+          asm volatile("" : "+v"(b0), "+v"(b1), "+v"(l), "+v"(now[n]));
+          __builtin_amdgcn_sched_barrier(0);
+          if (weighs) {
+            weigh(n, rests);
             if (n < kOuts)
               vf[n] = read_value(vb, n + kOuts);
             else if (kNext)
               vf[n - kOuts] = read_value(vb + 1, n - kOuts);
           }
-          const float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], scale, -ref));
-          const float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], scale, -ref));
-          l += p0 + p1;
-          now[n] = pack_bf16x2(p0, p1);  // one rounding
-          asm volatile("" : "+v"(now[n]), "+v"(l));  // here, under the products, and not where they are used
+          rest[n] = rests_of(p0, p1, b0, b1);
+          asm volatile("" : "+v"(rest[n]));
+          __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
-        for (int n = 0; n < 8; ++n) weights[n] = now[n];
+        for (int n = 0; n < 8; ++n) weights[n] = now[n], rests[n] = rest[n];
         if constexpr (kScores) x = y;
       };
       const std::true_type yes{};
@@ -741,7 +759,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         step(no, yes, yes, 0, 0);
 #pragma unroll
         for (uint32_t n = 0; n < 2 * kOuts; ++n) {
-          weigh(n);
+          weigh(n, weights);
+          weigh(n, rests);
           if (n < kOuts) vf[n] = read_value(1, n + kOuts);
         }
       }
@@ -873,15 +892,12 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
                   o[e] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, p[i], o[e], 0, 0, 0);
                 }
             } else {
-              // weights as a sum of two bf16, 16 bits of each, so that only the output is rounded to 8. Both are positive: the largest
-              // bf16 below the weight and what is left of it. A signed or empty rest would make a NaN of an infinite value.
               u32x4 hi[2], lo[2];
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                const float p0 = p[2 * i], p1 = p[2 * i + 1];
-                const uint32_t b0 = __builtin_elementwise_sub_sat(__float_as_uint(p0), 1u), b1 = __builtin_elementwise_sub_sat(__float_as_uint(p1), 1u);
-                hi[i / 4][i % 4] = __builtin_amdgcn_perm(b1, b0, 0x07060302u);
-                lo[i / 4][i % 4] = pack_bf16x2(p0 - __uint_as_float(b0 & 0xFFFF0000u), p1 - __uint_as_float(b1 & 0xFFFF0000u));
+                const uint32_t b0 = below(p[2 * i]), b1 = below(p[2 * i + 1]);
+                hi[i / 4][i % 4] = first_parts(b0, b1);
+                lo[i / 4][i % 4] = rests_of(p[2 * i], p[2 * i + 1], b0, b1);
               }
               if (b == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
