@@ -113,7 +113,7 @@ int zo_tree_accept(const zo_tree_walk* w, void* stream);
 
 /*
  * zo_tree_keep -- brings a walked path together: in each of n_tensors tensors (as in zo_cache_copy: the keys and the values of each
- * layer, all of the shape and strides of `shape`; a host array) every head's row at token lengths[s] + path[s][i] of sequence
+ * layer, all of the shape and strides of `shape`; a host array; one that is listed several times moves once) every head's row at token lengths[s] + path[s][i] of sequence
  * s goes to token lengths[s] + i. path (int32, rows path_stride apart) rises along a row and ends with its first negative
  * entry, or the first that does not rise. Rows of an absent page, or behind the table, are neither read nor written. Sequences do not
  * share pages that rows are moved in (ZoPages: extend() gives them pages of their own).

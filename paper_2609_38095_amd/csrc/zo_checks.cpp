@@ -130,9 +130,9 @@ bool sides_overlap(const zo_cache& c, size_t elem) {
   return same_strides_meet(axes, 3, address(c.v) - address(c.k), c.dim * size);
 }
 
-// Whether two tensors of a list, all of the (nested) shape of `c`, share elements. The same tensor twice does not count: its moves
-// are the same. Sorted by address; layers one behind another, or side by side inside a page's stride, need no pairs.
-bool tensors_overlap(const zo_cache& c, void* const* tensors, uint32_t n, size_t elem) {
+// Whether two tensors of a list, all of the (nested) shape of `c`, share elements. The same tensor twice does not count: `at` has each
+// once. Sorted by address; layers one behind another, or side by side inside a page's stride, need no pairs.
+bool tensors_overlap(const zo_cache& c, void* const* tensors, uint32_t n, size_t elem, std::vector<int64_t>& at) {
   const int64_t size = static_cast<int64_t>(elem), run = c.dim * size;
   Places all;
   const auto stride = [&](int64_t s, uint32_t count) { return count > 1 ? s * size : 0; };
@@ -141,7 +141,7 @@ bool tensors_overlap(const zo_cache& c, void* const* tensors, uint32_t n, size_t
                         {stride(c.token_stride, c.page_tokens), c.page_tokens, c.page_tokens}};
   for (const Both& a : axes) all.add(a.stride, a.n);
   all.close(run);
-  std::vector<int64_t> at(n);
+  at.resize(n);
   for (uint32_t i = 0; i < n; ++i) at[i] = address(tensors[i]);
   std::sort(at.begin(), at.end());
   at.erase(std::unique(at.begin(), at.end()), at.end());
@@ -390,7 +390,8 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
     if (!aligned(tensors[i], elem)) return ZO_ERR_ARG;
   }
   try {
-    if (tensors_overlap(first, tensors, n_tensors, elem)) return ZO_ERR_ARG;
+    std::vector<int64_t> each;  // the same copies twice write the same
+    if (tensors_overlap(first, tensors, n_tensors, elem, each)) return ZO_ERR_ARG;
     for (uint32_t i = 0; i < n_moves; ++i) {
       const zo_page_move& m = moves[i];
       if (m.src < 0 || m.dst < 0 || static_cast<uint32_t>(m.src) >= first.pages || static_cast<uint32_t>(m.dst) >= first.pages)
@@ -428,6 +429,11 @@ int check_walk(const zo_tree_walk& w) {
 }
 
 int check_moves(const zo_tree_moves& m) {
+  std::vector<int64_t> tensors;
+  return check_moves_of(m, tensors);
+}
+
+int check_moves_of(const zo_tree_moves& m, std::vector<int64_t>& tensors) {
   if (!dtype_ok(m.dtype) || m.table.seqs >= (1u << 17) || m.most > 0x7FFFFFFFu) return ZO_ERR_ARG;  // 2^32 threads at most in a launch
   if (m.n_tensors == 0 || m.table.seqs == 0 || m.most == 0) return ZO_OK;
   if (m.tensors == nullptr || m.lengths == nullptr || m.path == nullptr) return ZO_ERR_NULL;
@@ -443,7 +449,7 @@ int check_moves(const zo_tree_moves& m) {
     if (!aligned(m.tensors[i], elem)) return ZO_ERR_ARG;
   }
   try {
-    return tensors_overlap(first, m.tensors, m.n_tensors, elem) ? ZO_ERR_ARG : ZO_OK;
+    return tensors_overlap(first, m.tensors, m.n_tensors, elem, tensors) ? ZO_ERR_ARG : ZO_OK;
   } catch (const std::bad_alloc&) {
     return ZO_ERR_MEMORY;
   }

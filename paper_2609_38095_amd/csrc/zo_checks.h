@@ -5,6 +5,7 @@
 
 #include <cstddef>
 #include <cstdint>
+#include <vector>
 
 #include "zo_decode.h"
 #include "zo_tree.h"
@@ -23,6 +24,8 @@ int check_copy(const zo_cache* shape, void* const* tensors, uint32_t n_tensors, 
 int check_tree(const zo_tree& t);
 int check_walk(const zo_tree_walk& w);
 int check_moves(const zo_tree_moves& m);
+// The same, and the tensors' addresses, each once: where one moved row is the next one's source, moving a tensor twice moves it further.
+int check_moves_of(const zo_tree_moves& m, std::vector<int64_t>& tensors);
 int check_tree_attend(const zo_tree_attention& a);
 
 // Whether two sets of rows may share an element. Exact for rows of one interleaved buffer: equal strides, each as large as

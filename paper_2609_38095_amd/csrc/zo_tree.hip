@@ -3,6 +3,7 @@
 // moves of a batch by HBM.
 
 #include <algorithm>
+#include <vector>
 
 #include "zo_checks.h"
 #include "zo_lanes.h"
@@ -307,7 +308,8 @@ int zo_tree_accept(const zo_tree_walk* w, void* stream) {
 int zo_tree_keep(const zo_tree_moves* m, void* stream) {
   using namespace zo;
   if (m == nullptr) return ZO_ERR_NULL;
-  const int rc = check_moves(*m);
+  std::vector<int64_t> tensors;  // each once
+  const int rc = check_moves_of(*m, tensors);
   if (rc != ZO_OK) return rc;
   if (m->n_tensors == 0 || m->table.seqs == 0 || m->most == 0) return ZO_OK;
   const int64_t elem = static_cast<int64_t>(elem_bytes(m->dtype));
@@ -330,9 +332,10 @@ int zo_tree_keep(const zo_tree_moves* m, void* stream) {
   k.vecs = k.row_vecs * f.heads;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();
-  for (uint32_t t0 = 0; t0 < m->n_tensors; t0 += kTensors) {
-    k.n_tensors = std::min(kTensors, m->n_tensors - t0);
-    for (uint32_t i = 0; i < k.n_tensors; ++i) k.tensor[i] = static_cast<char*>(m->tensors[t0 + i]);
+  const uint32_t n_tensors = static_cast<uint32_t>(tensors.size());
+  for (uint32_t t0 = 0; t0 < n_tensors; t0 += kTensors) {
+    k.n_tensors = std::min(kTensors, n_tensors - t0);
+    for (uint32_t i = 0; i < k.n_tensors; ++i) k.tensor[i] = reinterpret_cast<char*>(tensors[t0 + i]);
     k.tensors_each = tensors_each(m->table.seqs, k.n_tensors, k.vecs);
     const dim3 grid(m->table.seqs, (k.n_tensors - 1) / k.tensors_each + 1), block(kKeepThreads);
     if (vectors)

@@ -50,7 +50,8 @@ def zo_tree_accept(drafted, drawn, starts, most, parents=None, stream=None):
 
 
 def zo_tree_keep(k_caches, v_caches, table, lengths, path, stream=None):
-    """In each layer's cache: the keys and values of sequence s at token lengths[s] + path[s][i] go to token lengths[s] + i."""
+    """In each layer's cache: the keys and values of sequence s at token lengths[s] + path[s][i] go to token lengths[s] + i. Layers
+    that share a cache may list it each; it moves once."""
     k_caches = list(k_caches)
     decode._call((decode._TENSORS or decode._tensors()).tree_keep, stream, k_caches[0] if k_caches else None, k_caches, list(v_caches),
                  table, lengths, path)
