@@ -50,7 +50,8 @@ int zo_tree_lay(const zo_tree* t, void* stream);
 
 /*
  * zo_norm_rotate_put_at -- zo_norm_rotate_put whose rows go to token places[token] of their sequence and are turned by
- * positions[token]: tokens of different branches of a tree share positions and not places. A negative place is not put.
+ * positions[token]: tokens of different branches of a tree share positions and not places. A token whose position or
+ * place is negative is not put.
  * places: [tokens]; NULL: the positions. Errors: as zo_norm_rotate_put.
  */
 int zo_norm_rotate_put_at(const zo_rotate_put* p, const int32_t* places, void* stream);

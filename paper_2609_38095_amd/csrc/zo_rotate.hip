@@ -174,7 +174,7 @@ __device__ __forceinline__ void turn_share(const Sh& sh, int n, float (&a)[kVec]
 __device__ __forceinline__ int64_t place_of(const Rotation& r, const Side& sd, uint32_t token, int32_t pos) {
   if (!sd.put) return static_cast<int64_t>(token) * sd.y_token;
   const uint32_t seq = r.seqs ? static_cast<uint32_t>(r.seqs[token]) : token;
-  if (r.places) pos = r.places[token];
+  if (r.places && pos >= 0) pos = r.places[token];  // padding has no place
   if (pos < 0 || seq >= r.table_seqs) return -1;
   const uint32_t slot = static_cast<uint32_t>(pos) / r.page_tokens;
   if (slot >= r.table_width) return -1;

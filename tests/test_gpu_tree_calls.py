@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_38095_amd as zo
 from oracle import tree as oracle
-from test_gpu_tree import cache_of, dev, ints, wide
+from test_gpu_tree import cache_of, dev, ints, normal, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -24,3 +24,26 @@ def test_keep_of_shared_caches(layers):
         k, v = tensors
         zo.zo_tree_keep([k] * layers, [k if v is None else v] * layers, dev(table), ints(lengths), dev(path))
         assert np.array_equal(wide(k), wants[0]) and (v is None or np.array_equal(wide(v), wants[1]))
+
+
+# ---- put
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(128, 16), (20, 5)])
+def test_a_token_without_a_position_is_not_put(dim, page, dtype):
+    """Padding: a negative position, a negative place, or both; what is cached at the place stays."""
+    n, hq, hk, width = 9, 4, 2, 3
+    table = dev(np.arange(3 * width, dtype=np.int32).reshape(3, width))
+    x = normal(1, (n, hq + 2 * hk, dim), dtype)
+    q, k, v = x[:, :hq], x[:, hq:hq + hk], x[:, hq + hk:]
+    kc, vc = cache_of("heads", 5, 3 * width, hk, page, dim, dtype)
+    first = kc.clone(), vc.clone()
+    seqs, places, positions = [0, 0, 0, 1, 1, 1, 2, 2, 2], [0, 1, -1, 3, 4, 5, -1, 7, 8], [0, -1, 2, 3, -2 ** 31, 4, -1, 7, -1]
+    turns = zo.zo_rotary_turns(dim)
+    zo.zo_norm_rotate_put(q, k, v, kc, vc, table, ints(positions), turns, seqs=ints(seqs), places=ints(places))
+    ko = zo.zo_norm_rotate(None, k, ints(positions), turns)[1]
+    for t in range(n):
+        if places[t] >= 0 and positions[t] >= 0:
+            at = int(table[seqs[t], places[t] // page]), slice(None), places[t] % page
+            first[0][at], first[1][at] = ko[t], v[t]
+    assert torch.equal(kc, first[0]) and torch.equal(vc, first[1])
