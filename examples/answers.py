@@ -194,11 +194,12 @@ def answer_drafted(model, prompts, answers, u, drafts, ahead=4, temperature=1.0,
         table = _on(dev, book.table([held[i] for i in live])[0])
         drafted, parents = (_on(dev, np.concatenate([np.array(t[k], np.int32) for t in trees])) for k in (0, 1))
         starts, dev_lengths = _on(dev, _starts(counts)), _on(dev, lengths)
-        logits = model.tree_logits(drafted, table, starts, dev_lengths, parents, words=-(-max(counts) // 64))
+        words = -(-max(counts) // 64)
+        logits = model.tree_logits(drafted, table, starts, dev_lengths, parents, words)
         # the token behind each is drawn with the random number of its place in its answer
         at = np.concatenate([len(tokens[i]) + np.array(t[2]) for i, t in zip(live, trees)])
         drawn, lp = zo.zo_draw(logits, u[_on(dev, at), _on(dev, np.repeat(live, counts))], **_settings(len(at), dev, temperature, top_k, top_p))
-        path, won, walked = zo.zo_tree_accept(drafted, drawn, starts, ahead + 1, parents)
+        path, won, walked = zo.zo_tree_accept(drafted, drawn, starts, ahead + 1, parents, words=words)
         zo.zo_tree_keep(*model.caches(), table, dev_lengths, path)
         rows = torch.gather(lp[(starts[:-1, None] + path.clamp(min=0)).long()], 1, torch.arange(ahead + 1, device=dev)[None].expand_as(path))
         won, walked, rows = won.tolist(), walked.tolist(), rows.tolist()

@@ -33,7 +33,7 @@ extern "C" {
  *   seq_of[t] = s, places[t] = lengths[s] + i, positions[t] = lengths[s] + the tokens before it on its branch,
  *   seen[t][w], bit b: whether it sees new token 64 w + b (itself and those before it on its branch).
  * Rows of no sequence get seq_of = positions = places = -1 and see nothing; so do, with their seq_of, new tokens from index
- * 64 words on of a tree, which the masks have no room for. Sums saturate at 2^31 - 1. parents NULL (a chain): words may be 0 and
+ * 64 words on of a tree, which the masks have no room for (zo_tree_accept takes `words` to know of them). Sums saturate at 2^31 - 1. parents NULL (a chain): words may be 0 and
  * seen NULL; positions are the places, and chains may be of any length (with words > 0: masks as for a tree, with its limit).
  * seen: [tokens, words], contiguous. The outputs do not overlap each other or the inputs.
  * Errors: ZO_ERR_NULL; ZO_ERR_ARG (alignment, words above ZO_TREE_WORDS, 0 words with parents, 2^24 tokens or sequences or more);
@@ -99,15 +99,18 @@ int zo_tree_attend(const zo_tree_attention* a, void* stream);
  * token drawn behind it. Sequence s walks from its new token 0 (a token that is certain): from the one it is at to the
  * first new token that comes behind it and whose drafted token is the one drawn there; until there is none, or `most` tokens are walked.
  * A negative token (zo_draw's for logits without any weight, or a place of a tree that is not used) agrees with none.
+ * words: those given to zo_tree_lay, which gave new tokens from index 64 words on no place: the walk does not come to them. 0: no limit (chains
+ * without masks).
  * path[s][i] is the index (within the sequence) of the walk's i-th token, tokens_out[s][i] the token drawn behind it, both
  * -1 behind the walk's end; counts[s] the tokens walked (0 for a sequence without new ones): as many are won, and the last is the
  * next step's token 0. path and tokens_out: [seqs, most], contiguous. The outputs do not overlap each other or the inputs.
- * Errors: ZO_ERR_NULL; ZO_ERR_ARG (alignment, most = 0, 2^24 tokens, sequences or entries of path or more); ZO_ERR_HIP.
+ * Errors: ZO_ERR_NULL; ZO_ERR_ARG (alignment, most = 0, words above ZO_TREE_WORDS, 2^24 tokens, sequences or entries of path or more);
+ * ZO_ERR_HIP.
  */
 typedef struct {
   const int32_t *drafted, *drawn, *starts, *parents;
   int32_t *path, *tokens_out, *counts;
-  uint32_t tokens, seqs, most;
+  uint32_t tokens, seqs, most, words;
 } zo_tree_walk;
 
 int zo_tree_accept(const zo_tree_walk* w, void* stream);

@@ -80,11 +80,12 @@ def attend(q, k_cache, v_cache, table, lengths, starts, seen, scale):
     return out, lse, mag, big
 
 
-def accept(drafted, drawn, starts, most, parents=None):
-    """(path, tokens, counts) of the walk along the drafted tokens that the draws agree with."""
+def accept(drafted, drawn, starts, most, parents=None, words=0):
+    """(path, tokens, counts) of the walk along the drafted tokens that the draws agree with, among the first 64 words of a tree."""
     at = spans(starts, len(drafted))
     path, won, counts = np.full((len(at), most), -1, np.int32), np.full((len(at), most), -1, np.int32), np.zeros(len(at), np.int32)
     for s, (first, count) in enumerate(at):
+        count = min(count, 64 * words) if words else count
         i = 0 if count else None
         while i is not None and counts[s] < most:
             path[s, counts[s]], won[s, counts[s]] = i, drawn[first + i]

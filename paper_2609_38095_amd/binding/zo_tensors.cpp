@@ -554,10 +554,11 @@ PyObject* tree_attend(PyObject* const* args, Py_ssize_t n) {
 }
 
 PyObject* tree_accept(PyObject* const* args, Py_ssize_t n) {
-  Args a(args, n, 7);
+  Args a(args, n, 8);
   const at::Tensor *drafted = a.tensor("drafted"), *drawn = a.tensor("drawn"), *starts = a.tensor("starts");
   const long long most = a.integer();
   const at::Tensor* parents = a.tensor("parents");
+  const long long words = a.integer();
   if (drafted == nullptr || drawn == nullptr) refuse(PyExc_TypeError, "drafted and drawn must be CUDA (HIP) torch tensors");
   if (drafted->dim() != 1) refuse(PyExc_ValueError, "drafted must be [tokens]");
   const int64_t tokens = drafted->size(0);
@@ -568,7 +569,9 @@ PyObject* tree_accept(PyObject* const* args, Py_ssize_t n) {
   w.parents = vector_of<const int32_t>(parents, "parents", at::kInt, tokens);
   w.tokens = count_of(tokens, "drafted");
   if (most < 1 || most >= (1 << 24) || static_cast<uint64_t>(most) * w.seqs >= (1u << 24)) return status(ZO_ERR_ARG);
+  if (words < 0 || words > static_cast<long long>(ZO_TREE_WORDS)) return status(ZO_ERR_ARG);
   w.most = static_cast<uint32_t>(most);
+  w.words = static_cast<uint32_t>(words);
   const at::Tensor path = fresh(*drafted, {w.seqs, most}, at::kInt), won = fresh(*drafted, {w.seqs, most}, at::kInt);
   const at::Tensor counts = fresh(*drafted, {w.seqs}, at::kInt);
   w.path = static_cast<int32_t*>(path.data_ptr());

@@ -417,7 +417,7 @@ int check_tree(const zo_tree& t) {
 }
 
 int check_walk(const zo_tree_walk& w) {
-  if (w.tokens >= (1u << 24) || w.seqs >= (1u << 24) || w.most == 0) return ZO_ERR_ARG;
+  if (w.tokens >= (1u << 24) || w.seqs >= (1u << 24) || w.most == 0 || w.words > ZO_TREE_WORDS) return ZO_ERR_ARG;
   if (static_cast<uint64_t>(w.seqs) * w.most >= (1u << 24)) return ZO_ERR_ARG;
   if (w.seqs == 0) return ZO_OK;
   if (w.starts == nullptr || w.path == nullptr || w.tokens_out == nullptr || w.counts == nullptr) return ZO_ERR_NULL;

@@ -118,7 +118,8 @@ constexpr uint32_t kNone = 0xFFFFFFFFu;
 __global__ void __launch_bounds__(kWalkThreads) accept_kernel(const zo_tree_walk w) {
   __shared__ uint32_t next[kWindow], path[kWindow], first, found, at_shared;
   const uint32_t seq = blockIdx.x;
-  const Span sp = span_of(w.starts, seq, w.tokens);
+  Span sp = span_of(w.starts, seq, w.tokens);
+  if (w.words > 0) sp.count = min(sp.count, kWave * w.words);  // the tokens that the masks have room for
   int32_t* path_out = w.path + static_cast<size_t>(seq) * w.most;
   int32_t* tokens_out = w.tokens_out + static_cast<size_t>(seq) * w.most;
   uint32_t at = 0, walked = 0;  // the token that the walk has come to; tokens before those found in this window

@@ -7,7 +7,7 @@ Argument marshalling only, as in decode.py, under the C names:
   zo_norm_rotate_put(..., seqs=, places=)               (decode.py) queries rotated, keys and values put at the places
   zo_tree_attend(q, k_cache, v_cache, table, lengths, starts, seen)
                                                         the new tokens over the cache and over each other
-  zo_tree_accept(drafted, drawn, starts, most, parents) the walk along the drafted tokens that the draws agree with
+  zo_tree_accept(drafted, drawn, starts, most, parents, words=) the walk along the drafted tokens that the draws agree with
   zo_tree_keep(k_caches, v_caches, table, lengths, path) its keys and values brought together, every layer
   ZoPages.cut(seq, tokens)                              (decode.py) the rest of the draft's pages goes back
 
@@ -42,11 +42,12 @@ def zo_tree_attend(q, k_cache, v_cache, table, lengths, starts, seen=None, scale
                         scale, out, lse, work)
 
 
-def zo_tree_accept(drafted, drawn, starts, most, parents=None, stream=None):
+def zo_tree_accept(drafted, drawn, starts, most, parents=None, stream=None, words=0):
     """(path, tokens, counts): int32 [sequences, most] indices of the walked tokens and the tokens drawn behind them, -1 behind
     the walk's end, and int32 [sequences] how many they are. drafted, drawn: int32 [tokens], the drafted tokens and those drawn
-    behind each of them."""
-    return decode._call((decode._TENSORS or decode._tensors()).tree_accept, stream, drafted, drafted, drawn, starts, most, parents)
+    behind each of them. words: the masks' of zo_tree_lay, whose trees end with them (0: no limit); new tokens behind have no place
+    in the cache and are not walked."""
+    return decode._call((decode._TENSORS or decode._tensors()).tree_accept, stream, drafted, drafted, drawn, starts, most, parents, words)
 
 
 def zo_tree_keep(k_caches, v_caches, table, lengths, path, stream=None):

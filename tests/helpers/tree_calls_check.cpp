@@ -42,9 +42,23 @@ void tensors_listed_twice() {
   CHECK(zo::check_moves_of(m, each) == ZO_ERR_ARG && zo::check_moves(m) == ZO_ERR_ARG);
 }
 
+void words_of_a_walk() {
+  zo_tree_walk w = {};
+  w.drafted = w.drawn = w.starts = at<const int32_t>(0x1000);
+  w.path = w.tokens_out = w.counts = at<int32_t>(0x2000);
+  w.tokens = 600;
+  w.seqs = 2;
+  w.most = 4;
+  w.words = ZO_TREE_WORDS;
+  CHECK(zo::check_walk(w) == ZO_OK);
+  w.words = ZO_TREE_WORDS + 1;
+  CHECK(zo::check_walk(w) == ZO_ERR_ARG);
+}
+
 }  // namespace
 
 int main() {
+  words_of_a_walk();
   tensors_listed_twice();
   std::printf("tree_calls_check ok\n");
 }

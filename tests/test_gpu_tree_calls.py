@@ -47,3 +47,28 @@ def test_a_token_without_a_position_is_not_put(dim, page, dtype):
             at = int(table[seqs[t], places[t] // page]), slice(None), places[t] % page
             first[0][at], first[1][at] = ko[t], v[t]
     assert torch.equal(kc, first[0]) and torch.equal(vc, first[1])
+
+
+# ---- walk
+
+@pytest.mark.parametrize("kind", ["tree", "chain"])
+@pytest.mark.parametrize("counts,words", [([100], 1), ([63, 64, 65, 200], 1), ([130, 1, 0, 700], 2), ([600, 512, 513], 8)])
+def test_the_walk_ends_where_the_masks_do(counts, words, kind):
+    """Every draw agrees: a walk goes on to the last token that zo_tree_lay gave a place, and what it moves was put."""
+    n, starts = sum(counts), np.concatenate(([0], np.cumsum(counts))).astype(np.int32)
+    parents = np.concatenate([np.arange(c) - 1 for c in counts]).astype(np.int32) if kind == "tree" else None
+    drafted = np.arange(n, dtype=np.int32)
+    args = dev(drafted), dev(drafted + 1), dev(starts)
+    own = None if parents is None else dev(parents)
+    lengths = ints([9] * len(counts))
+    places = zo.zo_tree_lay(args[2], lengths, n, own, words)[2].cpu().numpy()
+    path, tokens, walked = zo.zo_tree_accept(*args, 800, own, words=words)
+    for g, w in zip((path, tokens, walked), oracle.accept(drafted, drafted + 1, starts, 800, parents, words)):
+        assert np.array_equal(g.cpu().numpy(), w)
+    assert walked.tolist() == [min(c, 64 * words) for c in counts]
+    for s, c in enumerate(walked.tolist()):
+        assert (places[starts[s] + path[s, :c].cpu().numpy()] >= 0).all()
+    assert zo.zo_tree_accept(*args, 800, own)[2].tolist() == counts  # without words: chains of any length
+    for wrong in (-1, 9):
+        with pytest.raises(zo.ZoError):
+            zo.zo_tree_accept(*args, 800, own, words=wrong)
