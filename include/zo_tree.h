@@ -67,7 +67,7 @@ int zo_norm_rotate_put_at(const zo_rotate_put* p, const int32_t* places, void* s
  * q and out: [tokens] rows of q_heads heads; lse: float [tokens * q_heads], contiguous, or NULL. q_heads is a multiple of
  * cache.heads. seen: [tokens] rows of `words` words, seen_stride words apart, or NULL (a chain).
  * The work is split evenly over the chip whatever the lengths are, as in zo_cache_attend, and parts are joined by a
- * second launch. work: device memory of zo_tree_attend_work() bytes, aligned to 16, contents irrelevant, one
+ * second launch; lengths and starts, which every workgroup reads, do not change before the call is done. work: device memory of zo_tree_attend_work() bytes, aligned to 16, contents irrelevant, one
  * for each call in flight. Heads of 64, 128 and 256 in pages of whole sixteens of tokens, whose rows begin at multiples of 16 bytes (below
  * 2^28 bytes apart in a page), run on the matrix cores; every other size, page and stride takes a kernel that is several times slower.
  * Arithmetic as in zo_cache_attend. A value that is infinite or NaN reaches the outputs of the tokens that see it and of no other.

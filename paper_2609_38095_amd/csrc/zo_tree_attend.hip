@@ -39,6 +39,7 @@
 
 #include "zo_checks.h"
 #include "zo_lanes.h"
+#include "zo_tree_deal.h"
 
 namespace zo {
 namespace {
@@ -62,18 +63,17 @@ struct Split {
 };
 static_assert(sizeof(Split) == kTreeSplitWords * 4, "the workspace holds entries of this size");
 
-struct Attend {
+struct Attend : Batch {
   const char *q, *k, *v;
   char* out;
   float* lse;
   uint32_t* active;  // workgroups that have tiles
   Split* splits;
   float* parts;
-  const int32_t *ids, *lengths, *starts;
-  const uint64_t* seen;
+  const int32_t* ids;
   int64_t seen_stride, q_token, q_head, out_token, out_head, page_bytes, head_bytes, token_bytes, table_stride;
-  double inv_group, inv_page;  // of a group's query heads; of a page's sixteens
-  uint32_t tokens, words, seqs, width, pages, page_tokens, heads, group, dim, workers, part_row, visit;
+  double inv_page;  // of a page's sixteens
+  uint32_t words, pages, dim, workers, part_row;
   float scale;         // times log2(e)
 };
 
@@ -83,58 +83,9 @@ __device__ __forceinline__ uint64_t uniform(uint64_t v) {
   return static_cast<uint64_t>(uniform(static_cast<uint32_t>(v >> 32))) << 32 | uniform(static_cast<uint32_t>(v));
 }
 
-// Floor of n / d for n below 2^52: exact, since quotients of neighbours are further apart than an fp64 rounding.
-__device__ __forceinline__ uint64_t quotient(uint64_t n, uint64_t d) {
-  return static_cast<uint64_t>(static_cast<double>(n) / static_cast<double>(d));
-}
-
-struct Seq {
-  uint32_t token, count;  // its new tokens
-  uint32_t cached, len;   // tokens before them, and with them: as many as the table holds
-  uint32_t blocks;        // items of each key head
-};
-
-template <uint32_t kRows>
-__device__ __forceinline__ Seq seq_of(const Attend& a, uint32_t seq) {
-  const int64_t room = static_cast<int64_t>(a.width) * a.page_tokens, most = a.tokens;
-  int64_t first = a.starts[seq], last = a.starts[seq + 1], cached = a.lengths[seq];
-  first = first < 0 ? 0 : first > most ? most : first;
-  last = last < first ? first : last > most ? most : last;
-  cached = cached < 0 ? 0 : cached > room ? room : cached;
-  Seq s;
-  s.token = static_cast<uint32_t>(first);
-  s.count = static_cast<uint32_t>(last - first);
-  s.cached = static_cast<uint32_t>(cached);
-  s.len = static_cast<uint32_t>(cached + s.count < room ? cached + s.count : room);
-  s.blocks = (s.count * a.group + kRows - 1) / kRows;
-  return s;
-}
-
-// The same in scalar registers.
+// A sequence in scalar registers.
 __device__ __forceinline__ Seq uniform(const Seq& s) {
   return {uniform(s.token), uniform(s.count), uniform(s.cached), uniform(s.len), uniform(s.blocks)};
-}
-
-// The new token of a row (rows below 2^24: the product's error stays below the half's share).
-__device__ __forceinline__ uint32_t node_of(const Attend& a, uint32_t row) {
-  return static_cast<uint32_t>((static_cast<double>(row) + 0.5) * a.inv_group);
-}
-
-// How many tokens the rows of a sequence up to (and without) `row` can see.
-__device__ __forceinline__ uint32_t visible(const Attend& a, const Seq& s, uint32_t row) {
-  if (a.seen) return s.len;
-  const uint32_t rows = s.count * a.group;
-  return min(s.len, s.cached + node_of(a, min(row, rows) - 1) + 1);
-}
-
-// Tiles of an item; at least one, which writes the rows that see nothing. Its cost is a.visit tiles more.
-template <uint32_t kRows, uint32_t kTile>
-__device__ __forceinline__ uint32_t tiles_of(const Attend& a, const Seq& s, uint32_t block) {
-  return max(1u, (visible(a, s, (block + 1) * kRows) + kTile - 1) / kTile);
-}
-template <uint32_t kRows, uint32_t kTile>
-__device__ __forceinline__ uint32_t cost_of(const Attend& a, const Seq& s, uint32_t block) {
-  return tiles_of<kRows, kTile>(a, s, block) + a.visit;
 }
 
 // The sum over a wave of a value of each lane, and the sums up to each lane.
@@ -147,14 +98,36 @@ __device__ __forceinline__ uint64_t sums_upto(uint64_t v, uint32_t lane) {
   return v;
 }
 
-// The cost of one key head of a sequence, by all lanes together.
-template <uint32_t kRows, uint32_t kTile>
-__device__ uint64_t head_cost(const Attend& a, const Seq& s, uint32_t lane) {
-  if (a.seen) return static_cast<uint64_t>(s.blocks) * cost_of<kRows, kTile>(a, s, 0);
-  uint64_t mine = 0;
-  for (uint32_t b = lane; b < s.blocks; b += kWave) mine += cost_of<kRows, kTile>(a, s, b);
-  return uniform(__shfl(sums_upto(mine, lane), 63, 64));
-}
+// The deal's sums by all lanes of a wave together.
+template <uint32_t kRows>
+struct Lanes {
+  const Batch& batch;
+  const Seq* seqs;  // in LDS, where each thread has one; else NULL
+  uint32_t lane;
+  __device__ __forceinline__ Seq seq(uint32_t n) const { return uniform(seqs ? seqs[n] : seq_of<kRows>(batch, n)); }
+  template <class F>
+  __device__ __forceinline__ uint64_t sum(uint32_t n, const F& f) const {
+    uint64_t mine = 0;
+    for (uint32_t i = lane; i < n; i += kWave) mine += f(i);
+    return uniform(__shfl(sums_upto(mine, lane), 63, 64));
+  }
+  template <class F>
+  __device__ __forceinline__ bool first_over(uint32_t n, uint64_t rest, const F& f, uint32_t& at, uint64_t& before) const {
+    before = 0;
+    for (uint32_t i = 0; i < n; i += kWave) {
+      const uint32_t mine = i + lane < n ? f(i + lane) : 0;
+      const uint64_t upto = sums_upto(mine, lane), over = __ballot(before + upto > rest);
+      if (over != 0) {
+        const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(over));
+        at = i + l;
+        before += uniform(__shfl(upto - mine, l, 64));
+        return true;
+      }
+      before += uniform(__shfl(upto, 63, 64));
+    }
+    return false;
+  }
+};
 
 // The cost before each thread's sequences, and the sequences where each thread has one. Thread t counts sequences [t each, (t + 1) each).
 struct Deal {
@@ -189,7 +162,7 @@ __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
         one.cached = __builtin_amdgcn_readlane(s.cached, from);
         one.len = __builtin_amdgcn_readlane(s.len, from);
         one.blocks = __builtin_amdgcn_readlane(s.blocks, from);
-        const uint64_t all = head_cost<kRows, kTile>(a, one, lane);
+        const uint64_t all = head_cost<kRows, kTile>(a, one, Lanes<kRows>{a, nullptr, lane});
         if (lane == from) cost += all;
       }
     }
@@ -207,23 +180,6 @@ __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
   __syncthreads();
   return d;
 }
-
-// The run of each worker: the total cost in equal parts, the first ones longer by one.
-struct Runs {
-  uint64_t each, longer;
-  uint32_t workers;
-  __device__ Runs(uint64_t total, uint32_t most) {
-    workers = total < most ? static_cast<uint32_t>(total) : most;
-    if (workers == 0) workers = 1;
-    each = uniform(quotient(total, workers));
-    longer = total - each * workers;
-  }
-  __device__ uint64_t first(uint32_t w) const { return w * each + (w < longer ? w : longer); }
-  __device__ uint32_t worker_of(uint64_t place) const {
-    const uint64_t head = longer * (each + 1);  // of the longer runs
-    return static_cast<uint32_t>(place < head ? quotient(place, each + 1) : longer + quotient(place - head, each));
-  }
-};
 
 // A part in the workspace: for each row [m, l, -, -, o[dim]].
 template <uint32_t kRows>
@@ -347,7 +303,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     d = deal<kRows, kTile, F::kThreads>(a, before, seqs);
     workers = a.workers;
   }
-  const Runs runs(d.total, workers);
+  Runs runs(d.total, workers);
+  runs.each = uniform(runs.each);
   if (blockIdx.x == 0 && threadIdx.x == 0) *arguments().active = d.total > 0 ? runs.workers : 0;
   // neighbouring runs on one XCD: workgroup b runs on XCD b % 8
   const uint32_t per_xcd = (runs.workers + kXcds - 1) / kXcds;
@@ -358,9 +315,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   if (at >= end) return;
 
   // the sequence, key head and block that `at` lies in
-  uint32_t seq, head, block;
-  uint64_t item_first;  // the item's first tile, behind its own cost
-  Seq s;
+  const Seq* lds_seqs = d.each == 1 ? seqs : nullptr;
+  Item item;
   {
     const Attend a = arguments();
     uint32_t chunk = 0;  // the last thread's sequences that begin at or before it
@@ -368,39 +324,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     for (uint32_t step = F::kThreads / 2; step > 0; step /= 2)
       if (before[chunk + step] <= at) chunk += step;
     chunk = uniform(chunk);
-    seq = chunk * d.each;
-    uint64_t first = uniform(before[chunk]), cost;
-    for (;; ++seq) {  // `at` < the total: a sequence holds it
-      s = uniform(d.each == 1 ? seqs[seq] : seq_of<kRows>(a, seq));
-      cost = s.blocks ? head_cost<kRows, kTile>(a, s, lane) : 0;
-      if (at < first + cost * a.heads) break;
-      first += cost * a.heads;
-    }
-    head = uniform(static_cast<uint32_t>(quotient(at - first, cost)));
-    first += cost * head;
-    uint64_t rest = at - first;
-    if (a.seen) {
-      const uint32_t each = cost_of<kRows, kTile>(a, s, 0);
-      block = uniform(static_cast<uint32_t>(quotient(rest, each)));
-      item_first = first + static_cast<uint64_t>(block) * each;
-    } else {
-      for (block = 0;; block += kWave) {
-        const uint32_t mine = block + lane < s.blocks ? cost_of<kRows, kTile>(a, s, block + lane) : 0;
-        const uint64_t upto = sums_upto(mine, lane);
-        const uint64_t over = __ballot(upto > rest);
-        if (over != 0) {
-          const uint32_t l = static_cast<uint32_t>(__builtin_ctzll(over));
-          item_first = first + uniform(__shfl(upto - mine, l, 64));
-          block += l;
-          break;
-        }
-        const uint64_t all = uniform(__shfl(upto, 63, 64));
-        first += all;
-        rest -= all;
-      }
-    }
-    item_first = uniform(item_first + a.visit);
-    block = uniform(block);
+    if (!seek<kRows, kTile>(a, chunk * d.each, uniform(before[chunk]), at, Lanes<kRows>{a, lds_seqs, lane}, item)) return;
+    item.head = uniform(item.head);
+    item.block = uniform(item.block);
+    item.first = uniform(item.first);
   }
 
   // LDS places of the lane's shares: of the rows that it brings, of the key and of the values that it uses
@@ -423,13 +350,16 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   }
 
   if (threadIdx.x == 0) odd_there[0] = 0;
-  for (uint32_t turn = 0; at < end && item_first < end; turn ^= 1) {
+  for (uint32_t turn = 0; at < end && item.first < end; turn ^= 1) {
     const Attend a = arguments();
+    const Seq& s = item.s;
+    const uint32_t seq = item.seq, head = item.head, block = item.block;
+    const uint64_t item_first = item.first;
     const uint32_t rows = s.count * a.group, row0 = block * kRows, in_block = min(kRows, rows - row0);
     const uint32_t sees = uniform(visible(a, s, row0 + kRows));
     const uint32_t tiles = max(1u, (sees + kTile - 1) / kTile);
-    const uint32_t t_begin = uniform(at <= item_first ? 0u : static_cast<uint32_t>(at - item_first));
-    const uint32_t t_end = uniform(end - item_first < tiles ? static_cast<uint32_t>(end - item_first) : tiles);
+    const Share share(at, end, item_first, tiles);
+    const uint32_t t_begin = uniform(share.begin), t_end = uniform(share.end);
     // the lane's row, and what all rows of the workgroup and of the wave see for certain
     const uint32_t row = row0 + rw * 32 + r;
     const bool mine = rw * 32 + r < in_block;
@@ -1043,23 +973,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
     }
     // the next item
     at = item_first + t_end;
-    if (t_end == tiles) {
-      item_first = at + a.visit;
-      if (++block == s.blocks) {
-        block = 0;
-        if (++head == a.heads) {
-          head = 0;
-          if (at < end)
-            do {
-              ++seq;
-              s = uniform(d.each == 1 ? seqs[seq] : seq_of<kRows>(a, seq));
-            } while (s.blocks == 0);  // `at` < the total: one with tiles follows
-        }
-      }
-    }
+    if (t_end == tiles && !next_item(a, at, end, Lanes<kRows>{a, lds_seqs, lane}, item)) break;
   }
   // unless the last item goes on that began in this run
-  if (threadIdx.x == 0 && !(item_first >= runs.first(worker) && item_first < at)) arguments().splits[worker].last = 0;
+  if (threadIdx.x == 0 && !leaves_open(begin, at, item.first)) arguments().splits[worker].last = 0;
 }
 
 // Joins the parts of the items that were split. A workgroup takes a run of entries (few items lie evenly among these, so that
@@ -1079,7 +996,10 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
     const uint32_t each = (active + gridDim.x - 1) / gridDim.x, mine = blockIdx.x * each + i0 + lane;
     const bool have = i0 + lane < each && mine < active;
     const Split own = each == 1 ? guess : a.splits[have ? mine : 0];
-    for (uint64_t left = __ballot(have && own.last != 0); left != 0; left &= left - 1) {
+    // what no run has written, because lengths or starts changed under the call, is not taken for an entry outside the rows
+    const uint32_t room = own.token < a.tokens ? (a.tokens - own.token) * a.group : 0u;
+    const bool inside = own.last < active && own.head < a.heads && own.rows <= kRows && own.row < room && own.rows <= room - own.row;
+    for (uint64_t left = __ballot(have && own.last != 0 && inside); left != 0; left &= left - 1) {
       const uint32_t from = static_cast<uint32_t>(__builtin_ctzll(left)), first = blockIdx.x * each + i0 + from;
       const auto there = [&](uint32_t v) -> uint32_t { return __builtin_amdgcn_readlane(v, from); };
       const uint32_t last = there(own.last), token = there(own.token), row0 = there(own.row);

@@ -32,6 +32,11 @@ def test_checks(tmp_path):
     sanitized(tmp_path, "tree_calls_check", "zo_checks.cpp")
 
 
+def test_deal(tmp_path):
+    """The split of the tree attention's work over its workgroups, for random batches in every form's sizes."""
+    sanitized(tmp_path, "tree_deal_check")
+
+
 def test_a_walked_path_moves_once():
     """Moved twice, a path takes rows from where the first pass has put others: so a tensor that is listed twice may not."""
     cache, table, path = np.arange(4.0).reshape(1, 1, 4, 1), np.array([[0]]), np.array([[0, 2, 3]])
