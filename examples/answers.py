@@ -14,8 +14,9 @@ writes into it); each new token's queries and keys are normed, rotated and put i
 next token is drawn from the logits.
 
 With --drafted the clean answers are drafts of a probe's: the model reads several drafted tokens of every answer at once,
-draws behind each of them, and keeps the longest beginning that the draws agree with. The answers are the same ones, but for
-draws that the last digits of a sum decide. How many passes that saves is a matter of how alike the probes are: of 11, an
+draws behind each of them, and keeps the longest beginning that the draws agree with. The answers are the same ones up to
+rounding: in bf16 a draw among many tokens of nearly equal weight can be another one, and the answer goes on from there (at the defaults 204
+of 512 answers drafted by themselves; none at --temperature 0, none in fp32). How many passes that saves is a matter of how alike the probes are: of 11, an
 answer takes 3.0 at --temperature 0 --eps 1e-5 and 7.5 at --eps 1e-3, but all 11 at the defaults, where these random weights
 have no favourite token and eps is as large as they are.
 """

@@ -5,7 +5,9 @@
  * An objective that scores sampled answers draws nearly the same answers for every probe. Drawn with the same
  * random numbers (zo_draw is exact), an earlier answer is a draft of the next one: the model reads
  * all drafted tokens at once, a token is drawn behind each, and the longest beginning that the draws
- * agree with is kept. The answers are those of one token at a time.
+ * agree with is kept. The answers are those of one token at a time up to rounding: the logits of tokens that are read together
+ * come of other sums than those of one token, in the model's products as in the attention, and a draw that this decides is another
+ * one. Each token is a draw from the model's own logits behind the tokens before it.
  *
  * Conventions are those of zo_decode.h. The new tokens of all sequences lie packed, one sequence after another:
  * those of sequence s are starts[s] .. starts[s + 1] - 1 of `tokens`, its new token i is starts[s] + i. starts (int32 [seqs + 1])
