@@ -459,13 +459,13 @@ TreeShape tree_shape(uint32_t tokens, uint32_t seqs, uint32_t q_heads, uint32_t 
   TreeShape s = {};
   if (heads == 0 || q_heads % heads != 0 || q_heads == 0 || seqs == 0 || tokens == 0) return s;
   const uint64_t group = q_heads / heads, rows = (tokens * group + seqs - 1) / seqs;  // of a sequence, on average
-  // One row wave or more, us for 48 sequences of 500 to 4,000 tokens: bf16, heads of 128, 32 rows 104 | 120, 40 rows 134 | 123; of 64, 32
-  // rows 52 | 54, 40 rows 78 | 59; of 256, 32 rows 153 | 165, 40 rows 217 | 170; fp32, heads of 128, 64 rows 208 | 278, 96 rows 302 | 292;
-  // of 64, 64 rows 96 | 142, 128 rows 175 | 156. Keys and values of four waves' own tiles have to fit the LDS.
+  // One row wave or more, us for 48 sequences behind 500 to 4,000 tokens, 32 query heads on 8 (of 256: 16 on 4): bf16, heads of 128, 32 rows
+  // 109 | 117, 40 rows 143 | 119; of 64, 32 rows 47 | 49, 40 rows 74 | 61; of 256, 32 rows 142 | 147, 40 rows 209 | 152; fp32, heads of 128,
+  // 64 rows 372 | 498, 96 rows 544 | 511; of 64, 64 rows 162 | 253, 96 rows 244 | 260, 128 rows 309 | 267. With one sequence behind 1,037 it
+  // hardly counts (bf16, heads of 128: 40 rows 16.7 | 16.1, 128 rows 20 | 19). Keys and values of four waves' own tiles have to fit the LDS.
   const uint64_t few = dtype == ZO_F32 ? 64 : 32;
-  // Eight row waves or four, bf16: heads of 128, 48 sequences, 40 rows 125 | 123, 128 rows 143 | 142, 384 rows 277 | 314; four sequences of
-  // 2,000 tokens, 128 rows 26 | 39 (fewer parts to join); of 64, 48 sequences, 128 rows 86 | 80, 384 rows 182 | 174, eight prompts of 4,096
-  // rows 94 | 107.
+  // Eight row waves or four, bf16: heads of 128, 48 sequences, 40 rows 119 | 122, 384 rows 313 | 343; four sequences of 2,000 tokens, 128 rows
+  // 26 | 40 (fewer parts to join); of 64, 48 sequences, 128 rows 85 | 75, 384 rows 194 | 189, eight prompts of 4,096 rows 100 | 103.
   const uint64_t many = dim > 64 ? 0 : 1024;
   if (rows <= few && dim * elem_bytes(dtype) <= 512)
     s.row_waves = 1;
@@ -480,7 +480,7 @@ int check_tree_attend(const zo_tree_attention& a) {
   if (!dtype_ok(a.dtype)) return ZO_ERR_ARG;
   const size_t elem = elem_bytes(a.dtype);
   if (a.cache.heads == 0 || a.cache.heads > 0xFFFFu || a.q_heads > 0xFFFFu || a.q_heads % a.cache.heads != 0) return ZO_ERR_ARG;
-  // a workgroup for each item, 2^32 threads at most in a launch
+  // rows are numbered below 2^24, and the tiles of all items below 2^52
   if (static_cast<uint64_t>(a.tokens) * std::max(a.q_heads, 1u) >= (1u << 24)) return ZO_ERR_ARG;
   if (static_cast<uint64_t>(a.table.seqs) * a.cache.heads >= (1u << 23)) return ZO_ERR_ARG;
   if (!std::isfinite(a.scale)) return ZO_ERR_NONFINITE;

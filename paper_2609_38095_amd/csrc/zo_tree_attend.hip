@@ -28,10 +28,10 @@
 // Rounding. fp32 sums and bounds. bf16 weights are a sum of two bf16 (2^-16 of a weight is lost), two products with the values each: weights
 // rounded once would be 2^-8 of the weighted magnitudes, as much as the output's own rounding, for 1,060 instead of 1,342 us (prompts).
 //
-// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,342 us (1.16 PFLOP/s with the second
-// parts' products, what a large matrix product reaches); 48 trees of up to 64 behind up to 4,096, 205 us (2.9 TB/s); one tree of 12 behind
-// 1,037, 16.5 us (latencies: the deal 2 us, first loads 3, results 3, the join 4). fp32 trees, 16 of up to 23, 32 heads of 64 behind up to
-// 2,050: 85 us (4.4 TB/s).
+// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,342 to 1,377 us (1.13 to 1.16 PFLOP/s
+// with the second parts' products; a large matrix product reaches 1.20); 48 trees of up to 64 behind up to 4,096, 204 to 207 us (2.9 TB/s:
+// 1.5 to 2.5 us a tile, 14 an item, 15 the join); one tree of 12 behind 1,037, 15.8 to 16.5 us (latencies: the deal 2.6 us, first loads 4,
+// results 5, the join 4). fp32 trees, 16 of up to 23, 32 heads of 64 behind up to 2,050: 85 to 86 us (4.4 TB/s).
 
 #include <algorithm>
 #include <cmath>
@@ -148,7 +148,9 @@ __device__ Deal deal(const Attend& a, uint64_t* before, Seq* seqs) {
     Seq s = {};
     if (seq < a.seqs) s = seq_of<kRows>(a, seq);
     if (d.each == 1) seqs[threadIdx.x] = s;
-    constexpr uint32_t kFew = 8;  // blocks that a thread counts by itself; a longer sequence's by the whole wave
+    // Blocks that a thread counts by itself; a longer sequence's by the whole wave. 300 chains of 100, 32 heads on 8 of 64: 223 us, with
+    // all by the wave 281, with up to 64 by a thread 224.
+    constexpr uint32_t kFew = 8;
     if (a.seen) {
       if (s.blocks) cost += static_cast<uint64_t>(s.blocks) * cost_of<kRows, kTile>(a, s, 0);
     } else {
@@ -257,8 +259,8 @@ struct Form {
   static constexpr uint32_t kBufferBytes = 2 * kTile * kRowBytes;
   static constexpr uint32_t kLds = kBuffers * kBufferBytes;
   static constexpr bool kPiped = kRowWaves > 1 && sizeof(T) == 2 && kBlocks == 2;
-  // An item's own time in tiles. 0: prompts 1,082 us, 48 trees 190, fp32 trees (one row wave) 91; 2: 1,069, 180, 86; 4: 1,038, 171, 90;
-  // 6: 1,045, 171, 91; 1: fp32 trees 85.
+  // An item's own time in tiles. 0: prompts 1,415 us, 48 trees 229, fp32 trees (one row wave) 93; 1: 1,399, 217, 86; 2: 1,381, 221, 87;
+  // 4: 1,359, 204, 90; 6: 1,351, 205, 91.
   static constexpr uint32_t kVisit = kRowWaves > 1 ? 4 : 1;
   static constexpr uint32_t kSimdWaves = kRowBytes <= 256 ? 2 : 1;
   static_assert(kLoadRows <= 8 && kStageRows % kLoadRows == 0, "a load's rows lie in one sixteen");
@@ -276,7 +278,7 @@ template <int kLeft>
 __device__ __forceinline__ void loads_left() {
   asm volatile("s_waitcnt vmcnt(%0)" : : "n"(kLeft) : "memory");
   // The same, for the compiler: what it brought back from scratch memory before a loop is there as well, and it adds no waits inside the
-  // loop, which would be for all of the wave's loads (48 trees 199 -> 173 us).
+  // loop, which would be for all of the wave's loads (48 trees, weights of one part: 199 -> 173 us).
   __builtin_amdgcn_s_waitcnt(kLeft % 16 | 7 << 4 | 15 << 8 | kLeft / 16 << 14);
 }
 
@@ -335,7 +337,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
   char* own = lds + kw * 2 * kKeys * kRowBytes;  // the keys of the waves that share them, and their values behind these
   // Rows are swizzled by 16-byte chunks: eight neighbouring rows' same chunks (the keys' reads), and four rows' four chunks (the values')
   // lie in different banks. The keys' still meet a third of the time: lanes are served in groups of rows 0-3, 12-15, 20-23 and 24-27. A swizzle of
-  // theirs over sixteen rows ends that, and the offsets of two swizzles cost registers: prompts 1,074 -> 1,069 us, 48 trees 175 -> 178.
+  // theirs over sixteen rows ends that, and the offsets of two swizzles cost registers (weights of one part: prompts 1,074 -> 1,069 us, 48
+  // trees 175 -> 178).
   const auto swizzle = [](uint32_t row) {
     return kChunks >= 16 ? row % 4 * 4 + row / 4 % 2 : row / 2 % 2 * 4 + row / 4 % 2;
   };
@@ -1045,7 +1048,7 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Attend a) {
 // Any head size, page size and alignment: a workgroup has a row at a time, its waves every fourth 64 keys. 64 keys' scores at once, one
 // in each lane, then their values, a dim in each lane (and the dims 64, 128 and 192 behind it); each 64's sum is added to what was
 // there, and the waves join at the end. A token that the row does not see is not read. Every row reads its keys anew. 40 new tokens of
-// 4 heads of 96 behind 1,000: 73 us in bf16, 47 in fp32 (heads of 128 by the other kernel: 17 and 21).
+// 4 heads of 96 behind 1,000: 72 us in bf16, 48 in fp32 (heads of 128 by the other kernel: 17 and 23).
 template <class S>
 __global__ void __launch_bounds__(kThreads) plain_kernel(const Attend a) {
   typedef typename S::storage T;
@@ -1185,12 +1188,13 @@ int launch(Attend& a, hipStream_t st) {
                           F::kLds) != hipSuccess)
     return ZO_ERR_HIP;
   const uint64_t items = (static_cast<uint64_t>(a.tokens) * a.group / F::kRows + a.seqs) * a.heads;  // there are no more
-  // with few items all workgroups have one or two, and what an item costs would only leave some without a tile
+  // with few items all workgroups have one or two, and what an item costs would only leave some without a tile: trees of 12 behind 1,500, 32 heads
+  // on 8 of 128, 4 of them 20.3 us without and 22.4 with, 8: 24.3 and 25.2 (12: 34.8 and 31.5, 16: 31.7 and 33.8, 24: 44.6 and 43.8)
   a.visit = items * 2 >= a.workers ? F::kVisit : 0;
   attend_kernel<S, kDim, kRowWaves><<<dim3(a.workers), dim3(F::kThreads), F::kLds, st>>>(a);
   const int rc = launched();
   if (rc != ZO_OK) return rc;
-  // slices where an item has several parts
+  // slices where an item has several parts: of the same trees, one 16.7 us with and 17.4 without, 4 20.1 both, 8 25.3 and 24.0, 16 36.7 and 33.9
   const uint32_t most = static_cast<uint32_t>(std::min<uint64_t>(a.workers, items));
   if (items * 6 <= a.workers)
     join_kernel<S, kDim, F::kRows, 4><<<dim3(most, std::min(32u, F::kRows * kDim / 256)), dim3(kThreads), 0, st>>>(a);
