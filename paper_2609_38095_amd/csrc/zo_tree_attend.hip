@@ -28,7 +28,7 @@
 // Rounding. fp32 sums and bounds. bf16 weights are a sum of two bf16 (2^-16 of a weight is lost), two products with the values each: weights
 // rounded once would be 2^-8 of the weighted magnitudes, as much as the output's own rounding, for 1,060 instead of 1,342 us (prompts).
 //
-// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,342 to 1,377 us (1.13 to 1.16 PFLOP/s
+// Measured, heads of 128: four prompts of up to 6,001 tokens of 32 heads on 8 behind up to 2,048, 1,342 to 1,392 us (1.12 to 1.16 PFLOP/s
 // with the second parts' products; a large matrix product reaches 1.20); 48 trees of up to 64 behind up to 4,096, 204 to 207 us (2.9 TB/s:
 // 1.5 to 2.5 us a tile, 14 an item, 15 the join); one tree of 12 behind 1,037, 15.8 to 16.5 us (latencies: the deal 2.6 us, first loads 4,
 // results 5, the join 4). fp32 trees, 16 of up to 23, 32 heads of 64 behind up to 2,050: 85 to 86 us (4.4 TB/s).
@@ -52,6 +52,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr uint32_t kThreads = 256, kWave = 64, kWaves = kThreads / kWave, kXcds = 8;
 constexpr float kLazy = 8.0f;  // how far (in powers of two) the bound of the scores is set above their maximum
+// Scores from here on are rounded before the bound is taken from them. Below, an unrounded product differs from its rounding, which the bound is
+// made of, by half at most; at 2^125 all weights of a row would be 0 or infinite for that.
+constexpr float kLarge = 16777216.0f;
 
 // An item that was split: its parts are those of the workgroup that this is the entry of, in slot 1, and of the ones up to `last`, in
 // slot 0. At most one item that is split begins in a workgroup's run. last = 0: none does. Written by the workgroup of the item's last
@@ -477,7 +480,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
       for (uint32_t c = 0; c < kSteps; ++c) {
         q[c] = u32x4{0, 0, 0, 0};
-        if (mine) q[c] = *reinterpret_cast<const u32x4_any*>(qp + (2 * c + g) * 16);
+        if (mine && a.scale != 0.0f) q[c] = *reinterpret_cast<const u32x4_any*>(qp + (2 * c + g) * 16);
         if (a.scale < 0.0f) q[c] ^= kWide ? 0x80000000u : 0x80008000u;
       }
     }
@@ -506,8 +509,13 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
       for (int i = 0; i < 16; ++i) x[i] = shown >> (8 * (i / 4) + i % 4) & 1 ? x[i] : -INFINITY;
     };
-    // a scale of 0 would make a NaN of a masked score: all weights are 1 with the smallest one as well
-    const float scale = fmaxf(fabsf(a.scale), 1.17549435e-38f);
+    // a scale of 0 would make a NaN of a masked score: the queries are 0 instead
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    // What the lane's scores of this block are still multiplied by, and whether some are large or may meet a large bound. Looked at where the
+    // bound rises, and in each block from then on that some are: for every block it costs prompts 6 %.
+    float times = scale;
+    bool some_large = false;
+    const auto is_large = [](float v) { return fabsf(v) >= kLarge && fabsf(v) < INFINITY; };
 
     float m = -INFINITY, l = 0.0f;
     f32x16 o[kOuts];
@@ -579,7 +587,10 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
         for (int i = 1; i < 16; ++i) top = fmaxf(top, x[i]);
         top *= scale;
-        if (__any(top > m)) {
+        if (__any(top > m) || some_large) {
+          const bool large = is_large(top);
+          x *= large ? scale : 1.0f;
+          times = large ? 1.0f : scale;
           top = fmaxf(top, __shfl_xor(top, 32, 64));
           top = fmaxf(__builtin_ceilf(top) + kLazy, m);
           const float by = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);  // m = -inf: 0
@@ -592,6 +603,7 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
             rests[i] = pack_bf16x2(__uint_as_float(rests[i] << 16) * by, __uint_as_float(rests[i] & 0xFFFF0000u) * by);
           }
           m = top;
+          some_large = __any(large || is_large(m));
         }
       };
       // One step: the scores of block kb of a tile, the products of the waiting weights with the values of block vb of a tile (kValues),
@@ -612,8 +624,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
               kf[n % kAhead] = read_key(kb + 1, n + kAhead - kSteps);
           }
           const bool weighs = kValues && n < 2 * kOuts;
-          float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], scale, -ref));
-          float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], scale, -ref));
+          float p0 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], times, -ref));
+          float p1 = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], times, -ref));
           asm volatile("" : "+v"(p0), "+v"(p1));  // here, under the products, and not where they are used
           __builtin_amdgcn_sched_barrier(0);
           if (weighs) weigh(n, weights);
@@ -799,7 +811,11 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
             for (int i = 0; i < 16; ++i) top = fmaxf(top, x[b][i]);
           top *= scale;
-          if (__any(top > m)) {
+          if (__any(top > m) || some_large) {
+            const bool large = is_large(top);
+#pragma unroll
+            for (uint32_t b = 0; b < kBlocks; ++b) x[b] *= large ? scale : 1.0f;
+            times = large ? 1.0f : scale;
             top = fmaxf(top, __shfl_xor(top, 32, 64));
             top = fmaxf(top + kLazy, m);
             const float by = top == m ? 1.0f : __builtin_amdgcn_exp2f(m - top);  // m = -inf: 0
@@ -807,13 +823,14 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
 #pragma unroll
             for (uint32_t e = 0; e < kOuts; ++e) o[e] *= by;
             m = top;
+            some_large = __any(large || is_large(m));
           }
           const float ref = m == -INFINITY ? 0.0f : m;
 #pragma unroll
           for (uint32_t b = 0; b < kBlocks; ++b) {
             float p[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], scale, -ref));
+            for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[b][i], times, -ref));
             l += ((p[0] + p[1]) + (p[2] + p[3]) + ((p[4] + p[5]) + (p[6] + p[7]))) + ((p[8] + p[9]) + (p[10] + p[11]) + ((p[12] + p[13]) + (p[14] + p[15])));
             const char* vb = values + b * 32 * kRowBytes;
             if constexpr (kWide) {

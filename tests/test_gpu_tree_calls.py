@@ -6,7 +6,7 @@ import torch
 
 import paper_2609_38095_amd as zo
 from oracle import tree as oracle
-from test_gpu_tree import cache_of, dev, ints, normal, wide
+from test_gpu_tree import E, attend_case, cache_of, dev, ints, near, normal, starts_of, trees, wide
 
 pytestmark = pytest.mark.gpu
 
@@ -72,3 +72,47 @@ def test_the_walk_ends_where_the_masks_do(counts, words, kind):
     for wrong in (-1, 9):
         with pytest.raises(zo.ZoError):
             zo.zo_tree_accept(*args, 800, own, words=wrong)
+
+
+# ---- attention
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 48), (256, 32), (96, 16)])
+@pytest.mark.parametrize("nodes", [3, 70])
+@pytest.mark.parametrize("score", [-3e38, 3e38, 7e9, -7e9, 2.0 ** 25 + 2.0 ** 18])
+def test_scores_of_any_finite_size(score, nodes, dim, page, dtype):
+    """Equal scores, one product each, so equal weights whatever a score's rounding: the mean of the values, and no score's own error. Every seventh
+    key's is far below and has no part."""
+    cached, counts, scale = [100, 0], [nodes] * 2, 0.2
+    q, kc, vc, table, used = attend_case(cached, counts, 4, 2, dim, page, "heads", dtype)
+    q.zero_(), kc.zero_()
+    q[..., 0], kc[..., 0] = 1.0, score
+    for s, n in enumerate(used):
+        for j in range(6, n, 7):
+            kc[int(table[s, j // page]), :, j % page, 0] = -abs(score) * 1.125
+    starts = starts_of(counts)
+    for seen in (None, oracle.lay(starts, cached, 2 * nodes, trees(counts, 3), 2)[3]):
+        want, lse, mag, _ = oracle.attend(wide(q), wide(kc), wide(vc), table, cached, starts, seen, scale)
+        out, sums = zo.zo_tree_attend(q, kc, vc, dev(table), ints(cached), dev(starts), None if seen is None else dev(seen), scale, lse=True)
+        near(out, want, mag, 170 / 8 + 64 + (2.0 ** 8 if dtype == "bf16" else 0), dtype)
+        # the score, times scale log2(e) and ln 2 in fp32, scale itself rounded: below 8 e
+        assert np.all(np.abs(wide(sums) - lse) <= 8 * E * np.abs(lse) + 1e-5)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 48), (256, 32), (96, 16)])
+@pytest.mark.parametrize("nodes", [3, 70])
+@pytest.mark.parametrize("scale", [0.0, 1e-40])
+def test_scales_of_0_and_below_the_normal_ones(scale, nodes, dim, page, dtype):
+    """Scores of single products up to 3e38 times a scale that is nothing, or next to it. The latter is a multiple of 2^-149, as its product with
+    log2(e) is: scores of up to 0.04 are off by 2^-149 / 1e-40 of themselves, which moves a weight by 14 e at most, twice."""
+    cached, counts = [100, 0], [nodes] * 2
+    q, kc, vc, table, _ = attend_case(cached, counts, 4, 2, dim, page, "heads", dtype)
+    q.zero_()
+    q[..., 0] = 1.0
+    kc[..., 0] = (kc[..., 0].clamp(-3, 3) * 1e38).to(kc.dtype)
+    starts = starts_of(counts)
+    want, lse, mag, _ = oracle.attend(wide(q), wide(kc), wide(vc), table, cached, starts, None, scale)
+    out, sums = zo.zo_tree_attend(q, kc, vc, dev(table), ints(cached), dev(starts), scale=scale, lse=True)
+    near(out, want, mag, 170 / 8 + 64 + 28 + (2.0 ** 8 if dtype == "bf16" else 0), dtype)
+    assert np.all(np.abs(wide(sums) - lse) <= 8 * E * np.abs(lse) + 64 * E)

@@ -60,6 +60,25 @@ def test_rows_behind_a_long_context(counts, dim):
                 near(out[int(starts[s]) + i, h], wide(w @ v[h // 2, :live]), wide(w @ v[h // 2, :live].abs()), bound(dim, live, big, "bf16"), "bf16")
 
 
+@pytest.mark.parametrize("dim,page", [(64, 16), (128, 32), (256, 16)])
+@pytest.mark.parametrize("nodes", [3, 64])
+@pytest.mark.parametrize("rise", [0.25, -0.25, 1.0])
+def test_weights_that_wait_while_the_bound_rises(dim, page, nodes, rise):
+    """Scores that rise (or fall) with every key: both parts of the weights that wait are rescaled with the sums."""
+    cached, counts = [180, 20], [nodes] * 2
+    q, kc, vc, table, used = attend_case(cached, counts, 8, 2, dim, page, "heads", "bf16")
+    q[..., 0] = 1.0
+    kc *= 0.05
+    for s, n in enumerate(used):
+        for j in range(n):
+            kc[int(table[s, j // page]), :, j % page, 0] = rise * j
+    starts = starts_of(counts)
+    want, _, mag, big = oracle.attend(wide(q), wide(kc), wide(vc), table, cached, starts, None, 0.4)
+    spoil(kc, vc, table, used, page)
+    out = zo.zo_tree_attend(q, kc, vc, dev(table), ints(cached), dev(starts), scale=0.4)
+    near(out, want, mag, steps_of(dim, 250, big, page, "heads")[..., None], "bf16")
+
+
 @pytest.mark.parametrize("dim,page", [(64, 16), (128, 32), (256, 16), (96, 16), (64, 5)])
 @pytest.mark.parametrize("nodes", [3, 64])
 def test_a_row_that_sees_one_key_has_its_value(dim, page, nodes):
