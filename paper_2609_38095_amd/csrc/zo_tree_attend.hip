@@ -607,8 +607,8 @@ __global__ void __launch_bounds__((Form<S, kDim, kRowWaves>::kThreads), (Form<S,
         }
       };
       // One step: the scores of block kb of a tile, the products of the waiting weights with the values of block vb of a tile (kValues),
-      // this block's weights. A third of two weights' arithmetic lies behind each product (in the compiler's own order 3 % more). The first operands are there; the next step's first ones (of blocks kb + 1 and vb + 1) are read at its end
-      // (kNext).
+      // this block's weights. A third of two weights' arithmetic lies behind each product (in the compiler's own order 3 % more). The first
+      // operands are there; the next step's first ones (of blocks kb + 1 and vb + 1) are read at its end (kNext).
       const auto step = [&](auto scores, auto values, auto next, uint32_t kb, uint32_t vb) {
         constexpr bool kScores = scores.value, kValues = values.value, kNext = next.value;
         f32x16 y = {};

@@ -116,3 +116,29 @@ def test_scales_of_0_and_below_the_normal_ones(scale, nodes, dim, page, dtype):
     out, sums = zo.zo_tree_attend(q, kc, vc, dev(table), ints(cached), dev(starts), scale=scale, lse=True)
     near(out, want, mag, 170 / 8 + 64 + 28 + (2.0 ** 8 if dtype == "bf16" else 0), dtype)
     assert np.all(np.abs(wide(sums) - lse) <= 8 * E * np.abs(lse) + 64 * E)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,nodes", [(64, 3), (64, 60), (128, 3), (128, 60), (256, 30), (40, 9)])
+def test_queries_results_masks_and_tables_may_be_views(dim, nodes, dtype):
+    """Rows that begin at any element, heads and tokens any distance apart, masks and a table of wider tensors: the bits of a call with tensors of
+    their own, and nothing beside the result's rows is written."""
+    cached, counts, hq, hk, page = [70, 200], [nodes, nodes + 1], 4, 2, 16
+    q, kc, vc, table, _ = attend_case(cached, counts, hq, hk, dim, page, "heads", dtype)
+    n, starts = sum(counts), dev(starts_of(counts))
+    seen = dev(oracle.lay(starts_of(counts), cached, n, trees(counts, 3), 2)[3])
+    lengths, own_table = ints(cached), dev(table)
+    want, sums = zo.zo_tree_attend(q, kc, vc, own_table, lengths, starts, seen, lse=True)
+    wide_q = torch.zeros(n, hq + 3, dim + 5, dtype=q.dtype, device="cuda")
+    wide_q[:, 1:1 + hq, 3:3 + dim] = q
+    wide_seen = torch.full((n, 5), -1, dtype=torch.int64, device="cuda")
+    wide_seen[:, 2:4] = seen
+    wide_table = torch.full((2, table.shape[1] + 7), 2 ** 31 - 1, dtype=torch.int32, device="cuda")
+    wide_table[:, 3:3 + table.shape[1]] = own_table
+    buffer = torch.full((hq + 1, n + 2, dim + 3), 7.0, dtype=q.dtype, device="cuda")
+    out = buffer[:hq, 1:1 + n, 1:1 + dim].transpose(0, 1)
+    got, got_sums = zo.zo_tree_attend(wide_q[:, 1:1 + hq, 3:3 + dim], kc, vc, wide_table[:, 3:3 + table.shape[1]], lengths, starts, wide_seen[:, 2:4],
+                                      out=out, lse=True)
+    assert got.data_ptr() == out.data_ptr() and torch.equal(out, want) and torch.equal(got_sums, sums)
+    out.fill_(7.0)
+    assert bool((buffer == 7.0).all())
